@@ -277,6 +277,77 @@ ra_status ra_decode_step_q8(const void* q, const ra_index* idx, const void* K, c
                             int topk, int ef, int expand, void* stream, float* out, float* lse,
                             int32_t* ids, ra_stats* stats);
 
+/* ---- a cache in 4 bits, and the tokens that enter a cache -----------------------------
+ *
+ * A row of 128 values in 4 bits is 64 bytes of codes and 4 scale bytes, one per block of 32 dimensions:
+ *     codes  [n_seq][n_kv_heads][kv_stride][64] uint8, 16-byte aligned; dimension 2 i in the low half of byte i,
+ *     scale  [n_seq][n_kv_heads][kv_stride][4]  uint8, 4-byte aligned;
+ * a code is a sign (bit 3) and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6, a scale byte b stands for 2^(b - 127), 255 for NaN
+ * (the E2M1 and E8M0 formats of the OCP microscaling specification, which the matrix part of a compute unit converts
+ * by itself). kv_stride is the capacity: rows from one head to the next.
+ * Written here, the scale of a block is the least power of two with which no value exceeds 6 (at least 2^-125), and a
+ * value becomes the nearest code, ties to the even one. A block with a NaN, an infinity or a magnitude of 2^127 or more
+ * has scale byte 255 and codes of zero: all its values read as NaN.
+ *
+ * Where a call takes `first` and `n_new` (device int32 [n_seq], each may be NULL: 0, and T), sequence s has
+ * min(n_new[s], T) new tokens, token t of them has the position first[s] + t, and that is its row in the caches. Rows outside
+ * a cache's capacity, or below 0, are neither read nor written, and rows of other tokens stay as they are. Being device memory, both can
+ * be advanced between the replays of a captured graph. */
+
+/* The tokens that enter a cache, from the rows the projections have written: norm of every query and key head, position
+ * rotation, and the new rows of the caches, in one pass. Per head of a token, x of d = 128 values:
+ *     norm      n = x / sqrt(mean(x^2) + eps) * weight      (weight [128] of type dt; NULL: n = x)
+ *     rotation  of the first rot_dim dimensions (a multiple of 16, 0 .. 128) by the angles a_i = position * inv_freq[i],
+ *               i < rot_dim / 2: (n_j, n_k) becomes (n_j cos a_i - n_k sin a_i, n_k cos a_i + n_j sin a_i) for the pair
+ *               (j, k) = (i, i + rot_dim / 2), or with `interleaved` (2 i, 2 i + 1)
+ * and one rounding to dt. Values are copied. The mean is taken in 64 bits and angles, their sines and cosines are computed in 64
+ * bits (a position of a million times a frequency in 32 bits is off by a tenth of a radian); what follows is float32.
+ *   q_in, k_in, v_in  [n_seq][T][heads][128] of type dt, the heads of a token side by side, tokens q_row, k_row and v_row
+ *                     elements apart (the three may be parts of one buffer); each may be NULL with its outputs
+ *   inv_freq          device float32 [rot_dim / 2], NULL with rot_dim 0
+ *   q_out             [n_seq][n_q_heads][T][128], with T = 1 the q of the attention calls; rows t >= n_new[s] stay as they are
+ *   K, V              caches [n_seq][n_kv_heads][kv_stride][128] of type dt, each may be NULL
+ *   K4, K4s, V4, V4s  caches in 4 bits of capacity kv4_stride, codes and scale of each NULL or given: the rows of K and V (as
+ *                     rounded to dt) in 4 bits. (An index is built over a K of exactly N rows; the cache beside it has room to grow.)
+ * Outputs must not overlap inputs. Inputs, q_out, K and V 16-byte aligned, rows apart by a multiple of 16 bytes. */
+ra_status ra_append_tokens(const void* q_in, const void* k_in, const void* v_in, ra_dtype dt, int n_seq, int n_q_heads,
+                           int n_kv_heads, int64_t T, int d, int64_t q_row, int64_t k_row, int64_t v_row,
+                           const void* q_weight, const void* k_weight, double eps, const float* inv_freq, int rot_dim,
+                           int interleaved, const int32_t* first, const int32_t* n_new, int64_t kv_stride,
+                           int64_t kv4_stride, void* stream, void* q_out, void* K, void* V, uint8_t* K4, uint8_t* K4s, uint8_t* V4, uint8_t* V4s);
+
+/* Rows into 4 bits: X [n_seq][n_kv_heads][T][128] (dt, 16-byte aligned) -> rows first[s] + t, t < n_new[s], of codes and scale. */
+ra_status ra_quantize_kv4(const void* X, ra_dtype dt, int n_seq, int n_kv_heads, int64_t T, int d, const int32_t* first,
+                          const int32_t* n_new, int64_t kv_stride, void* stream, uint8_t* codes, uint8_t* scale);
+
+/* And back: rows first[s] + t, t < T -> X [n_seq][n_kv_heads][T][128] (dt, 16-byte aligned), the values they stand for, exactly
+ * (bfloat16 and float32 hold all of them). Rows outside [0, kv_stride) come as zeroes. What an index is built
+ * from again where the cache is kept in 4 bits only. */
+ra_status ra_dequantize_kv4(const uint8_t* codes, const uint8_t* scale, ra_dtype dt, int n_seq, int n_kv_heads, int64_t T, int d,
+                            const int32_t* first, int64_t kv_stride, void* stream, void* X);
+
+/* ra_full_attention over a cache in 4 bits: q [n_seq][n_q_heads][128] of type dt; rows [0, n) of sequence s, n =
+ * min(n_tokens[s], N) (device int32; NULL: N for every sequence). A sequence without rows gets out = 0 and lse = -inf. Rows
+ * from n on are not looked at. float32 accumulation; the weights of the softmax meet the values with 16 bits (dt = bfloat16)
+ * or 24 (float32) of mantissa.
+ * workspace: device memory of at least ra_full_attention_q4_workspace_bytes(...) bytes, 16-byte aligned, which nothing else may use
+ * until the call has run; it needs no initialisation. */
+size_t ra_full_attention_q4_workspace_bytes(ra_dtype dt, int n_seq, int n_q_heads, int n_kv_heads, int64_t N);
+ra_status ra_full_attention_q4(const void* q, ra_dtype dt, const uint8_t* K4, const uint8_t* K4s, const uint8_t* V4,
+                               const uint8_t* V4s, int n_seq, int n_q_heads, int n_kv_heads, int64_t N, int64_t kv_stride,
+                               int d, const int32_t* n_tokens, void* workspace, size_t workspace_bytes, void* stream,
+                               float* out, float* lse);
+
+/* ra_attend over a cache in 4 bits (what follows ra_search or ra_search_q8 where no other cache is kept): Eq. 2 over Omega = ids
+ * and over W, their combination by Eq. 4-5 into out/lse, and the four partial outputs, each of which may be NULL. N >= the
+ * index's N tokens are in the cache, N <= kv_stride; as in ra_decode_step_grown W = [0, sink) u [min(N - window, N_index), N).
+ * ids must not contain members of W; -1 and ids >= N are skipped. Errors as for ra_attend. Calls on one handle share its workspace:
+ * calls that overlap in time on one handle race. */
+ra_status ra_attend_q4(const void* q, const ra_index* idx, ra_dtype dt, const uint8_t* K4, const uint8_t* K4s,
+                       const uint8_t* V4, const uint8_t* V4s, int64_t N, int64_t kv_stride, int sink, int window, int topk,
+                       const int32_t* ids, void* stream, float* out, float* lse, float* o_omega, float* lse_omega,
+                       float* o_w, float* lse_w);
+
 /* what: 0 n_seq, 1 n_q_heads, 2 n_kv_heads, 3 N, 4 deg, 5 bytes of device memory owned,
  * 6 whether ra_decode_step will use helper workgroups (1 / 0; synchronises the device),
  * 7 the seed-set size in use (RA_CFG_SEEDS; 0: single entry point),

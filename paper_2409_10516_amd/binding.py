@@ -112,6 +112,19 @@ def lib() -> C.CDLL:
     L.ra_hbm_gather_probe.argtypes = [vp, C.c_size_t, C.c_size_t, C.c_uint32, vp, vp]
     L.ra_full_attention.argtypes = [vp, vp, vp, i32, i32, i32, i32, i64, i32, vp, C.c_size_t, vp, vp, vp]
     L.ra_full_attention.restype = i32
+    L.ra_append_tokens.argtypes = [vp, vp, vp, i32, i32, i32, i32, i64, i32, i64, i64, i64, vp, vp, C.c_double, vp, i32, i32, vp, vp,
+                                   i64, i64, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.ra_append_tokens.restype = i32
+    L.ra_quantize_kv4.argtypes = [vp, i32, i32, i32, i64, i32, vp, vp, i64, vp, vp, vp]
+    L.ra_quantize_kv4.restype = i32
+    L.ra_dequantize_kv4.argtypes = [vp, vp, i32, i32, i32, i64, i32, vp, i64, vp, vp]
+    L.ra_dequantize_kv4.restype = i32
+    L.ra_full_attention_q4_workspace_bytes.argtypes = [i32, i32, i32, i32, i64]
+    L.ra_full_attention_q4_workspace_bytes.restype = C.c_size_t
+    L.ra_full_attention_q4.argtypes = [vp, i32, vp, vp, vp, vp, i32, i32, i32, i64, i64, i32, vp, vp, C.c_size_t, vp, vp, vp]
+    L.ra_full_attention_q4.restype = i32
+    L.ra_attend_q4.argtypes = [vp, vp, i32, vp, vp, vp, vp, i64, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.ra_attend_q4.restype = i32
     for name in ("ra_knn", "ra_project", "ra_build_index", "ra_search", "ra_attend",
                  "ra_attend_noalloc", "ra_hbm_read_probe", "ra_hbm_gather_probe", "ra_decode_step", "ra_index_import",
                  "ra_index_export"):
@@ -165,6 +178,34 @@ def _stream(stream) -> int:
         return stream.cuda_stream
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     return torch.cuda.current_stream().cuda_stream if raw is None else raw(torch.cuda.current_device())
+
+
+def _here(*ts):
+    """The given tensors live on the current device, where the call is launched."""
+    here = torch.cuda.current_device()
+    for t in ts:
+        if t is not None and (not t.is_cuda or t.device.index != here):
+            raise ValueError(f"tensors must live on the current GPU ({here}), not on {t.device}")
+
+
+def _ints(t: Optional[torch.Tensor], n_seq: int, name: str):
+    if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != (n_seq,) or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous int32 tensor [n_seq]")
+
+
+def _kv4(x4, n_seq: int, n_kv: int, name: str, kv_stride: Optional[int] = None) -> int:
+    """Checks a cache in 4 bits (codes, scale) -> its capacity in rows."""
+    codes, scale = x4
+    rows = codes.shape[2] if codes.dim() == 4 else -1
+    if tuple(codes.shape) != (n_seq, n_kv, rows, 64) or tuple(scale.shape) != (n_seq, n_kv, rows, 4):
+        raise ValueError(f"{name} must be codes [n_seq][n_kv][capacity][64] and scale [n_seq][n_kv][capacity][4]")
+    if codes.dtype != torch.uint8 or scale.dtype != torch.uint8:
+        raise TypeError(f"{name} must be uint8")
+    if not codes.is_contiguous() or not scale.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if kv_stride is not None and rows != kv_stride:
+        raise ValueError(f"{name} holds {rows} rows per head, not {kv_stride}")
+    return rows
 
 
 class Index:
@@ -458,3 +499,163 @@ def ra_full_attention(q, K, V, stream=None, workspace=None, out=None, lse=None):
                                    _ptr(workspace), workspace.numel(), _stream(stream), _ptr(out),
                                    _ptr(lse)))
     return out, lse
+
+
+def ra_append_tokens(q, k, v, first, *, n_new=None, q_weight=None, k_weight=None, eps: float = 1e-6, inv_freq=None,
+                     interleaved: bool = False, q_out=None, K=None, V=None, k4=None, v4=None, stream=None):
+    """The tokens that enter a cache: norm of every query and key head (weight [128], None: no norm), rotation of the first
+    2 * len(inv_freq) dimensions at positions first[s] + t, new rows of the caches. q, k, v: [n_seq][T][heads][128] (any may be
+    None), the heads of a token side by side, tokens any multiple of 16 bytes apart, so that they may be parts of one buffer. first,
+    n_new: int32 [n_seq] on the GPU (None: 0, and T). K, V: caches [n_seq][n_kv][capacity][128]; k4, v4: caches in 4 bits, of a
+    capacity of their own, (codes, scale) as from ra_quantize_kv4. -> q_out [n_seq][n_q][T][128] (None without q); where tokens are fewer than T and no q_out is
+    given, the rows behind the last one are zero."""
+    some = next((t for t in (q, k, v) if t is not None), None)
+    if some is None:
+        raise ValueError("at least one of q, k and v is needed")
+    caches = (K, V) + tuple(k4 or ()) + tuple(v4 or ())
+    _here(q, k, v, first, n_new, q_weight, k_weight, inv_freq, q_out, *caches)
+    n_seq, T = some.shape[:2]
+    rows = [0, 0, 0]
+    for i, t in enumerate((q, k, v)):
+        if t is None:
+            continue
+        if t.dim() != 4 or tuple(t.shape[:2]) != (n_seq, T) or t.shape[3] != 128:
+            raise ValueError("q, k and v must be [n_seq][T][heads][128]")
+        if t.dtype != some.dtype:
+            raise TypeError("q, k and v must share a dtype")
+        # (strides of dimensions of one element say nothing)
+        rows[i] = t.stride(1) if T > 1 else t.stride(0) if n_seq > 1 else t.shape[2] * 128
+        if t.stride(3) != 1 or (t.shape[2] > 1 and t.stride(2) != 128) or (n_seq > 1 and t.stride(0) != T * rows[i]):
+            raise ValueError("the heads of a token must lie side by side, and all tokens equally far apart")
+    if k is not None and v is not None and k.shape[2] != v.shape[2]:
+        raise ValueError("k and v must have the same number of heads")
+    n_kv = next((t.shape[2] for t in (k, v) if t is not None), 1)
+    n_q = q.shape[2] if q is not None else n_kv
+    for w in (q_weight, k_weight):
+        if w is not None and (w.dtype != some.dtype or tuple(w.shape) != (128,) or not w.is_contiguous()):
+            raise ValueError("weights must be contiguous [128], of the dtype of q, k and v")
+    if inv_freq is not None and (inv_freq.dtype != torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous()):
+        raise ValueError("inv_freq must be a contiguous float32 tensor [rot_dim / 2]")
+    _ints(first, n_seq, "first")
+    _ints(n_new, n_seq, "n_new")
+    room = None
+    for t in (K, V):
+        if t is not None:
+            if t.dtype != some.dtype:
+                raise TypeError("caches and inputs must share a dtype")
+            if t.dim() != 4 or tuple(t.shape[:2]) != (n_seq, n_kv) or t.shape[3] != 128 or not t.is_contiguous() \
+                    or t.shape[2] != (room or t.shape[2]):
+                raise ValueError("K and V must be contiguous [n_seq][n_kv][capacity][128], of one capacity")
+            room = t.shape[2]
+    room4 = None
+    for x4, name in ((k4, "k4"), (v4, "v4")):
+        if x4 is not None:
+            room4 = _kv4(x4, n_seq, n_kv, name, room4)
+    if q is not None:
+        if q_out is None:
+            q_out = (torch.empty if n_new is None else torch.zeros)((n_seq, n_q, T, 128), dtype=q.dtype, device=q.device)
+        elif q_out.dtype != q.dtype or tuple(q_out.shape) != (n_seq, n_q, T, 128) or not q_out.is_contiguous():
+            raise ValueError("q_out must be contiguous [n_seq][n_q][T][128], of the dtype of q")
+    elif q_out is not None:
+        raise ValueError("q_out goes with q")
+    c = [None if x4 is None else x4[i] for x4 in (k4, v4) for i in range(2)]
+    _check(lib().ra_append_tokens(_ptr(q), _ptr(k), _ptr(v), _dt(some), n_seq, n_q, n_kv, T, 128, *rows, _ptr(q_weight),
+                                  _ptr(k_weight), eps, _ptr(inv_freq), 0 if inv_freq is None else 2 * inv_freq.numel(),
+                                  int(interleaved), _ptr(first), _ptr(n_new), room or 0, room4 or 0, _stream(stream), _ptr(q_out), _ptr(K),
+                                  _ptr(V), *[_ptr(t) for t in c]))
+    return q_out
+
+
+def ra_quantize_kv4(X, first=None, n_new=None, out=None, stream=None):
+    """Rows [n_seq][n_kv][T][128] into 4 bits -> (codes uint8 [n_seq][n_kv][capacity][64], scale uint8
+    [n_seq][n_kv][capacity][4]). With out = (codes, scale) given, row t of sequence s goes to row first[s] + t of these (first: int32
+    [n_seq] on the GPU; n_new likewise: only so many rows); without, they are new and hold T rows."""
+    _dev(X)
+    _here(X, first, n_new, *(out or ()))
+    n_seq, n_kv, T, d = X.shape
+    if out is None:
+        if first is not None or n_new is not None:
+            raise ValueError("first and n_new go with out")
+        out = (torch.empty((n_seq, n_kv, T, 64), dtype=torch.uint8, device=X.device),
+               torch.empty((n_seq, n_kv, T, 4), dtype=torch.uint8, device=X.device))
+    room = _kv4(out, n_seq, n_kv, "out")
+    _ints(first, n_seq, "first")
+    _ints(n_new, n_seq, "n_new")
+    _check(lib().ra_quantize_kv4(_ptr(X), _dt(X), n_seq, n_kv, T, d, _ptr(first), _ptr(n_new), room, _stream(stream),
+                                 _ptr(out[0]), _ptr(out[1])))
+    return out
+
+
+def ra_dequantize_kv4(x4, dtype, first=None, rows: Optional[int] = None, out=None, stream=None):
+    """Rows first[s] .. first[s] + rows (None: from 0, all) of a cache in 4 bits -> [n_seq][n_kv][rows][128] of the given dtype, the
+    values they stand for."""
+    _here(first, out, *x4)
+    n_seq, n_kv = x4[0].shape[:2]
+    room = _kv4(x4, n_seq, n_kv, "x4")
+    _ints(first, n_seq, "first")
+    rows = room if rows is None else rows
+    if out is None:
+        out = torch.empty((n_seq, n_kv, rows, 128), dtype=dtype, device=x4[0].device)
+    elif out.dtype != dtype or tuple(out.shape) != (n_seq, n_kv, rows, 128) or not out.is_contiguous():
+        raise ValueError("out must be contiguous [n_seq][n_kv][rows][128], of the given dtype")
+    _check(lib().ra_dequantize_kv4(_ptr(x4[0]), _ptr(x4[1]), _dt(out), n_seq, n_kv, rows, 128, _ptr(first), room, _stream(stream),
+                                   _ptr(out)))
+    return out
+
+
+def _results(n_seq, n_q, d, device, out, lse):
+    """out [n_seq][n_q][d] and lse [n_seq][n_q], the given ones or new ones."""
+    if out is None:
+        out = torch.empty((n_seq, n_q, d), dtype=torch.float32, device=device)
+    if lse is None:
+        lse = torch.empty((n_seq, n_q), dtype=torch.float32, device=device)
+    for t, shape in ((out, (n_seq, n_q, d)), (lse, (n_seq, n_q))):
+        if t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous():
+            raise ValueError(f"results must be contiguous float32 {list(shape)}")
+    return out, lse
+
+
+def ra_full_attention_q4(q, k4, v4, n_tokens=None, N: Optional[int] = None, stream=None, workspace=None, out=None, lse=None):
+    """Eq. 1 over the first n_tokens[s] rows (int32 [n_seq] on the GPU, at most N; None: N, by default the capacity) of a cache
+    in 4 bits -> (out float32 [n_seq][n_q][128], lse float32 [n_seq][n_q])."""
+    _dev(q, workspace)
+    _here(q, n_tokens, workspace, out, lse, *k4, *v4)
+    n_seq, n_q, d = q.shape
+    n_kv = k4[0].shape[1]
+    room = _kv4(k4, n_seq, n_kv, "k4")
+    _kv4(v4, n_seq, n_kv, "v4", room)
+    _ints(n_tokens, n_seq, "n_tokens")
+    N = room if N is None else N
+    if workspace is None:
+        need = lib().ra_full_attention_q4_workspace_bytes(_dt(q), n_seq, n_q, n_kv, N)
+        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
+    out, lse = _results(n_seq, n_q, d, q.device, out, lse)
+    _check(lib().ra_full_attention_q4(_ptr(q), _dt(q), _ptr(k4[0]), _ptr(k4[1]), _ptr(v4[0]), _ptr(v4[1]), n_seq, n_q, n_kv, N, room, d,
+                                      _ptr(n_tokens), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                      _stream(stream), _ptr(out), _ptr(lse)))
+    return out, lse
+
+
+def ra_attend_q4(q, idx: Index, k4, v4, sink: int, window: int, ids: torch.Tensor, N: Optional[int] = None, stream=None,
+                 partials: bool = False, out=None, lse=None):
+    """ra_attend over a cache in 4 bits that holds N >= idx.N tokens (by default as many as its capacity); tokens behind the
+    index's are static. -> (out, lse) or, with partials=True, (out, lse, o_omega, lse_omega, o_w, lse_w)."""
+    _dev(q, ids)
+    _here(q, ids, out, lse, *k4, *v4)
+    n_seq, n_q, d = q.shape
+    if (n_seq, n_q) != (idx.n_seq, idx.n_q_heads) or d != 128:
+        raise ValueError("q must be [n_seq][n_q][128], as the index has them")
+    if ids.dtype != torch.int32 or ids.dim() != 3 or tuple(ids.shape[:2]) != (n_seq, n_q):
+        raise ValueError("ids must be int32 [n_seq][n_q][topk]")
+    room = _kv4(k4, n_seq, idx.n_kv_heads, "k4")
+    _kv4(v4, n_seq, idx.n_kv_heads, "v4", room)
+    out, lse = _results(n_seq, n_q, d, q.device, out, lse)
+    extra = [None] * 4
+    if partials:
+        f = dict(dtype=torch.float32, device=q.device)
+        extra = [torch.empty((n_seq, n_q, d), **f), torch.empty((n_seq, n_q), **f),
+                 torch.empty((n_seq, n_q, d), **f), torch.empty((n_seq, n_q), **f)]
+    _check(_room(lib().ra_attend_q4, _ptr(q), idx.handle, _dt(q), _ptr(k4[0]), _ptr(k4[1]), _ptr(v4[0]), _ptr(v4[1]),
+                 room if N is None else N, room, sink, window, ids.shape[-1], _ptr(ids), _stream(stream), _ptr(out), _ptr(lse),
+                 *[_ptr(t) for t in extra]))
+    return (out, lse, *extra) if partials else (out, lse)

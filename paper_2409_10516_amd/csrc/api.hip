@@ -784,3 +784,130 @@ extern "C" ra_status ra_full_attention(const void* q, const void* K, const void*
     return ra_launch_attend(q, K, V, dt, n_seq, n_q, n_kv, N, (int)N, 0, 1, nullptr, (float*)workspace, nullptr,
                             (hipStream_t)stream, out, lse, nullptr, nullptr, nullptr, nullptr);
 }
+
+// ---- a cache in 4 bits ------------------------------------------------------------------
+static ra_status check_aligned(const void* p, size_t to, const char* what) {
+    if ((uintptr_t)p % to) RA_FAIL(RA_EINVAL, "%s is not %zu-byte aligned", what, to);
+    return RA_OK;
+}
+
+static ra_status check_q4(const uint8_t* codes, const uint8_t* scale, const char* what) {
+    if (!codes || !scale) RA_FAIL(RA_EINVAL, "NULL argument: codes or scale of %s", what);
+    RA_TRY(check_aligned(codes, 16, "an array of codes"));
+    return check_aligned(scale, 4, "an array of scale bytes");
+}
+
+// new rows [.][T] of a cache with room for kv_stride rows per head
+static ra_status check_rows(int n_seq, int n_kv, int64_t T, int64_t kv_stride) {
+    if (n_seq < 1 || n_kv < 1) RA_FAIL(RA_EINVAL, "n_seq and n_kv_heads must be positive");
+    if (T < 1 || kv_stride < 1) RA_FAIL(RA_EINVAL, "T and kv_stride must be positive");
+    if (T > 0x7fffffff / 2 || kv_stride > 0x7fffffff / 2) RA_FAIL(RA_EUNSUP, "T or kv_stride too large");
+    return RA_OK;
+}
+
+extern "C" ra_status ra_append_tokens(const void* q_in, const void* k_in, const void* v_in, ra_dtype dt, int n_seq, int n_q,
+                                      int n_kv, int64_t T, int d, int64_t q_row, int64_t k_row, int64_t v_row,
+                                      const void* q_weight, const void* k_weight, double eps, const float* inv_freq, int rot_dim,
+                                      int interleaved, const int32_t* first, const int32_t* n_new, int64_t kv_stride,
+                                      int64_t kv4_stride, void* stream, void* q_out, void* K, void* V, uint8_t* K4, uint8_t* K4s, uint8_t* V4,
+                                      uint8_t* V4s) {
+    RA_TRY(check_dtype(dt));
+    RA_TRY(check_heads(n_seq, n_q, n_kv));
+    RA_TRY(check_dim(d));
+    RA_TRY(check_rows(n_seq, n_kv, T, K || V ? kv_stride : 1));
+    RA_TRY(check_rows(n_seq, n_kv, T, K4 || V4 ? kv4_stride : 1));
+    if (!q_in && !k_in && !v_in) RA_FAIL(RA_EINVAL, "NULL argument: no input");
+    if (!q_in != !q_out) RA_FAIL(RA_EINVAL, "q_in and q_out go together");
+    if (!K4 != !K4s || !V4 != !V4s) RA_FAIL(RA_EINVAL, "codes and scale of a cache go together");
+    if (!k_in != (!K && !K4)) RA_FAIL(RA_EINVAL, "k_in goes with K or its 4-bit form");
+    if (!v_in != (!V && !V4)) RA_FAIL(RA_EINVAL, "v_in goes with V or its 4-bit form");
+    if (K4) RA_TRY(check_q4(K4, K4s, "K"));
+    if (V4) RA_TRY(check_q4(V4, V4s, "V"));
+    if (rot_dim < 0 || rot_dim > RA_D) RA_FAIL(RA_EINVAL, "rot_dim %d outside [0, %d]", rot_dim, RA_D);
+    if (rot_dim % 16) RA_FAIL(RA_EUNSUP, "rot_dim %d is not a multiple of 16", rot_dim);
+    if (rot_dim && (q_in || k_in) && !inv_freq) RA_FAIL(RA_EINVAL, "NULL argument: inv_freq");
+    if ((q_weight || k_weight) && !(eps >= 0.)) RA_FAIL(RA_EINVAL, "eps must be non-negative");
+    const size_t esz = dt == RA_BF16 ? 2 : 4;
+    AppendArgs a{{q_in, k_in, v_in}, {q_weight, k_weight}, {q_row, k_row, v_row}, {q_out, K, V}, {K4, V4}, {K4s, V4s},
+                 inv_freq, first, n_new, eps, T, {kv_stride, kv4_stride}, n_seq, n_q, n_kv, rot_dim, interleaved != 0};
+    for (int i = 0; i < 3; ++i) {
+        RA_TRY(check_aligned(a.in[i], 16, "an input"));
+        RA_TRY(check_aligned(a.out[i], 16, "q_out, K or V"));
+        const int64_t least = (int64_t)(i ? n_kv : n_q) * RA_D;
+        if (a.in[i] && a.row[i] < least)
+            RA_FAIL(RA_ESHAPE, "tokens are %lld elements apart, their heads take %lld", (long long)a.row[i], (long long)least);
+        if (a.in[i] && a.row[i] * esz % 16) RA_FAIL(RA_EUNSUP, "tokens are %lld elements apart: not a multiple of 16 bytes", (long long)a.row[i]);
+    }
+    for (int i = 0; i < 2; ++i) RA_TRY(check_aligned(a.weight[i], esz, "a weight"));
+    return ra_launch_append(a, dt, (hipStream_t)stream);
+}
+
+extern "C" ra_status ra_quantize_kv4(const void* X, ra_dtype dt, int n_seq, int n_kv, int64_t T, int d, const int32_t* first,
+                                     const int32_t* n_new, int64_t kv_stride, void* stream, uint8_t* codes, uint8_t* scale) {
+    if (!X) RA_FAIL(RA_EINVAL, "NULL argument");
+    RA_TRY(check_dtype(dt));
+    RA_TRY(check_dim(d));
+    RA_TRY(check_rows(n_seq, n_kv, T, kv_stride));
+    RA_TRY(check_q4(codes, scale, "the cache"));
+    RA_TRY(check_aligned(X, 16, "X"));
+    return ra_launch_quantize_kv4(X, dt, n_seq, n_kv, T, first, n_new, kv_stride, (hipStream_t)stream, codes, scale);
+}
+
+extern "C" ra_status ra_dequantize_kv4(const uint8_t* codes, const uint8_t* scale, ra_dtype dt, int n_seq, int n_kv, int64_t T,
+                                       int d, const int32_t* first, int64_t kv_stride, void* stream, void* X) {
+    if (!X) RA_FAIL(RA_EINVAL, "NULL argument");
+    RA_TRY(check_dtype(dt));
+    RA_TRY(check_dim(d));
+    RA_TRY(check_rows(n_seq, n_kv, T, kv_stride));
+    RA_TRY(check_q4(codes, scale, "the cache"));
+    RA_TRY(check_aligned(X, 16, "X"));
+    return ra_launch_dequantize_kv4(codes, scale, dt, n_seq, n_kv, T, first, kv_stride, (hipStream_t)stream, X);
+}
+
+extern "C" size_t ra_full_attention_q4_workspace_bytes(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N) {
+    if (check_dtype(dt) != RA_OK || check_heads(n_seq, n_q, n_kv) != RA_OK || N < 1 || N > 0x7fffffff / 2) return 0;
+    return 256 + ra_full_q4_partial_floats(dt, n_seq, n_q, n_kv, N) * sizeof(float);
+}
+
+extern "C" ra_status ra_full_attention_q4(const void* q, ra_dtype dt, const uint8_t* K4, const uint8_t* K4s, const uint8_t* V4,
+                                          const uint8_t* V4s, int n_seq, int n_q, int n_kv, int64_t N, int64_t kv_stride, int d,
+                                          const int32_t* n_tokens, void* workspace, size_t workspace_bytes, void* stream,
+                                          float* out, float* lse) {
+    if (!q || !out || !lse || !workspace) RA_FAIL(RA_EINVAL, "NULL argument");
+    RA_TRY(check_dtype(dt));
+    RA_TRY(check_heads(n_seq, n_q, n_kv));
+    RA_TRY(check_dim(d));
+    RA_TRY(check_q4(K4, K4s, "K"));
+    RA_TRY(check_q4(V4, V4s, "V"));
+    if (N < 1) RA_FAIL(RA_EINVAL, "N must be positive");
+    if (N > 0x7fffffff / 2 || kv_stride > 0x7fffffff / 2) RA_FAIL(RA_EUNSUP, "N or kv_stride too large");
+    if (kv_stride < N) RA_FAIL(RA_ESHAPE, "kv_stride %lld is below N = %lld", (long long)kv_stride, (long long)N);
+    RA_TRY(check_aligned(q, 16, "q"));
+    RA_TRY(check_aligned(workspace, 16, "workspace"));
+    if (workspace_bytes < ra_full_attention_q4_workspace_bytes(dt, n_seq, n_q, n_kv, N))
+        RA_FAIL(RA_ESHAPE, "workspace of %zu B is smaller than ra_full_attention_q4_workspace_bytes", workspace_bytes);
+    return ra_launch_full_q4(q, dt, Q4Cache{K4, K4s, V4, V4s, kv_stride}, n_seq, n_q, n_kv, N, n_tokens, (float*)workspace,
+                             (hipStream_t)stream, out, lse);
+}
+
+extern "C" ra_status ra_attend_q4(const void* q, const ra_index* idx, ra_dtype dt, const uint8_t* K4, const uint8_t* K4s,
+                                  const uint8_t* V4, const uint8_t* V4s, int64_t N, int64_t kv_stride, int sink, int window,
+                                  int topk, const int32_t* ids, void* stream, float* out, float* lse, float* o_omega,
+                                  float* lse_omega, float* o_w, float* lse_w) {
+    if (!q || !ids || !out || !lse) RA_FAIL(RA_EINVAL, "NULL argument");
+    RA_TRY(check_dtype(dt));
+    if (!idx) RA_FAIL(RA_EINVAL, "index handle is NULL");
+    RA_TRY(check_decode_args(idx, idx->N, sink, window, topk));
+    RA_TRY(check_q4(K4, K4s, "K"));
+    RA_TRY(check_q4(V4, V4s, "V"));
+    if (N < idx->N)
+        RA_FAIL(RA_ESHAPE, "N = %lld is below the %lld keys the index was built over", (long long)N, (long long)idx->N);
+    if (N > 0x7fffffff / 2 || kv_stride > 0x7fffffff / 2) RA_FAIL(RA_EUNSUP, "N or kv_stride too large");
+    if (kv_stride < N) RA_FAIL(RA_ESHAPE, "kv_stride %lld is below N = %lld", (long long)kv_stride, (long long)N);
+    RA_TRY(check_aligned(q, 16, "q"));
+    ra_index* ix = const_cast<ra_index*>(idx);
+    const size_t need = ra_attend_q4_partial_floats(dt, ix->n_seq, ix->n_q, ix->n_kv, N, ix->N, sink, window, topk) * sizeof(float);
+    RA_TRY(grow((void**)&ix->partials, &ix->partials_bytes, need));
+    return ra_launch_attend_q4(q, dt, Q4Cache{K4, K4s, V4, V4s, kv_stride}, ix->n_seq, ix->n_q, ix->n_kv, N, ix->N, sink, window, topk,
+                               ids, ix->partials, attend_tickets(ix), (hipStream_t)stream, out, lse, o_omega, lse_omega, o_w, lse_w);
+}

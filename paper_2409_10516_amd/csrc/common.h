@@ -161,6 +161,35 @@ ra_status ra_launch_flat_topk(const void* q, const void* K, ra_dtype dt, int n_s
                               int64_t N, int sink, int window, int topk, uint32_t* keys_ws,
                               hipStream_t st, int32_t* ids);
 
+// a cache in 4 bits (q4_dev.h): codes and scale bytes, heads `kv_stride` rows apart
+struct Q4Cache {
+    const uint8_t *k, *ks, *v, *vs;
+    int64_t kv_stride;
+};
+struct AppendArgs {
+    const void *in[3], *weight[2];          // q, k, v; q's and k's
+    int64_t row[3];                         // elements from token to token
+    void* out[3];                           // q_out, K, V
+    uint8_t *codes[2], *scale[2];           // of K and V in 4 bits
+    const float* inv_freq;
+    const int32_t *first, *n_new;
+    double eps;
+    int64_t T, stride[2];                    // capacity of K and V, and of their 4-bit form
+    int n_seq, n_q, n_kv, rot, interleaved;
+};
+ra_status ra_launch_append(const AppendArgs& a, ra_dtype dt, hipStream_t st);
+ra_status ra_launch_quantize_kv4(const void* X, ra_dtype dt, int n_seq, int n_kv, int64_t T, const int32_t* first,
+                                 const int32_t* n_new, int64_t kv_stride, hipStream_t st, uint8_t* codes, uint8_t* scale);
+ra_status ra_launch_dequantize_kv4(const uint8_t* codes, const uint8_t* scale, ra_dtype dt, int n_seq, int n_kv, int64_t T,
+                                   const int32_t* first, int64_t kv_stride, hipStream_t st, void* X);
+size_t ra_full_q4_partial_floats(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N);
+ra_status ra_launch_full_q4(const void* q, ra_dtype dt, const Q4Cache& c, int n_seq, int n_q, int n_kv, int64_t N,
+                            const int32_t* n_tokens, float* partials, hipStream_t st, float* out, float* lse);
+size_t ra_attend_q4_partial_floats(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N, int64_t Ng, int sink, int window, int topk);
+ra_status ra_launch_attend_q4(const void* q, ra_dtype dt, const Q4Cache& c, int n_seq, int n_q, int n_kv, int64_t N, int64_t Ng,
+                              int sink, int window, int topk, const int32_t* ids, float* partials, uint32_t* tickets,
+                              hipStream_t st, float* out, float* lse, float* o_omega, float* lse_omega, float* o_w, float* lse_w);
+
 // `workspace`: ra_knn_workspace_bytes(...) bytes of device memory, free again once the stream has run
 // the launch; with only as many as `plain` asks for, the lists come without 8-bit products
 ra_status ra_launch_knn(const void* K, const void* Q, ra_dtype dt, int n_seq, int n_q, int n_kv,
