@@ -8,6 +8,7 @@ if the library is missing, loading fails with an error.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Optional
 
@@ -180,32 +181,40 @@ def _stream(stream) -> int:
     return torch.cuda.current_stream().cuda_stream if raw is None else raw(torch.cuda.current_device())
 
 
+# The calls around a 4-bit cache take many tensors and are made once per token and layer: their checks read every attribute once
+# and build nothing (a tensor's attribute is some 0.1 us, a ctypes call with 20 arguments 2 us, a launch 2 us).
 def _here(*ts):
-    """The given tensors live on the current device, where the call is launched."""
+    """The given tensors live on the current device, where the call is launched -> its index."""
     here = torch.cuda.current_device()
     for t in ts:
-        if t is not None and (not t.is_cuda or t.device.index != here):
+        if t is not None and t.get_device() != here:
             raise ValueError(f"tensors must live on the current GPU ({here}), not on {t.device}")
+    return here
 
 
-def _ints(t: Optional[torch.Tensor], n_seq: int, name: str):
-    if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != (n_seq,) or not t.is_contiguous()):
+def _ints(t: torch.Tensor, n_seq: int, name: str) -> int:
+    """The address of a vector of n_seq 32-bit integers."""
+    if t.dtype is not torch.int32 or t.shape != (n_seq,) or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 tensor [n_seq]")
+    return t.data_ptr()
 
 
-def _kv4(x4, n_seq: int, n_kv: int, name: str, kv_stride: Optional[int] = None) -> int:
-    """Checks a cache in 4 bits (codes, scale) -> its capacity in rows."""
+def _kv4(x4, n_seq: int, n_kv: int, name: str, here: int, kv_stride: Optional[int] = None):
+    """Checks a cache in 4 bits (codes, scale) -> their addresses and its capacity in rows."""
     codes, scale = x4
-    rows = codes.shape[2] if codes.dim() == 4 else -1
-    if tuple(codes.shape) != (n_seq, n_kv, rows, 64) or tuple(scale.shape) != (n_seq, n_kv, rows, 4):
+    shape = codes.shape
+    rows = shape[2] if len(shape) == 4 else -1
+    if shape != (n_seq, n_kv, rows, 64) or scale.shape != (n_seq, n_kv, rows, 4):
         raise ValueError(f"{name} must be codes [n_seq][n_kv][capacity][64] and scale [n_seq][n_kv][capacity][4]")
-    if codes.dtype != torch.uint8 or scale.dtype != torch.uint8:
+    if codes.dtype is not torch.uint8 or scale.dtype is not torch.uint8:
         raise TypeError(f"{name} must be uint8")
     if not codes.is_contiguous() or not scale.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
+    if codes.get_device() != here or scale.get_device() != here:
+        raise ValueError(f"{name} must live on the current GPU ({here}), not on {codes.device} and {scale.device}")
     if kv_stride is not None and rows != kv_stride:
         raise ValueError(f"{name} holds {rows} rows per head, not {kv_stride}")
-    return rows
+    return codes.data_ptr(), scale.data_ptr(), rows
 
 
 class Index:
@@ -236,6 +245,11 @@ class Index:
     shared_launches = property(lambda s: s.info(11))
 
     n_seeds = property(lambda s: s.info(7))
+
+    @functools.cached_property
+    def heads(self):
+        """(n_seq, n_q_heads, n_kv_heads), which a handle keeps for life."""
+        return self.n_seq, self.n_q_heads, self.n_kv_heads
 
     def configure(self, what: int, value: int) -> None:
         """ra_index_configure: RA_CFG_HELPERS / RA_CFG_HELPER_SPIN / RA_CFG_SEEDS / RA_CFG_SEED_SHARES."""
@@ -507,62 +521,74 @@ def ra_append_tokens(q, k, v, first, *, n_new=None, q_weight=None, k_weight=None
     2 * len(inv_freq) dimensions at positions first[s] + t, new rows of the caches. q, k, v: [n_seq][T][heads][128] (any may be
     None), the heads of a token side by side, tokens any multiple of 16 bytes apart, so that they may be parts of one buffer. first,
     n_new: int32 [n_seq] on the GPU (None: 0, and T). K, V: caches [n_seq][n_kv][capacity][128]; k4, v4: caches in 4 bits, of a
-    capacity of their own, (codes, scale) as from ra_quantize_kv4. -> q_out [n_seq][n_q][T][128] (None without q); where tokens are fewer than T and no q_out is
-    given, the rows behind the last one are zero."""
-    some = next((t for t in (q, k, v) if t is not None), None)
+    capacity of their own, (codes, scale) as from ra_quantize_kv4. -> q_out [n_seq][n_q][T][128] (None without q); where tokens are fewer
+    than T and no q_out is given, the rows behind the last one are zero."""
+    some = q if q is not None else k if k is not None else v
     if some is None:
         raise ValueError("at least one of q, k and v is needed")
-    caches = (K, V) + tuple(k4 or ()) + tuple(v4 or ())
-    _here(q, k, v, first, n_new, q_weight, k_weight, inv_freq, q_out, *caches)
+    here = _here(q, k, v, first, n_new, q_weight, k_weight, inv_freq, q_out, K, V)
+    dtype = some.dtype
+    if some.dim() != 4:
+        raise ValueError("q, k and v must be [n_seq][T][heads][128]")
     n_seq, T = some.shape[:2]
-    rows = [0, 0, 0]
-    for i, t in enumerate((q, k, v)):
+
+    def rows(t):
+        """-> (address, heads, elements from token to token)"""
         if t is None:
-            continue
-        if t.dim() != 4 or tuple(t.shape[:2]) != (n_seq, T) or t.shape[3] != 128:
+            return None, 0, 0
+        shape = t.shape
+        if len(shape) != 4 or shape[0] != n_seq or shape[1] != T or shape[3] != 128:
             raise ValueError("q, k and v must be [n_seq][T][heads][128]")
-        if t.dtype != some.dtype:
+        if t.dtype is not dtype:
             raise TypeError("q, k and v must share a dtype")
-        # (strides of dimensions of one element say nothing)
-        rows[i] = t.stride(1) if T > 1 else t.stride(0) if n_seq > 1 else t.shape[2] * 128
-        if t.stride(3) != 1 or (t.shape[2] > 1 and t.stride(2) != 128) or (n_seq > 1 and t.stride(0) != T * rows[i]):
+        seq, token, head, one = t.stride()
+        heads = shape[2]
+        # (the stride of a dimension of one element says nothing)
+        row = token if T > 1 else seq if n_seq > 1 else heads * 128
+        if one != 1 or (heads > 1 and head != 128) or (n_seq > 1 and seq != T * row):
             raise ValueError("the heads of a token must lie side by side, and all tokens equally far apart")
-    if k is not None and v is not None and k.shape[2] != v.shape[2]:
+        return t.data_ptr(), heads, row
+
+    q_at, n_q, q_row = rows(q)
+    k_at, n_k, k_row = rows(k)
+    v_at, n_v, v_row = rows(v)
+    if n_k and n_v and n_k != n_v:
         raise ValueError("k and v must have the same number of heads")
-    n_kv = next((t.shape[2] for t in (k, v) if t is not None), 1)
-    n_q = q.shape[2] if q is not None else n_kv
+    n_kv = n_k or n_v or 1
     for w in (q_weight, k_weight):
-        if w is not None and (w.dtype != some.dtype or tuple(w.shape) != (128,) or not w.is_contiguous()):
+        if w is not None and (w.dtype is not dtype or w.shape != (128,) or not w.is_contiguous()):
             raise ValueError("weights must be contiguous [128], of the dtype of q, k and v")
-    if inv_freq is not None and (inv_freq.dtype != torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous()):
-        raise ValueError("inv_freq must be a contiguous float32 tensor [rot_dim / 2]")
-    _ints(first, n_seq, "first")
-    _ints(n_new, n_seq, "n_new")
-    room = None
+    rot = 0
+    if inv_freq is not None:
+        if inv_freq.dtype is not torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+            raise ValueError("inv_freq must be a contiguous float32 tensor [rot_dim / 2]")
+        rot = 2 * inv_freq.shape[0]
+    room = room4 = 0
     for t in (K, V):
         if t is not None:
-            if t.dtype != some.dtype:
+            if t.dtype is not dtype:
                 raise TypeError("caches and inputs must share a dtype")
-            if t.dim() != 4 or tuple(t.shape[:2]) != (n_seq, n_kv) or t.shape[3] != 128 or not t.is_contiguous() \
-                    or t.shape[2] != (room or t.shape[2]):
+            shape = t.shape
+            if len(shape) != 4 or shape != (n_seq, n_kv, room or shape[2], 128) or not t.is_contiguous():
                 raise ValueError("K and V must be contiguous [n_seq][n_kv][capacity][128], of one capacity")
-            room = t.shape[2]
-    room4 = None
-    for x4, name in ((k4, "k4"), (v4, "v4")):
-        if x4 is not None:
-            room4 = _kv4(x4, n_seq, n_kv, name, room4)
-    if q is not None:
-        if q_out is None:
-            q_out = (torch.empty if n_new is None else torch.zeros)((n_seq, n_q, T, 128), dtype=q.dtype, device=q.device)
-        elif q_out.dtype != q.dtype or tuple(q_out.shape) != (n_seq, n_q, T, 128) or not q_out.is_contiguous():
-            raise ValueError("q_out must be contiguous [n_seq][n_q][T][128], of the dtype of q")
-    elif q_out is not None:
-        raise ValueError("q_out goes with q")
-    c = [None if x4 is None else x4[i] for x4 in (k4, v4) for i in range(2)]
-    _check(lib().ra_append_tokens(_ptr(q), _ptr(k), _ptr(v), _dt(some), n_seq, n_q, n_kv, T, 128, *rows, _ptr(q_weight),
-                                  _ptr(k_weight), eps, _ptr(inv_freq), 0 if inv_freq is None else 2 * inv_freq.numel(),
-                                  int(interleaved), _ptr(first), _ptr(n_new), room or 0, room4 or 0, _stream(stream), _ptr(q_out), _ptr(K),
-                                  _ptr(V), *[_ptr(t) for t in c]))
+            room = shape[2]
+    k4_at = k4s_at = v4_at = v4s_at = None
+    if k4 is not None:
+        k4_at, k4s_at, room4 = _kv4(k4, n_seq, n_kv, "k4", here)
+    if v4 is not None:
+        v4_at, v4s_at, room4 = _kv4(v4, n_seq, n_kv, "v4", here, room4 or None)
+    if q is None:
+        if q_out is not None:
+            raise ValueError("q_out goes with q")
+    elif q_out is None:
+        q_out = (torch.empty if n_new is None else torch.zeros)((n_seq, n_q, T, 128), dtype=dtype, device=q.device)
+    elif q_out.dtype is not dtype or q_out.shape != (n_seq, n_q, T, 128) or not q_out.is_contiguous():
+        raise ValueError("q_out must be contiguous [n_seq][n_q][T][128], of the dtype of q")
+    _check(lib().ra_append_tokens(q_at, k_at, v_at, _dt(some), n_seq, n_q or n_kv, n_kv, T, 128, q_row, k_row, v_row, _ptr(q_weight),
+                                  _ptr(k_weight), eps, _ptr(inv_freq), rot, 1 if interleaved else 0,
+                                  None if first is None else _ints(first, n_seq, "first"),
+                                  None if n_new is None else _ints(n_new, n_seq, "n_new"), room, room4, _stream(stream), _ptr(q_out),
+                                  _ptr(K), _ptr(V), k4_at, k4s_at, v4_at, v4s_at))
     return q_out
 
 
@@ -571,35 +597,32 @@ def ra_quantize_kv4(X, first=None, n_new=None, out=None, stream=None):
     [n_seq][n_kv][capacity][4]). With out = (codes, scale) given, row t of sequence s goes to row first[s] + t of these (first: int32
     [n_seq] on the GPU; n_new likewise: only so many rows); without, they are new and hold T rows."""
     _dev(X)
-    _here(X, first, n_new, *(out or ()))
+    here = _here(X, first, n_new)
     n_seq, n_kv, T, d = X.shape
     if out is None:
         if first is not None or n_new is not None:
             raise ValueError("first and n_new go with out")
         out = (torch.empty((n_seq, n_kv, T, 64), dtype=torch.uint8, device=X.device),
                torch.empty((n_seq, n_kv, T, 4), dtype=torch.uint8, device=X.device))
-    room = _kv4(out, n_seq, n_kv, "out")
-    _ints(first, n_seq, "first")
-    _ints(n_new, n_seq, "n_new")
-    _check(lib().ra_quantize_kv4(_ptr(X), _dt(X), n_seq, n_kv, T, d, _ptr(first), _ptr(n_new), room, _stream(stream),
-                                 _ptr(out[0]), _ptr(out[1])))
+    codes, scale, room = _kv4(out, n_seq, n_kv, "out", here)
+    _check(lib().ra_quantize_kv4(X.data_ptr(), _dt(X), n_seq, n_kv, T, d, None if first is None else _ints(first, n_seq, "first"),
+                                 None if n_new is None else _ints(n_new, n_seq, "n_new"), room, _stream(stream), codes, scale))
     return out
 
 
 def ra_dequantize_kv4(x4, dtype, first=None, rows: Optional[int] = None, out=None, stream=None):
     """Rows first[s] .. first[s] + rows (None: from 0, all) of a cache in 4 bits -> [n_seq][n_kv][rows][128] of the given dtype, the
     values they stand for."""
-    _here(first, out, *x4)
+    here = _here(first, out)
     n_seq, n_kv = x4[0].shape[:2]
-    room = _kv4(x4, n_seq, n_kv, "x4")
-    _ints(first, n_seq, "first")
+    codes, scale, room = _kv4(x4, n_seq, n_kv, "x4", here)
     rows = room if rows is None else rows
     if out is None:
         out = torch.empty((n_seq, n_kv, rows, 128), dtype=dtype, device=x4[0].device)
-    elif out.dtype != dtype or tuple(out.shape) != (n_seq, n_kv, rows, 128) or not out.is_contiguous():
+    elif out.dtype is not dtype or out.shape != (n_seq, n_kv, rows, 128) or not out.is_contiguous():
         raise ValueError("out must be contiguous [n_seq][n_kv][rows][128], of the given dtype")
-    _check(lib().ra_dequantize_kv4(_ptr(x4[0]), _ptr(x4[1]), _dt(out), n_seq, n_kv, rows, 128, _ptr(first), room, _stream(stream),
-                                   _ptr(out)))
+    _check(lib().ra_dequantize_kv4(codes, scale, _dt(out), n_seq, n_kv, rows, 128, None if first is None else _ints(first, n_seq, "first"),
+                                   room, _stream(stream), out.data_ptr()))
     return out
 
 
@@ -607,32 +630,41 @@ def _results(n_seq, n_q, d, device, out, lse):
     """out [n_seq][n_q][d] and lse [n_seq][n_q], the given ones or new ones."""
     if out is None:
         out = torch.empty((n_seq, n_q, d), dtype=torch.float32, device=device)
+    elif out.dtype is not torch.float32 or out.shape != (n_seq, n_q, d) or not out.is_contiguous():
+        raise ValueError("out must be contiguous float32 [n_seq][n_q][128]")
     if lse is None:
         lse = torch.empty((n_seq, n_q), dtype=torch.float32, device=device)
-    for t, shape in ((out, (n_seq, n_q, d)), (lse, (n_seq, n_q))):
-        if t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous():
-            raise ValueError(f"results must be contiguous float32 {list(shape)}")
+    elif lse.dtype is not torch.float32 or lse.shape != (n_seq, n_q) or not lse.is_contiguous():
+        raise ValueError("lse must be contiguous float32 [n_seq][n_q]")
     return out, lse
+
+
+@functools.lru_cache(maxsize=256)
+def _full_q4_room(dt: int, n_seq: int, n_q: int, n_kv: int, N: int) -> int:
+    """ra_full_attention_q4_workspace_bytes, a function of sizes alone."""
+    return max(1, lib().ra_full_attention_q4_workspace_bytes(dt, n_seq, n_q, n_kv, N))
 
 
 def ra_full_attention_q4(q, k4, v4, n_tokens=None, N: Optional[int] = None, stream=None, workspace=None, out=None, lse=None):
     """Eq. 1 over the first n_tokens[s] rows (int32 [n_seq] on the GPU, at most N; None: N, by default the capacity) of a cache
     in 4 bits -> (out float32 [n_seq][n_q][128], lse float32 [n_seq][n_q])."""
     _dev(q, workspace)
-    _here(q, n_tokens, workspace, out, lse, *k4, *v4)
+    here = _here(q, n_tokens, workspace, out, lse)
     n_seq, n_q, d = q.shape
     n_kv = k4[0].shape[1]
-    room = _kv4(k4, n_seq, n_kv, "k4")
-    _kv4(v4, n_seq, n_kv, "v4", room)
-    _ints(n_tokens, n_seq, "n_tokens")
+    K4, K4s, room = _kv4(k4, n_seq, n_kv, "k4", here)
+    V4, V4s, _ = _kv4(v4, n_seq, n_kv, "v4", here, room)
+    dt = _dt(q)
     N = room if N is None else N
     if workspace is None:
-        need = lib().ra_full_attention_q4_workspace_bytes(_dt(q), n_seq, n_q, n_kv, N)
-        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
+        have = _full_q4_room(dt, n_seq, n_q, n_kv, N)
+        workspace = torch.empty(have, dtype=torch.uint8, device=q.device)
+    else:
+        have = workspace.numel() * workspace.element_size()
     out, lse = _results(n_seq, n_q, d, q.device, out, lse)
-    _check(lib().ra_full_attention_q4(_ptr(q), _dt(q), _ptr(k4[0]), _ptr(k4[1]), _ptr(v4[0]), _ptr(v4[1]), n_seq, n_q, n_kv, N, room, d,
-                                      _ptr(n_tokens), _ptr(workspace), workspace.numel() * workspace.element_size(),
-                                      _stream(stream), _ptr(out), _ptr(lse)))
+    _check(lib().ra_full_attention_q4(q.data_ptr(), dt, K4, K4s, V4, V4s, n_seq, n_q, n_kv, N, room, d,
+                                      None if n_tokens is None else _ints(n_tokens, n_seq, "n_tokens"), workspace.data_ptr(), have,
+                                      _stream(stream), out.data_ptr(), lse.data_ptr()))
     return out, lse
 
 
@@ -641,21 +673,22 @@ def ra_attend_q4(q, idx: Index, k4, v4, sink: int, window: int, ids: torch.Tenso
     """ra_attend over a cache in 4 bits that holds N >= idx.N tokens (by default as many as its capacity); tokens behind the
     index's are static. -> (out, lse) or, with partials=True, (out, lse, o_omega, lse_omega, o_w, lse_w)."""
     _dev(q, ids)
-    _here(q, ids, out, lse, *k4, *v4)
+    here = _here(q, ids, out, lse)
     n_seq, n_q, d = q.shape
-    if (n_seq, n_q) != (idx.n_seq, idx.n_q_heads) or d != 128:
-        raise ValueError("q must be [n_seq][n_q][128], as the index has them")
-    if ids.dtype != torch.int32 or ids.dim() != 3 or tuple(ids.shape[:2]) != (n_seq, n_q):
+    n_kv = k4[0].shape[1]
+    if (n_seq, n_q, n_kv) != idx.heads or d != 128:
+        raise ValueError("q must be [n_seq][n_q][128], and its heads and the cache's those of the index")
+    if ids.dtype is not torch.int32 or ids.dim() != 3 or ids.shape[:2] != (n_seq, n_q):
         raise ValueError("ids must be int32 [n_seq][n_q][topk]")
-    room = _kv4(k4, n_seq, idx.n_kv_heads, "k4")
-    _kv4(v4, n_seq, idx.n_kv_heads, "v4", room)
+    K4, K4s, room = _kv4(k4, n_seq, n_kv, "k4", here)
+    V4, V4s, _ = _kv4(v4, n_seq, n_kv, "v4", here, room)
     out, lse = _results(n_seq, n_q, d, q.device, out, lse)
-    extra = [None] * 4
+    extra = ()
     if partials:
         f = dict(dtype=torch.float32, device=q.device)
-        extra = [torch.empty((n_seq, n_q, d), **f), torch.empty((n_seq, n_q), **f),
-                 torch.empty((n_seq, n_q, d), **f), torch.empty((n_seq, n_q), **f)]
-    _check(_room(lib().ra_attend_q4, _ptr(q), idx.handle, _dt(q), _ptr(k4[0]), _ptr(k4[1]), _ptr(v4[0]), _ptr(v4[1]),
-                 room if N is None else N, room, sink, window, ids.shape[-1], _ptr(ids), _stream(stream), _ptr(out), _ptr(lse),
-                 *[_ptr(t) for t in extra]))
+        extra = (torch.empty((n_seq, n_q, d), **f), torch.empty((n_seq, n_q), **f),
+                 torch.empty((n_seq, n_q, d), **f), torch.empty((n_seq, n_q), **f))
+    _check(_room(lib().ra_attend_q4, q.data_ptr(), idx.handle, _dt(q), K4, K4s, V4, V4s, room if N is None else N, room, sink, window,
+                 ids.shape[-1], ids.data_ptr(), _stream(stream), out.data_ptr(), lse.data_ptr(),
+                 *([t.data_ptr() for t in extra] or (None, None, None, None))))
     return (out, lse, *extra) if partials else (out, lse)

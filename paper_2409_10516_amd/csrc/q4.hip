@@ -5,75 +5,13 @@
 // z log2(e), the sum of weights), and a second kernel combines a head's records. Weights are powers of two,
 // p = 2^(c <q, k> - m) with c = log2(e) / sqrt(d): one multiply-add and one instruction each.
 #include "q4_dev.h"
+#include "ticket.h"
 
 #define Q4_THREADS 256
-#define Q4_GROUPS (Q4_THREADS / 16)
 #define Q4_REC (RA_D + 4)           // floats of a record: sums, maximum, sum of weights, 2 pad
 #define Q4_PART 128                 // rows of a part of the sparse set
 #define Q4_C ((float)(1.4426950408889634 / 11.313708498984761))
 #define Q4_LN2 0.6931471805599453f
-
-// the rows of a job: ids of a head, or [0, s) and then from `w` on
-struct Q4Rows {
-    const int32_t* ids;
-    int64_t N, s, w, count;
-};
-__device__ __forceinline__ int64_t q4_row(const Q4Rows& src, int64_t r) {
-    if (src.ids) {
-        const int64_t id = src.ids[r];
-        return id < src.N ? id : -1;
-    }
-    return r < src.s ? r : src.w + (r - src.s);
-}
-
-template <int DT>
-__device__ __forceinline__ void q4_part(const void* q, const Q4Cache& c, size_t kv_head, const Q4Rows& src, int64_t from, int64_t to,
-                                        float* rec) {
-    __shared__ float s_m[Q4_GROUPS], s_l[Q4_GROUPS], s_a[Q4_GROUPS][RA_D];
-    const int tid = threadIdx.x, grp = tid >> 4, l16 = tid & 15;
-    float qv[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-        qv[e] = DT == RA_BF16 ? bf16_lo(reinterpret_cast<const uint16_t*>(q)[8 * l16 + e]) : reinterpret_cast<const float*>(q)[8 * l16 + e];
-    float m = -INFINITY, l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int64_t r = from + grp; r < to; r += Q4_GROUPS) {
-        const int64_t id = q4_row(src, r);
-        if (id < 0) continue;
-        const size_t row = kv_head * c.kv_stride + id;
-        float k[8], v[8];
-        q4_values(reinterpret_cast<const uint32_t*>(c.k + row * Q4_ROW)[l16], q4_unit(c.ks[row * Q4_BLOCKS + l16 / 4]), k);
-        q4_values(reinterpret_cast<const uint32_t*>(c.v + row * Q4_ROW)[l16], q4_unit(c.vs[row * Q4_BLOCKS + l16 / 4]), v);
-        float dot = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) dot = fmaf(qv[e], k[e], dot);
-#pragma unroll
-        for (int d = 1; d < 16; d <<= 1) dot += __shfl_xor(dot, d);
-        const float z = dot * Q4_C, mn = fmaxf(m, z), base = mn == -INFINITY ? 0.f : mn;
-        const float corr = exp2f(m - base), p = exp2f(z - base);
-        m = mn;
-        l = l * corr + p;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] = fmaf(p, v[e], acc[e] * corr);
-    }
-    // (a sum that is not a number keeps a maximum that is one, or its record would count as empty)
-    if (l != l) m = 0.f;
-    if (l16 == 0) { s_m[grp] = m; s_l[grp] = l; }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) s_a[grp][8 * l16 + e] = acc[e];
-    __syncthreads();
-    if (tid < RA_D) {
-        float mx = -INFINITY, a = 0.f, ll = 0.f;
-        for (int g = 0; g < Q4_GROUPS; ++g) mx = fmaxf(mx, s_m[g]);
-        for (int g = 0; g < Q4_GROUPS; ++g)
-            if (s_m[g] > -INFINITY) {
-                const float w = exp2f(s_m[g] - mx);
-                a = fmaf(s_a[g][tid], w, a);
-                ll = fmaf(s_l[g], w, ll);
-            }
-        rec[tid] = a;
-        if (tid == 0) { rec[RA_D] = mx; rec[RA_D + 1] = ll; }
-    }
-}
 
 // ---- chunks of 32 rows on the matrix cores ---------------------------------------------------
 // A wavefront takes 32 rows at a time for a tile of query heads of one KV head, two products of v_mfma_f32_16x16x32_bf16
@@ -402,53 +340,166 @@ __global__ __launch_bounds__(Q4_MERGE_THREADS) void q4_full_merge_kernel(const f
     if (t == 0) lse[head] = mx > -INFINITY ? mx * Q4_LN2 + logf(ll) : -INFINITY;
 }
 
-template <int DT>
-__global__ __launch_bounds__(Q4_THREADS) void q4_attend_kernel(const void* __restrict__ q, Q4Cache c, int n_q, int n_kv, int64_t N,
-                                                               int64_t s, int64_t w, int topk, const int32_t* __restrict__ ids, int nS,
-                                                               float* __restrict__ partials) {
-    const int x = blockIdx.x, h = blockIdx.y, seq = blockIdx.z;
-    const size_t head = (size_t)seq * n_q + h;
-    const Q4Rows src = x < nS ? Q4Rows{nullptr, N, s, w, s + N - w} : Q4Rows{ids + head * topk, N, 0, 0, topk};
-    const int64_t from = (int64_t)(x < nS ? x : x - nS) * Q4_PART, to = from + Q4_PART < src.count ? from + Q4_PART : src.count;
-    q4_part<DT>(reinterpret_cast<const char*>(q) + head * RA_D * (DT == RA_BF16 ? 2 : 4), c, (size_t)seq * n_kv + h / (n_q / n_kv), src,
-                from, to, partials + (head * gridDim.x + x) * Q4_REC);
+// ---- the retrieved set and the static set -------------------------------------------------------
+struct Q4Out {
+    uint32_t* tickets;                  // one word per query head (ticket.h), or null
+    float *out, *lse, *o_om, *lse_om, *o_w, *lse_w;
+};
+
+// the rows of a job: ids of a head, or [0, s) and then from `w` on
+struct Q4Rows {
+    const int32_t* ids;
+    int64_t N, s, w;
+    int count;
+};
+__device__ __forceinline__ int q4_row(const Q4Rows& src, int r) {
+    if (src.ids) {
+        const int id = src.ids[r < src.count ? r : src.count - 1];
+        return r < src.count && id < src.N ? id : -1;
+    }
+    return r >= src.count ? -1 : r < src.s ? r : (int)(src.w - src.s) + r;
+}
+// rows [at, at + 32) of a job; returns which of the lane's rows there are. Loads are never branched around: a row that is
+// not there is row 0.
+__device__ __forceinline__ uint32_t q4_gather(Q4Chunk& c, const Q4Cache& h, const Q4Rows& src, int at, int lane) {
+    const int kg = lane >> 4, r = lane & 15;
+    int kr[2], vr[8];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) kr[t] = q4_row(src, at + 16 * t + r);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) vr[j] = q4_row(src, at + (j & 4) * 4 + 4 * kg + (j & 3));
+    uint32_t there = 0u;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const size_t row = kr[t] >= 0 ? kr[t] : 0;
+        c.k[t] = *reinterpret_cast<const uint4*>(h.k + row * Q4_ROW + 16 * kg);
+        c.ks[t] = h.ks[row * Q4_BLOCKS + kg];
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const size_t row = vr[j] >= 0 ? vr[j] : 0;
+        c.v[j] = *reinterpret_cast<const uint32_t*>(h.v + row * Q4_ROW + 4 * r);
+        c.vs[j] = *reinterpret_cast<const uint32_t*>(h.vs + row * Q4_BLOCKS);
+        there |= (vr[j] >= 0 ? 1u : 0u) << j;
+    }
+    return there;
 }
 
-struct Q4Out { float *out, *lse, *o_om, *lse_om, *o_w, *lse_w; };
+template <bool COHERENT>
+__device__ __forceinline__ void q4_store(float* p, float v) {
+    if (COHERENT) __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    else *p = v;
+}
+template <bool COHERENT>
+__device__ __forceinline__ float q4_load(const float* p) {
+    return COHERENT ? __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : *p;
+}
 
-// grid: x = head (with its sequence); records of the static set (0) and then of Omega (1)
-__global__ __launch_bounds__(RA_D) void q4_merge_kernel(const float* __restrict__ partials, int nS, int nG, Q4Out o) {
-    const size_t head = blockIdx.x;
-    const int t = threadIdx.x;
-    const float* rec = partials + head * (nS + nG) * Q4_REC;
+// Dimension d of a head from its records, nS of the static set and nG of Omega: Eq. 4 for each, Eq. 5 for both.
+template <bool COHERENT>
+__device__ __forceinline__ void q4_finish(const float* rec, int nS, int nG, size_t head, int d, const Q4Out& o) {
     float M[2] = {-INFINITY, -INFINITY}, L[2] = {0.f, 0.f}, A[2] = {0.f, 0.f};
+    constexpr int FLY = 8;
 #pragma unroll
-    for (int set = 0; set < 2; ++set)
-        for (int i = set ? nS : 0; i < (set ? nS + nG : nS); ++i) {
-            const float m = rec[(size_t)i * Q4_REC + RA_D];
-            if (m == -INFINITY) continue;
-            const float mx = fmaxf(M[set], m), c0 = exp2f(M[set] - mx), c1 = exp2f(m - mx);
-            A[set] = A[set] * c0 + rec[(size_t)i * Q4_REC + t] * c1;
-            L[set] = L[set] * c0 + rec[(size_t)i * Q4_REC + RA_D + 1] * c1;
+    for (int set = 0; set < 2; ++set) {
+        const int first = set ? nS : 0, last = set ? nS + nG : nS;
+        for (int i0 = first; i0 < last; i0 += FLY) {
+            float m[FLY], l[FLY], a[FLY];
+#pragma unroll
+            for (int u = 0; u < FLY; ++u) {
+                const float* x = rec + (size_t)(i0 + u < last ? i0 + u : last - 1) * Q4_REC;
+                m[u] = q4_load<COHERENT>(x + RA_D);
+                l[u] = q4_load<COHERENT>(x + RA_D + 1);
+                a[u] = q4_load<COHERENT>(x + d);
+            }
+            float mx = M[set];
+#pragma unroll
+            for (int u = 0; u < FLY; ++u) mx = fmaxf(mx, m[u]);
+            if (mx == -INFINITY) continue;
+            const float corr = __builtin_amdgcn_exp2f(M[set] - mx);
+            A[set] *= corr;
+            L[set] *= corr;
+#pragma unroll
+            for (int u = 0; u < FLY; ++u) {
+                const float w = i0 + u < last ? __builtin_amdgcn_exp2f(m[u] - mx) : 0.f;
+                A[set] = fmaf(a[u], w, A[set]);
+                L[set] = fmaf(l[u], w, L[set]);
+            }
             M[set] = mx;
         }
+    }
     float* o_set[2] = {o.o_w, o.o_om};
     float* l_set[2] = {o.lse_w, o.lse_om};
 #pragma unroll
     for (int set = 0; set < 2; ++set) {
         const bool empty = M[set] == -INFINITY;
-        if (o_set[set]) o_set[set][head * RA_D + t] = empty ? 0.f : A[set] / L[set];
-        if (l_set[set] && t == 0) l_set[set][head] = empty ? -INFINITY : M[set] * Q4_LN2 + logf(L[set]);
+        if (o_set[set]) o_set[set][head * RA_D + d] = empty ? 0.f : A[set] / L[set];
+        if (l_set[set] && d == 0) l_set[set][head] = empty ? -INFINITY : M[set] * Q4_LN2 + logf(L[set]);
     }
     const float mx = fmaxf(M[0], M[1]);
     float out = 0.f, lse = -INFINITY;
     if (mx > -INFINITY) {
-        const float e0 = exp2f(M[0] - mx), e1 = exp2f(M[1] - mx), l = L[0] * e0 + L[1] * e1;
+        const float e0 = __builtin_amdgcn_exp2f(M[0] - mx), e1 = __builtin_amdgcn_exp2f(M[1] - mx), l = L[0] * e0 + L[1] * e1;
         out = (A[0] * e0 + A[1] * e1) / l;
         lse = mx * Q4_LN2 + logf(l);
     }
-    o.out[head * RA_D + t] = out;
-    if (t == 0) o.lse[head] = lse;
+    o.out[head * RA_D + d] = out;
+    if (d == 0) o.lse[head] = lse;
+}
+
+// grid: per (sequence, KV head) the parts of each of its query heads' Omega (their loads wait for ids, so they start first), then
+// the parts of the static set per tile of heads. `spanS`, `spanG`: rows of a part. TICKETS: the workgroup that stores a head's last
+// record combines them all (ticket.h), which saves a launch.
+template <int DT, bool TICKETS>
+__global__ __launch_bounds__(Q4_THREADS) void q4_attend_kernel(const void* __restrict__ q, Q4Cache c, int n_q, int n_kv, int64_t N,
+                                                               int64_t s, int64_t w, int topk, const int32_t* __restrict__ ids, int nS,
+                                                               int nG, int spanS, int spanG, int tiles, float* partials, Q4Out o) {
+    typedef Q4Form<DT> F;
+    __shared__ Q4Lds lds;
+    __shared__ uint32_t s_last[F::HEADS];
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid / RA_WAVE);
+    const int group = n_q / n_kv, per = tiles * nS + group * nG, P = nS + nG;
+    const size_t kv_head = blockIdx.x / per;
+    const int x = blockIdx.x % per;
+    const size_t group0 = kv_head / n_kv * n_q + kv_head % n_kv * group;
+    const bool om = x < group * nG;
+    const int first = om ? x / nG : (x - group * nG) / nS * F::HEADS;        // of the group's heads
+    const int part = om ? x % nG : (x - group * nG) % nS, slot = om ? nS + part : part;
+    const int heads = om ? 1 : group - first < F::HEADS ? group - first : F::HEADS;
+    const size_t head0 = group0 + first;
+    const Q4Cache h{c.k + kv_head * c.kv_stride * Q4_ROW, c.ks + kv_head * c.kv_stride * Q4_BLOCKS, c.v + kv_head * c.kv_stride * Q4_ROW,
+                    c.vs + kv_head * c.kv_stride * Q4_BLOCKS, c.kv_stride};
+    const Q4Rows src = om ? Q4Rows{ids + head0 * topk, N, 0, 0, topk} : Q4Rows{nullptr, N, s, w, (int)(s + N - w)};
+    const int span = om ? spanG : spanS, from = part * span, to = from + span < src.count ? from + span : src.count;
+    Q4Wave<DT> st;
+    st.start(reinterpret_cast<const char*>(q) + head0 * RA_D * (DT == RA_BF16 ? 2 : 4), heads, lane);
+    for (int at = from + wv * Q4_CHUNK; at < to; at += Q4_WAVES * Q4_CHUNK) {
+        Q4Chunk ch;
+        const uint32_t there = q4_gather(ch, h, src, at, lane);
+        st.template add<false>(ch, there, lane);
+    }
+    q4_close<DT>(st, lds, heads, [&](int hd, int d, float sum, float mx, float l) {
+        float* rec = partials + ((head0 + hd) * P + slot) * Q4_REC;
+        q4_store<TICKETS>(rec + d, sum);
+        if (d == 0) { q4_store<TICKETS>(rec + RA_D, mx); q4_store<TICKETS>(rec + RA_D + 1, l); }
+    });
+    if constexpr (TICKETS) {
+        __builtin_amdgcn_s_waitcnt(0x0F70);     // vmcnt(0): this wavefront's record stores have completed
+        __syncthreads();                        // ... and every other's
+        if (tid < heads) {
+            const uint32_t step = ticket_step(slot, P);
+            s_last[tid] = ticket_last(__hip_atomic_fetch_add(o.tickets + head0 + tid, step, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), step);
+        }
+        __syncthreads();
+        for (int y = tid; y < heads * RA_D; y += Q4_THREADS)
+            if (s_last[y / RA_D]) q4_finish<true>(partials + (head0 + y / RA_D) * P * Q4_REC, nS, nG, head0 + y / RA_D, y % RA_D, o);
+    }
+}
+
+// grid: x = head (with its sequence)
+__global__ __launch_bounds__(RA_D) void q4_merge_kernel(const float* __restrict__ partials, int nS, int nG, Q4Out o) {
+    const size_t head = blockIdx.x;
+    q4_finish<false>(partials + head * (nS + nG) * Q4_REC, nS, nG, head, threadIdx.x, o);
 }
 
 // Rows of a part of all tokens, a multiple of what a workgroup's wavefronts take at once: parts for about four workgroups
@@ -499,27 +550,52 @@ static void q4_static(int64_t N, int64_t Ng, int sink, int window, int64_t* s, i
     if (*w <= *s) { *s = N; *w = N; }
 }
 
-size_t ra_attend_q4_partial_floats(ra_dtype, int n_seq, int n_q, int, int64_t N, int64_t Ng, int sink, int window, int topk) {
+// parts of the two sets: 128 rows each, a chunk for each wavefront of a workgroup; longer ones where they would be very many
+struct Q4Parts { int nS, nG, spanS, spanG, tiles; };
+static Q4Parts q4_parts(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t n_static, int topk) {
+    const int heads = dt == RA_BF16 ? Q4Form<RA_BF16>::HEADS : Q4Form<RA_F32>::HEADS;
+    Q4Parts p;
+    p.tiles = (n_q / n_kv + heads - 1) / heads;
+    p.spanG = Q4_PART;
+    p.nG = (topk + p.spanG - 1) / p.spanG;
+    int64_t most = 2048 / ((int64_t)n_seq * n_kv * p.tiles);
+    if (most < 1) most = 1;
+    int64_t nS = (n_static + Q4_PART - 1) / Q4_PART;
+    if (nS > most) nS = most;
+    if (nS < 1) nS = n_static > 0;
+    p.spanS = nS ? (int)((n_static + nS - 1) / nS + Q4_PART - 1) / Q4_PART * Q4_PART : Q4_PART;
+    p.nS = (int)((n_static + p.spanS - 1) / p.spanS);
+    return p;
+}
+
+size_t ra_attend_q4_partial_floats(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N, int64_t Ng, int sink, int window, int topk) {
     int64_t s, w;
     q4_static(N, Ng, sink, window, &s, &w);
-    return (size_t)n_seq * n_q * ((s + N - w + Q4_PART - 1) / Q4_PART + (topk + Q4_PART - 1) / Q4_PART) * Q4_REC;
+    const Q4Parts p = q4_parts(dt, n_seq, n_q, n_kv, s + N - w, topk);
+    return (size_t)n_seq * n_q * (p.nS + p.nG) * Q4_REC;
 }
+
+#define Q4_TICKET_RECORDS 512
 
 ra_status ra_launch_attend_q4(const void* q, ra_dtype dt, const Q4Cache& c, int n_seq, int n_q, int n_kv, int64_t N, int64_t Ng,
                               int sink, int window, int topk, const int32_t* ids, float* partials, uint32_t* tickets,
                               hipStream_t st, float* out, float* lse, float* o_omega, float* lse_omega, float* o_w, float* lse_w) {
-    (void)tickets;
     int64_t s, w;
     q4_static(N, Ng, sink, window, &s, &w);
-    const int nS = (int)((s + N - w + Q4_PART - 1) / Q4_PART), nG = (topk + Q4_PART - 1) / Q4_PART;
-    const dim3 grid(nS + nG, n_q, n_seq);
-    if (dt == RA_BF16)
-        hipLaunchKernelGGL(q4_attend_kernel<RA_BF16>, grid, dim3(Q4_THREADS), 0, st, q, c, n_q, n_kv, N, s, w, topk, ids, nS, partials);
-    else
-        hipLaunchKernelGGL(q4_attend_kernel<RA_F32>, grid, dim3(Q4_THREADS), 0, st, q, c, n_q, n_kv, N, s, w, topk, ids, nS, partials);
+    const Q4Parts p = q4_parts(dt, n_seq, n_q, n_kv, s + N - w, topk);
+    const int64_t blocks = (int64_t)n_seq * n_kv * (p.tiles * p.nS + n_q / n_kv * p.nG);
+    if (blocks > (1 << 24) - 1) RA_FAIL(RA_EUNSUP, "too many heads for one launch");
+    if ((int64_t)n_seq * n_q * (p.nS + p.nG) > Q4_TICKET_RECORDS) tickets = nullptr;
+    const Q4Out o{tickets, out, lse, o_omega, lse_omega, o_w, lse_w};
+#define Q4_GO(DTV, TK)                                                                                                       \
+    hipLaunchKernelGGL((q4_attend_kernel<DTV, TK>), dim3((unsigned)blocks), dim3(Q4_THREADS), 0, st, q, c, n_q, n_kv, N, s, w, topk, ids, \
+                       p.nS, p.nG, p.spanS, p.spanG, p.tiles, partials, o)
+    if (dt == RA_BF16) { if (tickets) Q4_GO(RA_BF16, true); else Q4_GO(RA_BF16, false); }
+    else { if (tickets) Q4_GO(RA_F32, true); else Q4_GO(RA_F32, false); }
+#undef Q4_GO
     RA_HIP(hipGetLastError());
-    hipLaunchKernelGGL(q4_merge_kernel, dim3(n_seq * n_q), dim3(RA_D), 0, st, partials, nS, nG,
-                       Q4Out{out, lse, o_omega, lse_omega, o_w, lse_w});
+    if (tickets) return RA_OK;
+    hipLaunchKernelGGL(q4_merge_kernel, dim3(n_seq * n_q), dim3(RA_D), 0, st, partials, p.nS, p.nG, o);
     RA_HIP(hipGetLastError());
     return RA_OK;
 }
