@@ -7,16 +7,24 @@
 #define KV_THREADS 256
 #define KV_GROUPS (KV_THREADS / 16)
 
-// values [8 l16, 8 l16 + 8) of a row
+// values [8 l16, 8 l16 + 8) of a row, as loaded. Rows are read once and written once: non-temporal both ways (131072 rows of 8 heads
+// into 4 bits and back 131 -> 119 us with such loads, 112 with such stores; a 32K prompt's rows 196 -> 194, 191).
+typedef uint32_t kv_u32x4 __attribute__((ext_vector_type(4)));
+template <int DT> struct KvRaw { kv_u32x4 a[DT == RA_BF16 ? 1 : 2]; };
 template <int DT>
-__device__ __forceinline__ void kv_load8(const void* row, int l16, float (&v)[8]) {
-    if constexpr (DT == RA_BF16) {
-        const uint4 u = reinterpret_cast<const uint4*>(row)[l16];
-        v[0] = bf16_lo(u.x); v[1] = bf16_hi(u.x); v[2] = bf16_lo(u.y); v[3] = bf16_hi(u.y);
-        v[4] = bf16_lo(u.z); v[5] = bf16_hi(u.z); v[6] = bf16_lo(u.w); v[7] = bf16_hi(u.w);
-    } else {
-        const float4 a = reinterpret_cast<const float4*>(row)[2 * l16], b = reinterpret_cast<const float4*>(row)[2 * l16 + 1];
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+__device__ __forceinline__ KvRaw<DT> kv_load8(const void* row, int l16) {
+    constexpr int W = DT == RA_BF16 ? 1 : 2;
+    KvRaw<DT> x;
+#pragma unroll
+    for (int i = 0; i < W; ++i) x.a[i] = __builtin_nontemporal_load(reinterpret_cast<const kv_u32x4*>(row) + W * l16 + i);
+    return x;
+}
+template <int DT>
+__device__ __forceinline__ void kv_floats(const KvRaw<DT>& x, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if constexpr (DT == RA_BF16) v[e] = e & 1 ? bf16_hi(x.a[0][e / 2]) : bf16_lo(x.a[0][e / 2]);
+        else v[e] = __uint_as_float(x.a[e / 4][e & 3]);
     }
 }
 typedef __bf16 kv_bf16x8 __attribute__((ext_vector_type(8)));
@@ -29,14 +37,17 @@ __device__ __forceinline__ void kv_round8(float (&v)[8]) {
 }
 template <int DT>
 __device__ __forceinline__ void kv_store8(void* row, int l16, const float (&v)[8]) {
+    kv_u32x4* to = reinterpret_cast<kv_u32x4*>(row);
     if constexpr (DT == RA_BF16) {
         kv_bf16x8 b;
 #pragma unroll
         for (int e = 0; e < 8; ++e) b[e] = (__bf16)v[e];
-        reinterpret_cast<uint4*>(row)[l16] = __builtin_bit_cast(uint4, b);
+        __builtin_nontemporal_store(__builtin_bit_cast(kv_u32x4, b), to + l16);
     } else {
-        reinterpret_cast<float4*>(row)[2 * l16] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4*>(row)[2 * l16 + 1] = make_float4(v[4], v[5], v[6], v[7]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            __builtin_nontemporal_store(kv_u32x4{__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]),
+                                                 __float_as_uint(v[4 * i + 3])}, to + 2 * l16 + i);
     }
 }
 // A row of 16 lanes x 8 values into 4 bits. Called by whole groups of 16 lanes.
@@ -48,96 +59,163 @@ __device__ __forceinline__ void kv_store4(uint8_t* codes, uint8_t* scale, int l1
     m = max(m, lane_xor32<2>(m, lane));
     const uint32_t byte = q4_scale_byte(m);
     reinterpret_cast<uint32_t*>(codes)[l16] = q4_codes(v, byte);
-    if ((l16 & 3) == 0) scale[l16 / 4] = (uint8_t)byte;
+    uint32_t all = byte << (8 * (l16 / 4));              // the four blocks' bytes, in one word
+    all |= lane_xor32<4>(all, lane);
+    all |= lane_xor32<8>(all, lane);
+    if (l16 == 0) *reinterpret_cast<uint32_t*>(scale) = all;
 }
 
-// One workgroup per token: the sines and cosines of its angles, then its heads' rows, one per 16 lanes.
+__device__ __forceinline__ double xor_add(double x, uint32_t lo, uint32_t hi) {
+    return x + __hiloint2double((int)hi, (int)lo);
+}
+// sum over a row of 16 lanes, the same in all of them
+__device__ __forceinline__ double sum16(double x, int lane) {
+    uint32_t lo, hi;
+#define KV_STEP(J)                                                                             \
+    lo = (uint32_t)__double2loint(x); hi = (uint32_t)__double2hiint(x);                        \
+    x = xor_add(x, lane_xor32<J>(lo, lane), lane_xor32<J>(hi, lane));
+    KV_STEP(1) KV_STEP(2) KV_STEP(4) KV_STEP(8)
+#undef KV_STEP
+    return x;
+}
+
+// 1 / sqrt(x) to the last few bits of a double: the hardware's estimate and one step of Newton's method
+__device__ __forceinline__ double rsqrt64(double x) {
+    const double y = __builtin_amdgcn_rsq(x), z = y * fma(-0.5 * x * y, y, 1.5);
+    return y > 0. && y < INFINITY ? z : y;               // (zero and infinity are their own)
+}
+
+// The sine and cosine of x, to float32: x less the nearest multiple of pi / 2, in two parts, and the series of both about zero,
+// to terms below 2^-44 of the result at pi / 4.
+__device__ __forceinline__ float2 cos_sin64(double x) {
+    const double n = rint(x * 0.63661977236758134308);
+    const double r = fma(-n, 6.123233995736766036e-17, fma(-n, 1.57079632679489655800, x)), t = r * r;
+    double s = fma(t, 1. / 6227020800., -1. / 39916800.), c = fma(t, -1. / 87178291200., 1. / 479001600.);
+    s = fma(t, s, 1. / 362880.); c = fma(t, c, -1. / 3628800.);
+    s = fma(t, s, -1. / 5040.); c = fma(t, c, 1. / 40320.);
+    s = fma(t, s, 1. / 120.); c = fma(t, c, -1. / 720.);
+    s = fma(t, s, -1. / 6.); c = fma(t, c, 1. / 24.);
+    s = fma(t * r, s, r); c = fma(t, c, -0.5);
+    c = fma(t, c, 1.);
+    const int k = (int)((long long)n & 3);               // quarter turns
+    const float fs = (float)(k & 1 ? c : s), fc = (float)(k & 1 ? s : c);
+    return make_float2(k == 1 || k == 2 ? -fc : fc, k & 2 ? -fs : fs);
+}
+
+// the value that the lane `step` further in the row's rotated part holds for the lower half, `step` back for the upper
+template <int STEP>
+__device__ __forceinline__ float other_half(float v, int lane, int from) {
+    if constexpr (STEP == 0) return __shfl(v, from);
+    else return __uint_as_float(lane_xor32<STEP>(__float_as_uint(v), lane));
+}
+template <int STEP>
+__device__ __forceinline__ void turn_halves(float (&v)[8], const float2* cs, bool in_rot, bool low, int lane, int from) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float other = other_half<STEP>(v[e], lane, from);
+        if (in_rot) v[e] = v[e] * cs[e].x + (low ? -other : other) * cs[e].y;
+    }
+}
+
+// A workgroup takes a token, or with few tokens, one of `split` parts of its heads: the sines and cosines of the token's angles, one
+// per lane of its first wavefront, then the heads' rows, one per 16 lanes. The first rows are asked for before the angles are
+// worked on. What this is bound by is how many rows are in flight: registers for eight wavefronts per SIMD.
+// A 32K prompt of 32 + 8 + 8 heads, us: with four tokens per workgroup, their factors and the weights in registers, and one row
+// asked for ahead 303; the same with one token 285.
 template <int DT>
-__global__ __launch_bounds__(KV_THREADS) void append_kernel(AppendArgs a) {
+__global__ __launch_bounds__(KV_THREADS) void append_kernel(AppendArgs a, int split) {
     __shared__ float2 s_cs[RA_D / 2];
+    __shared__ float4 s_w[2][RA_D / 4];
     const int tid = threadIdx.x, lane = tid & (RA_WAVE - 1), l16 = tid & 15, grp = tid >> 4;
     const size_t esz = DT == RA_BF16 ? 2 : 4;
-    const int64_t tok = blockIdx.x, seq = tok / a.T, t = tok % a.T;
+    const int T = (int)a.T, tok = blockIdx.x / split, seq = tok / T, t = tok % T;
     if (a.n_new && t >= a.n_new[seq]) return;                       // (uniform)
-    const int64_t pos = (a.first ? a.first[seq] : 0) + t;
-    const int rot = a.rot, half = rot / 2;
-    if (tid < half) {
-        double s, c;
-        sincos((double)pos * (double)a.inv_freq[tid], &s, &c);
-        s_cs[tid] = make_float2((float)c, (float)s);
+    const int64_t pos = (int64_t)(a.first ? a.first[seq] : 0) + t;
+    const bool there[2] = {pos >= 0 && pos < a.stride[0], pos >= 0 && pos < a.stride[1]};
+    const int n_rows = a.n_q + 2 * a.n_kv, step = KV_GROUPS * split, rot = a.rot, half = rot / 2;
+    // a row's input; none where there is no such row, no input, or no cache that has the row
+    auto row_of = [&](int r) __attribute__((always_inline)) -> const char* {
+        if (r >= n_rows) return nullptr;
+        const int which = r < a.n_q ? 0 : r < a.n_q + a.n_kv ? 1 : 2;
+        if (!a.in[which] || (which && !there[0] && !there[1])) return nullptr;
+        const int h = which == 0 ? r : which == 1 ? r - a.n_q : r - a.n_q - a.n_kv;
+        return reinterpret_cast<const char*>(a.in[which]) + ((size_t)tok * a.row[which] + (size_t)h * RA_D) * esz;
+    };
+    if (tid < half) s_cs[tid] = cos_sin64((double)pos * (double)a.inv_freq[tid]);
+    if (tid >= KV_THREADS - RA_D) {                                // (other wavefronts than those of the angles)
+        const int d = tid - (KV_THREADS - RA_D);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (a.weight[i])
+                reinterpret_cast<float*>(s_w[i])[d] = DT == RA_BF16 ? bf16_lo(reinterpret_cast<const uint16_t*>(a.weight[i])[d])
+                                                                    : reinterpret_cast<const float*>(a.weight[i])[d];
     }
     __syncthreads();
-    const int n_rows = a.n_q + 2 * a.n_kv;
-    for (int r = grp; r < n_rows; r += KV_GROUPS) {
+    const int near = half / 8;                                     // lanes of a half
+    const bool low = l16 < near, in_rot = l16 < 2 * near;
+    const int from = (lane & ~15) + (low ? l16 + near : in_rot ? l16 - near : l16);
+    const float2* cs = s_cs + (!in_rot ? 0 : a.interleaved ? 4 * l16 : 8 * (low ? l16 : l16 - near));
+    for (int r = grp + (int)(blockIdx.x % split) * KV_GROUPS; r < n_rows; r += step) {
+        const char* in = row_of(r);
+        if (!in) continue;
         const int which = r < a.n_q ? 0 : r < a.n_q + a.n_kv ? 1 : 2;
         const int h = which == 0 ? r : which == 1 ? r - a.n_q : r - a.n_q - a.n_kv;
-        const char* in = reinterpret_cast<const char*>(a.in[which]);
-        const bool row_there = pos >= 0 && pos < a.stride[0], row4_there = pos >= 0 && pos < a.stride[1];
-        if (!in || (which && !row_there && !row4_there)) continue;
         float v[8];
-        kv_load8<DT>(in + ((size_t)tok * a.row[which] + (size_t)h * RA_D) * esz, l16, v);
+        kv_floats<DT>(kv_load8<DT>(in, l16), v);
         if (which < 2) {
-            if (const void* weight = a.weight[which]) {
+            if (a.weight[which]) {
                 double sum = 0.;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum += (double)v[e] * (double)v[e];
+                for (int e = 0; e < 8; ++e) sum = fma((double)v[e], (double)v[e], sum);
+                const float rinv = (float)rsqrt64(sum16(sum, lane) * (1. / RA_D) + a.eps);
+                const float4 w0 = s_w[which][2 * l16], w1 = s_w[which][2 * l16 + 1];
+                const float w[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
 #pragma unroll
-                for (int d = 1; d < 16; d <<= 1) sum += __shfl_xor(sum, d);
-                const float rinv = (float)(1.0 / sqrt(sum / RA_D + a.eps));
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int d = 8 * l16 + e;
-                    const float w = DT == RA_BF16 ? bf16_lo(reinterpret_cast<const uint16_t*>(weight)[d])
-                                                  : reinterpret_cast<const float*>(weight)[d];
-                    v[e] = v[e] * rinv * w;
-                }
+                for (int e = 0; e < 8; ++e) v[e] = v[e] * rinv * w[e];
             }
             if (a.interleaved) {
-                if (8 * l16 < rot)
+                if (in_rot)
 #pragma unroll
                     for (int e = 0; e < 8; e += 2) {
-                        const float2 cs = s_cs[4 * l16 + e / 2];
                         const float x = v[e], y = v[e + 1];
-                        v[e] = x * cs.x - y * cs.y;
-                        v[e + 1] = y * cs.x + x * cs.y;
+                        v[e] = x * cs[e / 2].x - y * cs[e / 2].y;
+                        v[e + 1] = y * cs[e / 2].x + x * cs[e / 2].y;
                     }
-            } else if (rot) {
-                const int step = half / 8;
-                const bool low = l16 < step, in_rot = l16 < 2 * step;
-                const int from = (lane & ~15) + (low ? l16 + step : in_rot ? l16 - step : l16);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float other = __shfl(v[e], from);
-                    if (in_rot) {
-                        const float2 cs = s_cs[8 * (low ? l16 : l16 - step) + e];
-                        v[e] = low ? v[e] * cs.x - other * cs.y : v[e] * cs.x + other * cs.y;
-                    }
-                }
-            }
+            } else if (near == 8) turn_halves<8>(v, cs, in_rot, low, lane, from);
+            else if (near == 4) turn_halves<4>(v, cs, in_rot, low, lane, from);
+            else if (near) turn_halves<0>(v, cs, in_rot, low, lane, from);
             kv_round8<DT>(v);
         }
         if (which == 0) {
-            kv_store8<DT>(reinterpret_cast<char*>(a.out[0]) + (((size_t)seq * a.n_q + h) * a.T + t) * RA_D * esz, l16, v);
+            kv_store8<DT>(reinterpret_cast<char*>(a.out[0]) + (((size_t)seq * a.n_q + h) * T + t) * RA_D * esz, l16, v);
         } else {
             const size_t head = (size_t)seq * a.n_kv + h, row = head * a.stride[0] + pos, row4 = head * a.stride[1] + pos;
-            if (a.out[which] && row_there) kv_store8<DT>(reinterpret_cast<char*>(a.out[which]) + row * RA_D * esz, l16, v);
-            if (a.codes[which - 1] && row4_there)
+            if (a.out[which] && there[0]) kv_store8<DT>(reinterpret_cast<char*>(a.out[which]) + row * RA_D * esz, l16, v);
+            if (a.codes[which - 1] && there[1])
                 kv_store4(a.codes[which - 1] + row4 * Q4_ROW, a.scale[which - 1] + row4 * Q4_BLOCKS, l16, lane, v);
         }
     }
 }
 
 ra_status ra_launch_append(const AppendArgs& a, ra_dtype dt, hipStream_t st) {
-    const int64_t blocks = a.T * a.n_seq;
-    if (blocks > (1u << 24) - 1) RA_FAIL(RA_EUNSUP, "more than 2^24 - 1 tokens in a call");
-    if (dt == RA_BF16) hipLaunchKernelGGL(append_kernel<RA_BF16>, dim3((unsigned)blocks), dim3(KV_THREADS), 0, st, a);
-    else hipLaunchKernelGGL(append_kernel<RA_F32>, dim3((unsigned)blocks), dim3(KV_THREADS), 0, st, a);
+    const int64_t tokens = a.T * a.n_seq;
+    if (tokens > (1 << 24) - 1) RA_FAIL(RA_EUNSUP, "more than 2^24 - 1 tokens in a call");
+    // where a workgroup per token leaves compute units idle, a workgroup for every 16 heads of one
+    const int heads = a.n_q + 2 * a.n_kv, split = tokens <= 128 ? (heads + KV_GROUPS - 1) / KV_GROUPS : 1;
+    const int64_t blocks = tokens * split;
+    if (blocks > (1 << 24) - 1) RA_FAIL(RA_EUNSUP, "too many heads for one launch");
+#define KV_GO(DTV) hipLaunchKernelGGL(append_kernel<DTV>, dim3((unsigned)blocks), dim3(KV_THREADS), 0, st, a, split)
+    if (dt == RA_BF16) KV_GO(RA_BF16); else KV_GO(RA_F32);
+#undef KV_GO
     RA_HIP(hipGetLastError());
     return RA_OK;
 }
 
-// grid: x = rows of a head, 16 to a workgroup, y = head (with its sequence)
-template <int DT>
+// grid: x = rows of a head, KV_GROUPS x FLY to a workgroup, y = head (with its sequence). A group of 16 lanes takes FLY rows, whose
+// loads are all on their way before the first is worked on; a row that is not there is loaded as another one that is. Four rows where
+// there are many, else one (us into 4 bits and back: 8 heads of 131072 bf16 rows 105 with four, 108 with one, 112 with eight; 6 heads
+// of 1003 float32 rows 7.0, 5.7, 9.0).
+template <int DT, int FLY>
 __global__ __launch_bounds__(KV_THREADS) void quantize_kv4_kernel(const void* __restrict__ X, int n_kv, int64_t T,
                                                                   const int32_t* __restrict__ first, const int32_t* __restrict__ n_new,
                                                                   int64_t kv_stride, uint8_t* __restrict__ codes,
@@ -145,48 +223,82 @@ __global__ __launch_bounds__(KV_THREADS) void quantize_kv4_kernel(const void* __
     const int tid = threadIdx.x, lane = tid & (RA_WAVE - 1), l16 = tid & 15;
     const size_t head = blockIdx.y;
     const int seq = (int)(head / n_kv);
-    const int64_t t = (int64_t)blockIdx.x * KV_GROUPS + (tid >> 4), at = t + (first ? first[seq] : 0);
-    if (t >= T || (n_new && t >= n_new[seq]) || at < 0 || at >= kv_stride) return;
-    float v[8];
-    kv_load8<DT>(reinterpret_cast<const char*>(X) + (head * T + t) * RA_D * (DT == RA_BF16 ? 2 : 4), l16, v);
-    const size_t row = head * kv_stride + at;
-    kv_store4(codes + row * Q4_ROW, scale + row * Q4_BLOCKS, l16, lane, v);
+    const int64_t t0 = (int64_t)blockIdx.x * (KV_GROUPS * FLY) + (tid >> 4), at0 = first ? first[seq] : 0;
+    const int64_t n = n_new && n_new[seq] < T ? n_new[seq] : T;
+    const char* rows = reinterpret_cast<const char*>(X) + head * T * RA_D * (DT == RA_BF16 ? 2 : 4);
+    KvRaw<DT> raw[FLY];
+#pragma unroll
+    for (int u = 0; u < FLY; ++u) {
+        const int64_t t = t0 + KV_GROUPS * u;
+        raw[u] = kv_load8<DT>(rows + (t < T ? t : T - 1) * RA_D * (DT == RA_BF16 ? 2 : 4), l16);
+    }
+#pragma unroll
+    for (int u = 0; u < FLY; ++u) {
+        const int64_t t = t0 + KV_GROUPS * u, at = at0 + t;
+        if (t >= n || at < 0 || at >= kv_stride) continue;
+        float v[8];
+        kv_floats<DT>(raw[u], v);
+        const size_t row = head * kv_stride + at;
+        kv_store4(codes + row * Q4_ROW, scale + row * Q4_BLOCKS, l16, lane, v);
+    }
 }
 
-template <int DT>
+template <int DT, int FLY>
 __global__ __launch_bounds__(KV_THREADS) void dequantize_kv4_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scale,
                                                                     int n_kv, int64_t T, const int32_t* __restrict__ first,
                                                                     int64_t kv_stride, void* __restrict__ X) {
     const int tid = threadIdx.x, l16 = tid & 15;
     const size_t head = blockIdx.y;
     const int seq = (int)(head / n_kv);
-    const int64_t t = (int64_t)blockIdx.x * KV_GROUPS + (tid >> 4), at = t + (first ? first[seq] : 0);
-    if (t >= T) return;
-    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (at >= 0 && at < kv_stride) {
-        const size_t row = head * kv_stride + at;
-        q4_values(reinterpret_cast<const uint32_t*>(codes + row * Q4_ROW)[l16], q4_unit(scale[row * Q4_BLOCKS + l16 / 4]), v);
+    const int64_t t0 = (int64_t)blockIdx.x * (KV_GROUPS * FLY) + (tid >> 4), at0 = first ? first[seq] : 0;
+    uint32_t c[FLY], b[FLY];
+    bool there[FLY];
+#pragma unroll
+    for (int u = 0; u < FLY; ++u) {
+        const int64_t at = at0 + t0 + KV_GROUPS * u;
+        there[u] = at >= 0 && at < kv_stride;
+        const size_t row = head * kv_stride + (there[u] ? at : 0);
+        c[u] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(codes + row * Q4_ROW) + l16);
+        b[u] = scale[row * Q4_BLOCKS + l16 / 4];
     }
-    kv_store8<DT>(reinterpret_cast<char*>(X) + (head * T + t) * RA_D * (DT == RA_BF16 ? 2 : 4), l16, v);
+#pragma unroll
+    for (int u = 0; u < FLY; ++u) {
+        const int64_t t = t0 + KV_GROUPS * u;
+        if (t >= T) continue;
+        float v[8];
+        q4_values(there[u] ? c[u] : 0u, q4_unit(there[u] ? b[u] : 127u), v);
+        kv_store8<DT>(reinterpret_cast<char*>(X) + (head * T + t) * RA_D * (DT == RA_BF16 ? 2 : 4), l16, v);
+    }
 }
 
-static ra_status rows_grid(int n_seq, int n_kv, int64_t T, dim3* grid) {
-    const int64_t heads = (int64_t)n_seq * n_kv, blocks = (T + KV_GROUPS - 1) / KV_GROUPS;
+// what both launch: rows per group of lanes, and the grid
+static ra_status rows_grid(int n_seq, int n_kv, int64_t T, bool* four, dim3* grid) {
+    const int64_t heads = (int64_t)n_seq * n_kv;
+    *four = heads * T >= 1 << 16;
+    const int64_t rows = KV_GROUPS * (*four ? 4 : 1), blocks = (T + rows - 1) / rows;
     if (heads > 65535) RA_FAIL(RA_EUNSUP, "more than 65535 (sequence, KV head) pairs");
     if (blocks > (1 << 24) - 1) RA_FAIL(RA_EUNSUP, "T too large");
     *grid = dim3((unsigned)blocks, (unsigned)heads);
     return RA_OK;
 }
+#define KV_ROWS_GO(KERNEL, ...)                                                                                          \
+    do {                                                                                                                 \
+        if (dt == RA_BF16) {                                                                                             \
+            if (four) hipLaunchKernelGGL((KERNEL<RA_BF16, 4>), grid, dim3(KV_THREADS), 0, st, __VA_ARGS__);              \
+            else hipLaunchKernelGGL((KERNEL<RA_BF16, 1>), grid, dim3(KV_THREADS), 0, st, __VA_ARGS__);                   \
+        } else {                                                                                                         \
+            if (four) hipLaunchKernelGGL((KERNEL<RA_F32, 4>), grid, dim3(KV_THREADS), 0, st, __VA_ARGS__);               \
+            else hipLaunchKernelGGL((KERNEL<RA_F32, 1>), grid, dim3(KV_THREADS), 0, st, __VA_ARGS__);                    \
+        }                                                                                                                \
+    } while (0)
 
 ra_status ra_launch_quantize_kv4(const void* X, ra_dtype dt, int n_seq, int n_kv, int64_t T, const int32_t* first,
                                  const int32_t* n_new, int64_t kv_stride, hipStream_t st, uint8_t* codes, uint8_t* scale) {
     dim3 grid;
-    const ra_status rc = rows_grid(n_seq, n_kv, T, &grid);
+    bool four;
+    const ra_status rc = rows_grid(n_seq, n_kv, T, &four, &grid);
     if (rc != RA_OK) return rc;
-    if (dt == RA_BF16)
-        hipLaunchKernelGGL(quantize_kv4_kernel<RA_BF16>, grid, dim3(KV_THREADS), 0, st, X, n_kv, T, first, n_new, kv_stride, codes, scale);
-    else
-        hipLaunchKernelGGL(quantize_kv4_kernel<RA_F32>, grid, dim3(KV_THREADS), 0, st, X, n_kv, T, first, n_new, kv_stride, codes, scale);
+    KV_ROWS_GO(quantize_kv4_kernel, X, n_kv, T, first, n_new, kv_stride, codes, scale);
     RA_HIP(hipGetLastError());
     return RA_OK;
 }
@@ -194,12 +306,10 @@ ra_status ra_launch_quantize_kv4(const void* X, ra_dtype dt, int n_seq, int n_kv
 ra_status ra_launch_dequantize_kv4(const uint8_t* codes, const uint8_t* scale, ra_dtype dt, int n_seq, int n_kv, int64_t T,
                                    const int32_t* first, int64_t kv_stride, hipStream_t st, void* X) {
     dim3 grid;
-    const ra_status rc = rows_grid(n_seq, n_kv, T, &grid);
+    bool four;
+    const ra_status rc = rows_grid(n_seq, n_kv, T, &four, &grid);
     if (rc != RA_OK) return rc;
-    if (dt == RA_BF16)
-        hipLaunchKernelGGL(dequantize_kv4_kernel<RA_BF16>, grid, dim3(KV_THREADS), 0, st, codes, scale, n_kv, T, first, kv_stride, X);
-    else
-        hipLaunchKernelGGL(dequantize_kv4_kernel<RA_F32>, grid, dim3(KV_THREADS), 0, st, codes, scale, n_kv, T, first, kv_stride, X);
+    KV_ROWS_GO(dequantize_kv4_kernel, codes, scale, n_kv, T, first, kv_stride, X);
     RA_HIP(hipGetLastError());
     return RA_OK;
 }
