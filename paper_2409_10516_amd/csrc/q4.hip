@@ -22,38 +22,38 @@
 //   sums    O[dimension][column] += V^T P. The lane's weights of the two halves are 8 consecutive slots of the contraction, so
 //           they go in as they come out; V^T wants for them, per dimension, the same 8 rows. Lane (kg, r) reads codes 8 r .. 8 r + 7 of
 //           these rows, four bytes each (16 lanes read a row): instruction m takes the m-th of each, dimension 8 r + m.
-// Codes become bfloat16 exactly. The columns are terms of weights: a bfloat16 weight has 8 bits, so column c holds term c / H of head
-// c % H, the first as rounded, the next what the rounding left; 2 terms of 8 heads (bfloat16), 3 of 4 (float32, whose queries are
-// three bfloat16 terms too, in three instructions). The terms of a head are added at the end. The sum of the weights is that of the
-// terms (an instruction with a row of ones), so that what their rounding does to a weight that has nearly everything cancels.
+// Codes become bfloat16 exactly. A float32 weight goes in as terms of bfloat16, the first as rounded, the next what the rounding left, an
+// instruction for each: 2 (16 bits) for bfloat16, 3 (24 bits) for float32, whose queries are three terms too. The sum of the
+// weights is that of the terms (an instruction with a row of ones), so that what their rounding does to a weight that has nearly
+// everything cancels.
+// Columns are heads, HEADS of them; where that is 8 or 4, two or four groups of columns have the same heads, and a lane makes the weights of
+// half or a quarter of its rows only (the others are zero): exponentials and splits are what vector instructions are short of,
+// not matrix instructions. Every column has a maximum and sums of its own; they are put together at the end.
 // The running maximum of a column moves only when a logit exceeds it by more than 8 (in powers of two), which keeps the
 // lanes' exchange and the scaling of sums out of nearly every chunk.
 typedef __bf16 q4_bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 q4_bf16x8 __attribute__((ext_vector_type(8)));
 typedef float q4_f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t q4_u32x4 __attribute__((ext_vector_type(4), aligned(4)));
 #define Q4_CHUNK 32
 #define Q4_LOWEST (-1.7e38f)        // below every logit: a maximum that nothing has moved yet
-
-template <int DT> struct Q4Form;
-template <> struct Q4Form<RA_BF16> { enum { HEADS = 8, TERMS = 2, Q = 1 }; };
-template <> struct Q4Form<RA_F32> { enum { HEADS = 4, TERMS = 3, Q = 3 }; };
 
 struct Q4Chunk {
     uint4 k[2];
     uint32_t ks[2], v[8], vs[8];
 };
 
-template <int DT>
+template <int DT, int HEADS>
 struct Q4Wave {
-    typedef Q4Form<DT> F;
-    q4_bf16x8 q[F::Q][4];
-    q4_f32x4 acc[8], sum;      // weighted sums, and the sum of the weights as they went in, the same in all rows
+    static constexpr int TERMS = DT == RA_BF16 ? 2 : 3, QTERMS = DT == RA_BF16 ? 1 : 3;
+    static constexpr int SHARES = 16 / HEADS, MINE = 8 / SHARES;        // groups of columns; rows of a lane's 8 that are its own
+    q4_bf16x8 q[QTERMS][4];
+    q4_f32x4 acc[8], sum;       // weighted sums, and the sum of the weights as they went in, the same in all rows
     float m;
+    uint32_t turn;              // by how much a word of four scale bytes turns for the lane's to lie at the exponent
 
     // queries of heads 0 .. n - 1 of a tile, 128 values each; columns past them are zero
     __device__ __forceinline__ void start(const void* q0, int n, int lane) {
-        const int kg = lane >> 4, h = (lane & 15) % F::HEADS;
+        const int kg = lane >> 4, h = (lane & 15) % HEADS;
         const bool have = h < n;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -64,9 +64,10 @@ struct Q4Wave {
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    float x = have ? reinterpret_cast<const float*>(q0)[at + e] : 0.f;
+                    float x = reinterpret_cast<const float*>(q0)[at + e];
+                    x = have ? x : 0.f;
 #pragma unroll
-                    for (int t = 0; t < F::Q; ++t) {
+                    for (int t = 0; t < QTERMS; ++t) {
                         q[t][i][e] = (__bf16)x;
                         x -= (float)q[t][i][e];
                     }
@@ -77,6 +78,7 @@ struct Q4Wave {
         for (int d = 0; d < 8; ++d) acc[d] = q4_f32x4{0.f, 0.f, 0.f, 0.f};
         sum = q4_f32x4{0.f, 0.f, 0.f, 0.f};
         m = Q4_LOWEST;
+        turn = (8 * ((lane & 15) / 4) + 9) & 31;
     }
 
     // `there`: bit j says whether the lane's row j is one (rows 4 kg + j of the first half, j < 4, then of the second); ALL: all are
@@ -95,15 +97,23 @@ struct Q4Wave {
                 b.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], unit, 2));
                 b.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], unit, 3));
 #pragma unroll
-                for (int x = F::Q - 1; x >= 0; --x)         // (the smallest term first)
+                for (int x = QTERMS - 1; x >= 0; --x)       // (the smallest term first)
                     S[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(q4_bf16x8, b), q[x][i], S[t], 0, 0, 0);
             }
         }
-        float z[8], top = Q4_LOWEST;
+        // the lane's own rows: MINE from g MINE on
+        const int g = (lane & 15) / HEADS;
+        float z[MINE], top = Q4_LOWEST;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < MINE; ++j) {
             z[j] = S[j / 4][j & 3];
-            if (!ALL) z[j] = (there >> j) & 1u ? z[j] : -INFINITY;
+            if (SHARES == 2) z[j] = g ? S[1][j & 3] : z[j];
+            if (SHARES == 4) {
+                z[j] = g & 1 ? S[0][2 + (j & 1)] : z[j];
+                const float far = g & 1 ? S[1][2 + (j & 1)] : S[1][j & 1];
+                z[j] = g & 2 ? far : z[j];
+            }
+            if (!ALL) z[j] = (there >> (g * MINE + j)) & 1u ? z[j] : -INFINITY;
             top = fmaxf(top, z[j]);
         }
         if (__builtin_amdgcn_ballot_w64(top * Q4_C > m + 8.f) != 0ull) {
@@ -115,71 +125,115 @@ struct Q4Wave {
 #pragma unroll
             for (int d = 0; d < 8; ++d) acc[d] *= corr;
         }
-        // weights, and this column's term of them
-        const int term = (lane & 15) / F::HEADS;
-        q4_bf16x8 P;
+        q4_bf16x8 P[TERMS];
+        {
+            float x[MINE];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            float x = __builtin_amdgcn_exp2f(fmaf(z[j], Q4_C, -m));
+            for (int j = 0; j < MINE; ++j) x[j] = __builtin_amdgcn_exp2f(fmaf(z[j], Q4_C, -m));
 #pragma unroll
-            for (int t = 1; t < F::TERMS; ++t) x = fmaf(term >= t ? -1.f : 0.f, (float)(__bf16)x, x);
-            P[j] = (__bf16)x;
+            for (int t = 0; t < TERMS; ++t) {
+                uint32_t pair[MINE / 2], w[4];
+#pragma unroll
+                for (int j = 0; j < MINE / 2; ++j) {
+                    const q4_bf16x2 b = {(__bf16)x[2 * j], (__bf16)x[2 * j + 1]};
+                    pair[j] = __builtin_bit_cast(uint32_t, b);
+                    if (t + 1 < TERMS) { x[2 * j] -= bf16_lo(pair[j]); x[2 * j + 1] -= bf16_hi(pair[j]); }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = SHARES == 1 || g == i / (MINE / 2) ? pair[i % (MINE / 2)] : 0u;
+                P[t] = __builtin_bit_cast(q4_bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+            }
         }
-        sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(q4_bf16x8, make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u)),
-                                                      P, sum, 0, 0, 0);
-        uint32_t pair[4][8];                                 // [dimensions 2 y, 2 y + 1][row]
+        const q4_bf16x8 ones = __builtin_bit_cast(q4_bf16x8, make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u));
+#pragma unroll
+        for (int t = TERMS - 1; t >= 0; --t) sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, P[t], sum, 0, 0, 0);
+        float unit[8];                                       // the scale byte of the lane's block, where its exponent goes
+        uint32_t w[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            float unit = q4_unit((c.vs[j] >> (8 * ((lane & 15) / 4))) & 255u);
-            uint32_t w = c.v[j];
+            unit[j] = __uint_as_float(__builtin_amdgcn_alignbit(c.vs[j], c.vs[j], turn));
+            w[j] = c.v[j];
             if (!ALL) {                                      // (0 * NaN is not 0)
                 const bool have = (there >> j) & 1u;
-                unit = have ? unit : 1.f;
-                w = have ? w : 0u;
+                unit[j] = have ? unit[j] : 1.f;
+                w[j] = have ? w[j] : 0u;
             }
-            pair[0][j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 0));
-            pair[1][j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 1));
-            pair[2][j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 2));
-            pair[3][j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 3));
         }
+        sums<0>(w, unit, P);
+        sums<1>(w, unit, P);
+        sums<2>(w, unit, P);
+        sums<3>(w, unit, P);
+    }
+    // dimensions 2 Y and 2 Y + 1 of the lane's 8, which share a byte of every row's codes
+    template <int Y>
+    __device__ __forceinline__ void sums(const uint32_t (&w)[8], const float (&unit)[8], const q4_bf16x8 (&P)[TERMS]) {
+        uint32_t p[8];
 #pragma unroll
-        for (int d = 0; d < 8; ++d) {
-            const uint32_t half = d & 1 ? 0x07060302u : 0x05040100u;
-            const uint32_t(&p)[8] = pair[d / 2];
+        for (int j = 0; j < 8; ++j) p[j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[j], unit[j], Y));
+#pragma unroll
+        for (int o = 0; o < 2; ++o) {
+            const uint32_t half = o ? 0x07060302u : 0x05040100u;
             uint4 a;
             a.x = __builtin_amdgcn_perm(p[1], p[0], half);
             a.y = __builtin_amdgcn_perm(p[3], p[2], half);
             a.z = __builtin_amdgcn_perm(p[5], p[4], half);
             a.w = __builtin_amdgcn_perm(p[7], p[6], half);
-            acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(q4_bf16x8, a), P, acc[d], 0, 0, 0);
+#pragma unroll
+            for (int t = TERMS - 1; t >= 0; --t)
+                acc[2 * Y + o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(q4_bf16x8, a), P[t], acc[2 * Y + o], 0, 0, 0);
         }
     }
 };
 
-// rows [from, from + 32) of a head (`from` the same in all lanes); past the last row, n - 1, that one
-template <bool ALL>
-__device__ __forceinline__ void q4_fetch(Q4Chunk& c, const Q4Cache& h, int64_t from, int64_t n, int lane) {
-    const int kg = lane >> 4, r = lane & 15;
+// Rows of one head from `first` on, read through buffer descriptors: a lane's places in a chunk never change, and what moves
+// from chunk to chunk is one scalar, so that no vector instruction is spent on addresses.
+#define Q4_RSRC 0x00020000          // raw buffer, no format
+struct Q4Stream {
+    __amdgpu_buffer_rsrc_t k, ks, v, vs;
+    int at_k, at_ks, at_v, at_vs;
+
+    __device__ __forceinline__ void start(const Q4Cache& h, int64_t first, int64_t rows, int lane) {
+        const int kg = lane >> 4, r = lane & 15;
+        auto rsrc = [&](const uint8_t* p, int row) {
+            return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p) + first * row, 0, (int)(rows * row), Q4_RSRC);
+        };
+        k = rsrc(h.k, Q4_ROW); ks = rsrc(h.ks, Q4_BLOCKS); v = rsrc(h.v, Q4_ROW); vs = rsrc(h.vs, Q4_BLOCKS);
+        at_k = r * Q4_ROW + 16 * kg; at_ks = r * Q4_BLOCKS + kg; at_v = 4 * kg * Q4_ROW + 4 * r; at_vs = 4 * kg * Q4_BLOCKS;
+    }
+    // rows [row, row + 32), all of which there are; `row` is the same in all lanes
+    __device__ __forceinline__ void fetch(Q4Chunk& c, int row) const {
+        const int by = row * Q4_ROW, bys = row * Q4_BLOCKS;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            c.k[t] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(k, at_k, by + 16 * t * Q4_ROW, 0));
+            c.ks[t] = __builtin_amdgcn_raw_buffer_load_b8(ks, at_ks, bys + 16 * t * Q4_BLOCKS, 0);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            c.v[j] = __builtin_amdgcn_raw_buffer_load_b32(v, at_v, by + ((j & 4) * 4 + (j & 3)) * Q4_ROW, 0);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const uint4 w = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(vs, at_vs, bys + 16 * t * Q4_BLOCKS, 0));
+            c.vs[4 * t] = w.x; c.vs[4 * t + 1] = w.y; c.vs[4 * t + 2] = w.z; c.vs[4 * t + 3] = w.w;
+        }
+    }
+};
+// rows [from, from + 32) of a head; past the last row, n - 1, that one
+__device__ __forceinline__ void q4_fetch_last(Q4Chunk& c, const Q4Cache& h, int64_t from, int64_t n, int lane) {
+    const int kg = lane >> 4, r = lane & 15, last = (int)(n - 1 - from);
     const uint8_t *k = h.k + from * Q4_ROW, *ks = h.ks + from * Q4_BLOCKS, *v = h.v + from * Q4_ROW, *vs = h.vs + from * Q4_BLOCKS;
-    const int last = ALL ? 31 : (int)(n - 1 - from);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        const int row = ALL ? 16 * t + r : min(16 * t + r, last);
+        const int row = min(16 * t + r, last);
         c.k[t] = *reinterpret_cast<const uint4*>(k + row * Q4_ROW + 16 * kg);
         c.ks[t] = ks[row * Q4_BLOCKS + kg];
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const int row = (j & 4) * 4 + 4 * kg + (j & 3);
-        c.v[j] = *reinterpret_cast<const uint32_t*>(v + (ALL ? row : min(row, last)) * Q4_ROW + 4 * r);
-        if (!ALL) c.vs[j] = *reinterpret_cast<const uint32_t*>(vs + min(row, last) * Q4_BLOCKS);
+        const int row = min((j & 4) * 4 + 4 * kg + (j & 3), last);
+        c.v[j] = *reinterpret_cast<const uint32_t*>(v + row * Q4_ROW + 4 * r);
+        c.vs[j] = *reinterpret_cast<const uint32_t*>(vs + row * Q4_BLOCKS);
     }
-    if (ALL)
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const q4_u32x4 w = *reinterpret_cast<const q4_u32x4*>(vs + (16 * t + 4 * kg) * Q4_BLOCKS);
-            c.vs[4 * t] = w.x; c.vs[4 * t + 1] = w.y; c.vs[4 * t + 2] = w.z; c.vs[4 * t + 3] = w.w;
-        }
 }
 // which of the lane's rows of [from, from + 32) are below n
 __device__ __forceinline__ uint32_t q4_there(int64_t from, int64_t n, int lane) {
@@ -193,12 +247,12 @@ __device__ __forceinline__ uint32_t q4_there(int64_t from, int64_t n, int lane) 
 #define Q4_PAD (RA_D + 4)
 struct Q4Lds { float a[Q4_WAVES][16][Q4_PAD], m[Q4_WAVES][16], l[Q4_WAVES][16]; };
 
-// The wavefronts' states -> one per head: f(head of the tile, dimension, sum, maximum, sum of weights), called by one thread
-// for each; a head without rows has the maximum -infinity.
-template <int DT, class Fn>
-__device__ __forceinline__ void q4_close(Q4Wave<DT>& s, Q4Lds& lds, int n, Fn f) {
-    typedef Q4Form<DT> F;
-    const int tid = threadIdx.x, wv = tid / RA_WAVE, lane = tid & 63, kg = lane >> 4, col = lane & 15;
+// The states of the wavefronts' columns -> one per head: f(head of the tile, dimension, sum, maximum, sum of weights), called by
+// one thread for each; a head without rows has the maximum -infinity.
+template <int DT, int HEADS, class Fn>
+__device__ __forceinline__ void q4_close(Q4Wave<DT, HEADS>& s, Q4Lds& lds, int n, int tid, Fn f) {
+    constexpr int SHARES = 16 / HEADS;
+    const int wv = tid / RA_WAVE, lane = tid & 63, kg = lane >> 4, col = lane & 15;
     const float l = s.sum[0];
     // a sum that is not a number keeps a maximum that is one, or it would count as empty
     if (kg == 0) {
@@ -214,130 +268,294 @@ __device__ __forceinline__ void q4_close(Q4Wave<DT>& s, Q4Lds& lds, int n, Fn f)
     __syncthreads();
     for (int x = tid; x < n * RA_D; x += Q4_THREADS) {
         const int h = x / RA_D, d = x % RA_D;
-        float mx = -INFINITY, a = 0.f, ll = 0.f;
+        float m[Q4_WAVES][SHARES], mx = -INFINITY, a = 0.f, ll = 0.f;
 #pragma unroll
-        for (int w = 0; w < Q4_WAVES; ++w) mx = fmaxf(mx, lds.m[w][h]);
-        if (mx > -INFINITY)
+        for (int w = 0; w < Q4_WAVES; ++w)
 #pragma unroll
-            for (int w = 0; w < Q4_WAVES; ++w) {
-                const float wt = __builtin_amdgcn_exp2f(lds.m[w][h] - mx);
-                float sum = lds.a[w][h][d];
+            for (int g = 0; g < SHARES; ++g) mx = fmaxf(mx, m[w][g] = lds.m[w][g * HEADS + h]);
+        const float base = mx > -INFINITY ? mx : 0.f;
 #pragma unroll
-                for (int t = 1; t < F::TERMS; ++t) sum += lds.a[w][h + t * F::HEADS][d];
-                float l = lds.l[w][h];
+        for (int w = 0; w < Q4_WAVES; ++w)
 #pragma unroll
-                for (int t = 1; t < F::TERMS; ++t) l += lds.l[w][h + t * F::HEADS];
-                if (lds.m[w][h] > -INFINITY) {
-                    a = fmaf(sum, wt, a);
-                    ll = fmaf(l, wt, ll);
-                }
+            for (int g = 0; g < SHARES; ++g) {              // (a column without rows has sums of zero)
+                const float wt = __builtin_amdgcn_exp2f(m[w][g] - base);
+                a = fmaf(lds.a[w][g * HEADS + h][d], wt, a);
+                ll = fmaf(lds.l[w][g * HEADS + h], wt, ll);
             }
         f(h, d, a, mx, ll);
     }
 }
 
-// Attention over all tokens. A workgroup takes `span` rows of a KV head for a tile of its query heads, its wavefronts
-// chunks in turn, the next one's loads before the present one's work. grid: per (KV head, tile of heads, part), eight parts side by side,
-// then the next tile of the same ones, which then find their rows in the L2 of their XCD. A launch of one part per head writes
-// the results; otherwise parts with rows leave records.
-template <int DT>
-__global__ __launch_bounds__(Q4_THREADS) void q4_full_kernel(const void* __restrict__ q, Q4Cache c, int n_q, int n_kv, int64_t N,
-                                                             const int32_t* __restrict__ n_tokens, int span, int parts, int tiles,
-                                                             float* __restrict__ partials, float* __restrict__ out,
-                                                             float* __restrict__ lse) {
-    typedef Q4Form<DT> F;
-    __shared__ Q4Lds lds;
-    const int rows8 = (parts + 7) / 8, lane = threadIdx.x & 63, wv = threadIdx.x / RA_WAVE;
-    const int part = (blockIdx.x / (8 * tiles)) % rows8 * 8 + blockIdx.x % 8, tile = blockIdx.x / 8 % tiles;
-    const size_t kv_head = blockIdx.x / (8u * tiles * rows8);
-    const int seq = (int)(kv_head / n_kv), group = n_q / n_kv;
-    int64_t n = n_tokens ? n_tokens[seq] : N;
-    n = n < 0 ? 0 : n < N ? n : N;
-    if (part >= parts || (parts > 1 && (int64_t)part * span >= n)) return;
-    const int64_t from = (int64_t)part * span, to = from + span < n ? from + span : n;
-    const size_t head0 = (size_t)seq * n_q + (kv_head % n_kv) * group + tile * F::HEADS;
-    const int heads = group - tile * F::HEADS < F::HEADS ? group - tile * F::HEADS : F::HEADS;
-    const Q4Cache h{c.k + kv_head * c.kv_stride * Q4_ROW, c.ks + kv_head * c.kv_stride * Q4_BLOCKS, c.v + kv_head * c.kv_stride * Q4_ROW,
-                    c.vs + kv_head * c.kv_stride * Q4_BLOCKS, c.kv_stride};
-    Q4Wave<DT> s;
-    s.start(reinterpret_cast<const char*>(q) + head0 * RA_D * (DT == RA_BF16 ? 2 : 4), heads, lane);
-    const int wave_first = __builtin_amdgcn_readfirstlane(wv) * Q4_CHUNK;
-    int64_t at = from + wave_first;
-    const int64_t step = Q4_WAVES * Q4_CHUNK;
-    Q4Chunk a, b;
-    if (at + Q4_CHUNK <= to) {
-        q4_fetch<true>(a, h, at, to, lane);
-        while (true) {
-            const bool more = at + step + Q4_CHUNK <= to;
-            if (more) q4_fetch<true>(b, h, at + step, to, lane);
-            s.template add<true>(a, 255u, lane);
-            at += step;
-            if (!more) break;
-            const bool more2 = at + step + Q4_CHUNK <= to;
-            if (more2) q4_fetch<true>(a, h, at + step, to, lane);
-            s.template add<true>(b, 255u, lane);
-            at += step;
-            if (!more2) break;
+// Attention over all tokens. The work is a list: per sequence, KV head and tile of its query heads (a job) the job's rows in units of
+// 128 (a chunk for each wavefront of a workgroup) or, for lists that would be too long for 32 bits, a power of two of these. Workgroups
+// take equal stretches of that list, whatever the lengths of the sequences are, and leave a record per job they touched, at place
+// (workgroup + job): going along the list, one or the other grows by one at a time.
+// A launch of as many workgroups as jobs (`whole`) gives each its job, and the workgroup writes the result.
+#define Q4_UNIT (Q4_WAVES * Q4_CHUNK)
+#define Q4_MOST_UNITS (1u << 21)    // times the workgroups, below 2^32
+#define Q4_LEAST_UNITS 2u           // units that are worth a workgroup
+struct Q4List {
+    uint32_t units, first;          // of the whole list; before a sequence's jobs
+    int n;                          // rows of the sequence
+    uint32_t workgroups;            // that have a stretch
+
+    __device__ __forceinline__ uint32_t from(uint32_t wg) const { return units * wg / workgroups; }
+    __device__ __forceinline__ uint32_t owner(uint32_t unit) const { return ((unit + 1) * workgroups - 1) / units; }
+};
+__device__ __forceinline__ int q4_rows_of(const int32_t* n_tokens, int seq, int N) {
+    const int n = n_tokens ? n_tokens[seq] : N;
+    return n < 0 ? 0 : n < N ? n : N;
+}
+__device__ __forceinline__ uint32_t q4_units(int rows, int unit_log2) { return ((uint32_t)rows + (1u << unit_log2) - 1u) >> unit_log2; }
+// the list, and where sequence `seq`'s part of it begins; called by whole wavefronts, the same in all lanes
+__device__ __forceinline__ Q4List q4_list(const int32_t* n_tokens, int n_seq, int seq, int N, int unit_log2, uint32_t jobs, uint32_t grid) {
+    Q4List x;
+    if (!n_tokens) {
+        x.units = q4_units(N, unit_log2) * n_seq * jobs;
+        x.first = q4_units(N, unit_log2) * seq * jobs;
+        x.n = N;
+    } else {
+        uint32_t all = 0, before = 0;
+        int mine = 0;
+        for (int s0 = 0; s0 < n_seq; s0 += RA_WAVE) {
+            const int s = s0 + (threadIdx.x & 63), rows = s < n_seq ? q4_rows_of(n_tokens, s, N) : 0;
+            const uint32_t u = q4_units(rows, unit_log2);
+            all += u;
+            before += s < seq ? u : 0u;
+            mine += s == seq ? rows : 0;
         }
+#pragma unroll
+        for (int d = 1; d < RA_WAVE; d <<= 1) { all += __shfl_xor(all, d); before += __shfl_xor(before, d); mine += __shfl_xor(mine, d); }
+        x.units = __builtin_amdgcn_readfirstlane(all) * jobs;
+        x.first = __builtin_amdgcn_readfirstlane(before) * jobs;
+        x.n = __builtin_amdgcn_readfirstlane(mine);
     }
-    if (at < to) {
-        q4_fetch<false>(a, h, at, to, lane);
-        s.template add<false>(a, q4_there(at, to, lane), lane);
+    const uint32_t most = (x.units + Q4_LEAST_UNITS - 1u) / Q4_LEAST_UNITS;
+    x.workgroups = most < grid ? most : grid;
+    return x;
+}
+// the sequence that has unit `unit` (one of the list's), and where its part begins
+__device__ __forceinline__ int q4_seq_of(const int32_t* n_tokens, int n_seq, int N, int unit_log2, uint32_t jobs, uint32_t unit,
+                                         uint32_t* first) {
+    if (!n_tokens) {
+        const uint32_t per = q4_units(N, unit_log2) * jobs, seq = unit / per;
+        *first = seq * per;
+        return (int)seq;
     }
-    q4_close<DT>(s, lds, heads, [&](int hd, int d, float sum, float mx, float l) {
-        if (parts > 1) {
-            float* rec = partials + ((head0 + hd) * parts + part) * Q4_REC;
-            rec[d] = sum;
-            if (d == 0) { rec[RA_D] = mx; rec[RA_D + 1] = l; }
-        } else {
-            out[(head0 + hd) * RA_D + d] = mx > -INFINITY ? sum / l : 0.f;
-            if (d == 0) lse[head0 + hd] = mx > -INFINITY ? mx * Q4_LN2 + logf(l) : -INFINITY;
+    const int lane = threadIdx.x & 63;
+    uint32_t at = 0;
+    for (int s0 = 0;; s0 += RA_WAVE) {
+        const int s = s0 + lane;
+        const uint32_t u = s < n_seq ? q4_units(q4_rows_of(n_tokens, s, N), unit_log2) : 0u;
+        uint32_t upto = u;
+#pragma unroll
+        for (int d = 1; d < RA_WAVE; d <<= 1) {
+            const uint32_t below = __shfl_up(upto, d);
+            upto += lane >= d ? below : 0u;
         }
-    });
+        const unsigned long long past = __ballot(at + upto * jobs > unit);
+        if (past != 0ull || s0 + RA_WAVE >= n_seq) {
+            const int l = past != 0ull ? __ffsll(past) - 1 : 63;
+            *first = at + (uint32_t)__builtin_amdgcn_readlane((int)(upto - u), l) * jobs;
+            return s0 + l;
+        }
+        at += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63) * jobs;
+    }
 }
 
-// The records of a head of all tokens. grid: x = head (with its sequence)
-#define Q4_MAX_PARTS 512
-#define Q4_MERGE_THREADS 512
-__global__ __launch_bounds__(Q4_MERGE_THREADS) void q4_full_merge_kernel(const float* __restrict__ partials, int n_q, int64_t N,
-                                                                         const int32_t* __restrict__ n_tokens, int span, int parts,
-                                                                         float* __restrict__ out, float* __restrict__ lse) {
-    __shared__ float s_w[Q4_MAX_PARTS], s_x[Q4_MERGE_THREADS / RA_WAVE], s_a[Q4_MERGE_THREADS / RA_D][RA_D];
-    const int tid = threadIdx.x, t = tid % RA_D, slice = tid / RA_D, lane = tid & 63;
+template <int DT, int HEADS>
+__global__ __launch_bounds__(Q4_THREADS, 3) void q4_full_kernel(const void* __restrict__ q, Q4Cache c, int n_seq, int n_q,
+                                                                                  int n_kv, int N, const int32_t* __restrict__ n_tokens,
+                                                                                  int tiles, int unit_log2, int whole, float* __restrict__ partials,
+                                                                                  float* __restrict__ out, float* __restrict__ lse) {
+    __shared__ Q4Lds lds;
+    const int jobs = n_kv * tiles, group = n_q / n_kv, wg = blockIdx.x;
+    uint32_t at = 0, end = 1, first = 0;
+    int seq = wg / jobs;
+    if (!whole) {
+        const Q4List x = q4_list(n_tokens, n_seq, 0, N, unit_log2, jobs, gridDim.x);
+        if ((uint32_t)wg >= x.workgroups) return;
+        at = x.from(wg);
+        end = x.from(wg + 1);
+        seq = q4_seq_of(n_tokens, n_seq, N, unit_log2, jobs, at, &first);
+    }
+    while (at < end) {
+        // (what depends on the thread alone is worked out anew for each job: kept over the loop it takes 80 registers)
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));
+        const int lane = tid & 63, wv = tid / RA_WAVE;
+        const int n = q4_rows_of(n_tokens, seq, N);
+        const uint32_t units = q4_units(n, unit_log2);
+        int job = wg % jobs;
+        uint32_t unit0 = 0, unit1 = units;
+        if (!whole) {
+            if (at >= first + units * jobs) {                // (the stretch goes on in the next sequence that has rows)
+                first += units * jobs;
+                ++seq;
+                continue;
+            }
+            job = (int)((at - first) / units);
+            unit0 = at - first - (uint32_t)job * units;
+            unit1 = unit0 + (end - at) < units ? unit0 + (end - at) : units;
+        }
+        const size_t kv_head = (size_t)seq * n_kv + job / tiles;
+        const int head_in_group = job % tiles * HEADS, heads = group - head_in_group < HEADS ? group - head_in_group : HEADS;
+        const size_t head0 = (size_t)seq * n_q + (size_t)(job / tiles) * group + head_in_group;
+        const int64_t from = (int64_t)unit0 << unit_log2, upto = (int64_t)unit1 << unit_log2, to = upto < n ? upto : n;
+        const Q4Cache h{c.k + kv_head * c.kv_stride * Q4_ROW, c.ks + kv_head * c.kv_stride * Q4_BLOCKS,
+                        c.v + kv_head * c.kv_stride * Q4_ROW, c.vs + kv_head * c.kv_stride * Q4_BLOCKS, c.kv_stride};
+        // whole chunks, then the last, if it is not. Loads are not branched around (the counts of what is on its way would have to
+        // hold for both ways, and every chunk would wait for the next one's loads): past the end it is the last chunk again.
+        const int step = Q4_UNIT, rows = (int)(to - from);
+        int row = __builtin_amdgcn_readfirstlane(wv) * Q4_CHUNK;
+        const int last = row + (rows - Q4_CHUNK - row) / step * step;
+        Q4Wave<DT, HEADS> s;
+        Q4Chunk a, b;
+        s.start(reinterpret_cast<const char*>(q) + head0 * RA_D * (DT == RA_BF16 ? 2 : 4), heads, lane);
+        if (row + Q4_CHUNK <= rows) {
+            Q4Stream x;
+            x.start(h, from, rows, lane);
+            x.fetch(a, row);
+            while (true) {
+                x.fetch(b, row + step < last ? row + step : last);
+                s.template add<true>(a, 255u, lane);
+                row += step;
+                if (row > last) break;
+                x.fetch(a, row + step < last ? row + step : last);
+                s.template add<true>(b, 255u, lane);
+                row += step;
+                if (row > last) break;
+            }
+        }
+        if (row < rows) {
+            q4_fetch_last(a, h, from + row, to, lane);
+            s.template add<false>(a, q4_there(from + row, to, lane), lane);
+        }
+        const size_t slot = ((size_t)wg + (size_t)seq * jobs + job) * HEADS;
+        q4_close<DT, HEADS>(s, lds, heads, tid, [&](int hd, int d, float sum, float mx, float l) {
+            if (!whole) {
+                float* rec = partials + (slot + hd) * Q4_REC;
+                rec[d] = sum;
+                if (d == 0) { rec[RA_D] = mx; rec[RA_D + 1] = l; }
+            } else {
+                out[(head0 + hd) * RA_D + d] = mx > -INFINITY ? sum / l : 0.f;
+                if (d == 0) lse[head0 + hd] = mx > -INFINITY ? mx * Q4_LN2 + logf(l) : -INFINITY;
+            }
+        });
+        if (whole) return;
+        at += unit1 - unit0;
+        if (at < end) __syncthreads();                       // (the next job's sums go through the same LDS)
+    }
+}
+
+// Where a head's records are, those of a row of workgroups: the first one, how many, and from one to the next.
+struct Q4Records { const float* rec; int have; size_t stride; };
+__device__ __forceinline__ Q4Records q4_records(const float* partials, size_t head, int n_seq, int n_q, int n_kv, int N,
+                                                const int32_t* n_tokens, int tiles, int unit_log2, int heads, int grid) {
+    const int seq = (int)(head / n_q), group = n_q / n_kv, h = (int)(head % n_q), jobs = n_kv * tiles;
+    const int job = h / group * tiles + h % group / heads;
+    const Q4List x = q4_list(n_tokens, n_seq, seq, N, unit_log2, jobs, grid);
+    const uint32_t units = q4_units(x.n, unit_log2);
+    int have = 0, wg0 = 0;
+    if (units) {
+        const uint32_t unit0 = x.first + job * units;
+        wg0 = (int)x.owner(unit0);
+        have = (int)x.owner(unit0 + units - 1) - wg0 + 1;
+    }
+    return {partials + (((size_t)wg0 + (size_t)seq * jobs + job) * heads + h % group % heads) * Q4_REC, have, (size_t)heads * Q4_REC};
+}
+
+// The records of a head, few of them. grid: x = head; a thread per dimension, eight records on their way at a time.
+__global__ __launch_bounds__(RA_D) void q4_full_merge_kernel(const float* __restrict__ partials, int n_seq, int n_q, int n_kv, int N,
+                                                             const int32_t* __restrict__ n_tokens, int tiles, int unit_log2, int heads,
+                                                             int grid, float* __restrict__ out, float* __restrict__ lse) {
     const size_t head = blockIdx.x;
-    int64_t n = n_tokens ? n_tokens[head / n_q] : N;
-    n = n < 0 ? 0 : n < N ? n : N;
-    const int have = (int)((n + span - 1) / span);           // parts with rows
-    const float* rec = partials + head * parts * Q4_REC;
-    const float m = tid < have ? rec[(size_t)tid * Q4_REC + RA_D] : -INFINITY, l = tid < have ? rec[(size_t)tid * Q4_REC + RA_D + 1] : 0.f;
+    const int d = threadIdx.x;
+    const Q4Records x = q4_records(partials, head, n_seq, n_q, n_kv, N, n_tokens, tiles, unit_log2, heads, grid);
+    float M = -INFINITY, L = 0.f, A = 0.f;
+    constexpr int FLY = 8;
+    for (int i0 = 0; i0 < x.have; i0 += FLY) {
+        float m[FLY], l[FLY], a[FLY], mx = M;
+#pragma unroll
+        for (int u = 0; u < FLY; ++u) {
+            const float* r = x.rec + (size_t)(i0 + u < x.have ? i0 + u : x.have - 1) * x.stride;
+            m[u] = r[RA_D];
+            l[u] = r[RA_D + 1];
+            a[u] = r[d];
+        }
+#pragma unroll
+        for (int u = 0; u < FLY; ++u) mx = fmaxf(mx, m[u]);
+        if (mx == -INFINITY) continue;
+        const float corr = __builtin_amdgcn_exp2f(M - mx);
+        A *= corr;
+        L *= corr;
+#pragma unroll
+        for (int u = 0; u < FLY; ++u) {
+            const float w = i0 + u < x.have ? __builtin_amdgcn_exp2f(m[u] - mx) : 0.f;
+            A = fmaf(a[u], w, A);
+            L = fmaf(l[u], w, L);
+        }
+        M = mx;
+    }
+    out[head * RA_D + d] = M > -INFINITY ? A / L : 0.f;
+    if (d == 0) lse[head] = M > -INFINITY ? M * Q4_LN2 + logf(L) : -INFINITY;
+}
+
+// The same for many. grid: x = a quarter of the dimensions of a head. 32 groups of threads take records in turn, FLY of each at a
+// time; the first ones are on their way before the weights are known.
+#define Q4_MERGE_THREADS 1024
+#define Q4_MERGE_DIMS 32
+#define Q4_MOST_WORKGROUPS 768      // three per compute unit, and the most records of a head
+__global__ __launch_bounds__(Q4_MERGE_THREADS) void q4_full_merge_many_kernel(const float* __restrict__ partials, int n_seq, int n_q,
+                                                                              int n_kv, int N, const int32_t* __restrict__ n_tokens,
+                                                                              int tiles, int unit_log2, int heads, int grid,
+                                                                              float* __restrict__ out, float* __restrict__ lse) {
+    constexpr int WAVES = Q4_MERGE_THREADS / RA_WAVE, SL = Q4_MERGE_THREADS / Q4_MERGE_DIMS, FLY = 8;
+    static_assert(Q4_MOST_WORKGROUPS <= Q4_MERGE_THREADS, "a thread has the weight of a record");
+    __shared__ float s_w[Q4_MERGE_THREADS], s_m[WAVES], s_l[WAVES], s_a[SL][Q4_MERGE_DIMS];
+    const int tid = threadIdx.x, t = tid % Q4_MERGE_DIMS, slice = tid / Q4_MERGE_DIMS, lane = tid & 63;
+    const size_t head = blockIdx.x / (RA_D / Q4_MERGE_DIMS);
+    const int dim = blockIdx.x % (RA_D / Q4_MERGE_DIMS) * Q4_MERGE_DIMS + t;
+    const Q4Records x = q4_records(partials, head, n_seq, n_q, n_kv, N, n_tokens, tiles, unit_log2, heads, grid);
+    const float* rec = x.rec;
+    const size_t stride = x.stride;
+    const int have = x.have;
+    float r[FLY];
+#pragma unroll
+    for (int u = 0; u < FLY; ++u) r[u] = slice + u * SL < have ? rec[(slice + u * SL) * stride + dim] : 0.f;
+    const float m = tid < have ? rec[tid * stride + RA_D] : -INFINITY, l = tid < have ? rec[tid * stride + RA_D + 1] : 0.f;
     float mx = m;
 #pragma unroll
     for (int d = 1; d < RA_WAVE; d <<= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
-    if (lane == 0) s_x[tid / RA_WAVE] = mx;
+    if (lane == 0) s_m[tid / RA_WAVE] = mx;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < Q4_MERGE_THREADS / RA_WAVE; ++w) mx = fmaxf(mx, s_x[w]);
+    for (int w = 0; w < WAVES; ++w) mx = fmaxf(mx, s_m[w]);
     const float w = mx > -INFINITY ? __builtin_amdgcn_exp2f(m - mx) : 0.f;
     s_w[tid] = w;
     float ll = l * w;
 #pragma unroll
     for (int d = 1; d < RA_WAVE; d <<= 1) ll += __shfl_xor(ll, d);
+    if (lane == 0) s_l[tid / RA_WAVE] = ll;
     __syncthreads();
-    if (lane == 0) s_x[tid / RA_WAVE] = ll;
     float a = 0.f;
-    constexpr int SL = Q4_MERGE_THREADS / RA_D;
-#pragma unroll 8
-    for (int i = slice; i < have; i += SL) a = fmaf(rec[(size_t)i * Q4_REC + t], s_w[i], a);
+    for (int i = slice; i < have; i += SL * FLY) {
+#pragma unroll
+        for (int u = 0; u < FLY; ++u)
+            if (i + u * SL < have) a = fmaf(r[u], s_w[i + u * SL], a);
+#pragma unroll
+        for (int u = 0; u < FLY; ++u) r[u] = i + (u + FLY) * SL < have ? rec[(i + (u + FLY) * SL) * stride + dim] : 0.f;
+    }
     s_a[slice][t] = a;
     __syncthreads();
     if (slice) return;
     ll = 0.f;
 #pragma unroll
-    for (int x = 0; x < Q4_MERGE_THREADS / RA_WAVE; ++x) ll += s_x[x];
+    for (int w = 0; w < WAVES; ++w) ll += s_l[w];
 #pragma unroll
-    for (int x = 1; x < SL; ++x) a += s_a[x][t];
-    out[head * RA_D + t] = mx > -INFINITY ? a / ll : 0.f;
-    if (t == 0) lse[head] = mx > -INFINITY ? mx * Q4_LN2 + logf(ll) : -INFINITY;
+    for (int s = 1; s < SL; ++s) a += s_a[s][t];
+    out[head * RA_D + dim] = mx > -INFINITY ? a / ll : 0.f;
+    if (dim == 0) lse[head] = mx > -INFINITY ? mx * Q4_LN2 + logf(ll) : -INFINITY;
 }
 
 // ---- the retrieved set and the static set -------------------------------------------------------
@@ -450,35 +668,34 @@ __device__ __forceinline__ void q4_finish(const float* rec, int nS, int nG, size
 // grid: per (sequence, KV head) the parts of each of its query heads' Omega (their loads wait for ids, so they start first), then
 // the parts of the static set per tile of heads. `spanS`, `spanG`: rows of a part. TICKETS: the workgroup that stores a head's last
 // record combines them all (ticket.h), which saves a launch.
-template <int DT, bool TICKETS>
+template <int DT, int HEADS, bool TICKETS>
 __global__ __launch_bounds__(Q4_THREADS) void q4_attend_kernel(const void* __restrict__ q, Q4Cache c, int n_q, int n_kv, int64_t N,
                                                                int64_t s, int64_t w, int topk, const int32_t* __restrict__ ids, int nS,
                                                                int nG, int spanS, int spanG, int tiles, float* partials, Q4Out o) {
-    typedef Q4Form<DT> F;
     __shared__ Q4Lds lds;
-    __shared__ uint32_t s_last[F::HEADS];
+    __shared__ uint32_t s_last[HEADS];
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid / RA_WAVE);
     const int group = n_q / n_kv, per = tiles * nS + group * nG, P = nS + nG;
     const size_t kv_head = blockIdx.x / per;
     const int x = blockIdx.x % per;
     const size_t group0 = kv_head / n_kv * n_q + kv_head % n_kv * group;
     const bool om = x < group * nG;
-    const int first = om ? x / nG : (x - group * nG) / nS * F::HEADS;        // of the group's heads
+    const int first = om ? x / nG : (x - group * nG) / nS * HEADS;        // of the group's heads
     const int part = om ? x % nG : (x - group * nG) % nS, slot = om ? nS + part : part;
-    const int heads = om ? 1 : group - first < F::HEADS ? group - first : F::HEADS;
+    const int heads = om ? 1 : group - first < HEADS ? group - first : HEADS;
     const size_t head0 = group0 + first;
     const Q4Cache h{c.k + kv_head * c.kv_stride * Q4_ROW, c.ks + kv_head * c.kv_stride * Q4_BLOCKS, c.v + kv_head * c.kv_stride * Q4_ROW,
                     c.vs + kv_head * c.kv_stride * Q4_BLOCKS, c.kv_stride};
     const Q4Rows src = om ? Q4Rows{ids + head0 * topk, N, 0, 0, topk} : Q4Rows{nullptr, N, s, w, (int)(s + N - w)};
     const int span = om ? spanG : spanS, from = part * span, to = from + span < src.count ? from + span : src.count;
-    Q4Wave<DT> st;
+    Q4Wave<DT, HEADS> st;
     st.start(reinterpret_cast<const char*>(q) + head0 * RA_D * (DT == RA_BF16 ? 2 : 4), heads, lane);
     for (int at = from + wv * Q4_CHUNK; at < to; at += Q4_WAVES * Q4_CHUNK) {
         Q4Chunk ch;
         const uint32_t there = q4_gather(ch, h, src, at, lane);
         st.template add<false>(ch, there, lane);
     }
-    q4_close<DT>(st, lds, heads, [&](int hd, int d, float sum, float mx, float l) {
+    q4_close<DT, HEADS>(st, lds, heads, tid, [&](int hd, int d, float sum, float mx, float l) {
         float* rec = partials + ((head0 + hd) * P + slot) * Q4_REC;
         q4_store<TICKETS>(rec + d, sum);
         if (d == 0) { q4_store<TICKETS>(rec + RA_D, mx); q4_store<TICKETS>(rec + RA_D + 1, l); }
@@ -502,43 +719,57 @@ __global__ __launch_bounds__(RA_D) void q4_merge_kernel(const float* __restrict_
     q4_finish<false>(partials + head * (nS + nG) * Q4_REC, nS, nG, head, threadIdx.x, o);
 }
 
-// Rows of a part of all tokens, a multiple of what a workgroup's wavefronts take at once: parts for about four workgroups
-// per compute unit, at least 256 rows each.
-static int full_span(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N, int* parts, int* tiles) {
-    const int heads = dt == RA_BF16 ? Q4Form<RA_BF16>::HEADS : Q4Form<RA_F32>::HEADS;
-    *tiles = (n_q / n_kv + heads - 1) / heads;
-    const int64_t jobs = (int64_t)n_seq * n_kv * *tiles, unit = Q4_WAVES * Q4_CHUNK;
-    int64_t want = (1024 + jobs - 1) / jobs;
-    if (want > N / 256) want = N / 256;
-    if (want > Q4_MAX_PARTS) want = Q4_MAX_PARTS;
-    if (want < 1) want = 1;
-    const int64_t span = ((N + want - 1) / want + unit - 1) / unit * unit;
-    *parts = (int)((N + span - 1) / span);
-    return (int)span;
+// query heads of a tile (columns of the matrix instructions)
+static int q4_heads(int group) { return group <= 4 ? 4 : group <= 8 ? 8 : 16; }
+#define Q4_HEADS_GO(GO, DTV)                            \
+    do {                                                \
+        const int hv_ = q4_heads(n_q / n_kv);           \
+        if (hv_ == 4) GO(DTV, 4);                       \
+        else if (hv_ == 8) GO(DTV, 8);                  \
+        else GO(DTV, 16);                               \
+    } while (0)
+
+// How a call is cut: tiles of query heads per KV head, workgroups, and whether each has a job of its own. That is so where the jobs are
+// many, or all of a head's rows are few units.
+struct Q4Cut { int tiles, workgroups, unit_log2; bool whole; };
+static Q4Cut q4_cut(int n_seq, int n_q, int n_kv, int64_t N) {
+    Q4Cut x;
+    const int heads = q4_heads(n_q / n_kv);
+    x.tiles = (n_q / n_kv + heads - 1) / heads;
+    const int64_t jobs = (int64_t)n_seq * n_kv * x.tiles;
+    x.whole = jobs >= 2048 || N <= Q4_LEAST_UNITS * Q4_UNIT;
+    x.unit_log2 = 7;
+    static_assert(Q4_UNIT == 1 << 7, "rows of a unit");
+    auto units = [&] { return jobs * ((N + ((int64_t)1 << x.unit_log2) - 1) >> x.unit_log2); };
+    while (!x.whole && units() > Q4_MOST_UNITS) ++x.unit_log2;
+    x.workgroups = (int)(x.whole ? (jobs < (1 << 24) ? jobs : 1 << 24) : units() < Q4_MOST_WORKGROUPS ? units() : Q4_MOST_WORKGROUPS);
+    return x;
 }
 
-size_t ra_full_q4_partial_floats(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N) {
-    int parts, tiles;
-    full_span(dt, n_seq, n_q, n_kv, N, &parts, &tiles);
-    return parts > 1 ? (size_t)n_seq * n_q * parts * Q4_REC : 0;
+size_t ra_full_q4_partial_floats(ra_dtype, int n_seq, int n_q, int n_kv, int64_t N) {
+    const Q4Cut x = q4_cut(n_seq, n_q, n_kv, N);
+    return x.whole ? 0 : ((size_t)x.workgroups + (size_t)n_seq * n_kv * x.tiles) * q4_heads(n_q / n_kv) * Q4_REC;
 }
 
+#define Q4_FEW_RECORDS 32
 ra_status ra_launch_full_q4(const void* q, ra_dtype dt, const Q4Cache& c, int n_seq, int n_q, int n_kv, int64_t N,
                             const int32_t* n_tokens, float* partials, hipStream_t st, float* out, float* lse) {
-    int parts, tiles;
-    const int span = full_span(dt, n_seq, n_q, n_kv, N, &parts, &tiles);
-    const int64_t blocks = (int64_t)n_seq * n_kv * tiles * ((parts + 7) / 8 * 8);
-    if (blocks > (1 << 24) - 1) RA_FAIL(RA_EUNSUP, "too many (sequence, KV head) pairs for one launch");
-    if (dt == RA_BF16)
-        hipLaunchKernelGGL(q4_full_kernel<RA_BF16>, dim3((unsigned)blocks), dim3(Q4_THREADS), 0, st, q, c, n_q, n_kv, N, n_tokens, span,
-                           parts, tiles, partials, out, lse);
-    else
-        hipLaunchKernelGGL(q4_full_kernel<RA_F32>, dim3((unsigned)blocks), dim3(Q4_THREADS), 0, st, q, c, n_q, n_kv, N, n_tokens, span,
-                           parts, tiles, partials, out, lse);
+    const Q4Cut x = q4_cut(n_seq, n_q, n_kv, N);
+    if (x.workgroups >= 1 << 24) RA_FAIL(RA_EUNSUP, "too many (sequence, KV head) pairs for one launch");
+#define Q4_GO(DTV, HV)                                                                                                         \
+    hipLaunchKernelGGL((q4_full_kernel<DTV, HV>), dim3(x.workgroups), dim3(Q4_THREADS), 0, st, q, c, n_seq, n_q, n_kv, (int)N, n_tokens, \
+                       x.tiles, x.unit_log2, (int)x.whole, partials, out, lse)
+    if (dt == RA_BF16) Q4_HEADS_GO(Q4_GO, RA_BF16); else Q4_HEADS_GO(Q4_GO, RA_F32);
+#undef Q4_GO
     RA_HIP(hipGetLastError());
-    if (parts == 1) return RA_OK;
-    hipLaunchKernelGGL(q4_full_merge_kernel, dim3(n_seq * n_q), dim3(Q4_MERGE_THREADS), 0, st, partials, n_q, N, n_tokens, span, parts, out,
-                       lse);
+    if (x.whole) return RA_OK;
+#define Q4_MERGE(KERNEL, GRID, THREADS)                                                                                                 \
+    hipLaunchKernelGGL(KERNEL, dim3(GRID), dim3(THREADS), 0, st, partials, n_seq, n_q, n_kv, (int)N, n_tokens, x.tiles, x.unit_log2,  \
+                       q4_heads(n_q / n_kv), x.workgroups, out, lse)
+    // records per head, were all sequences as long as the longest
+    if (x.workgroups / (n_seq * n_kv * x.tiles) <= Q4_FEW_RECORDS) Q4_MERGE(q4_full_merge_kernel, n_seq * n_q, RA_D);
+    else Q4_MERGE(q4_full_merge_many_kernel, n_seq * n_q * (RA_D / Q4_MERGE_DIMS), Q4_MERGE_THREADS);
+#undef Q4_MERGE
     RA_HIP(hipGetLastError());
     return RA_OK;
 }
@@ -550,10 +781,13 @@ static void q4_static(int64_t N, int64_t Ng, int sink, int window, int64_t* s, i
     if (*w <= *s) { *s = N; *w = N; }
 }
 
+// Columns of the sparse set's tiles: a wavefront has a chunk or two, and what counts is the way to its end, which is longer the more
+// columns a head has.
+#define Q4_ATTEND_HEADS 16
 // parts of the two sets: 128 rows each, a chunk for each wavefront of a workgroup; longer ones where they would be very many
 struct Q4Parts { int nS, nG, spanS, spanG, tiles; };
-static Q4Parts q4_parts(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t n_static, int topk) {
-    const int heads = dt == RA_BF16 ? Q4Form<RA_BF16>::HEADS : Q4Form<RA_F32>::HEADS;
+static Q4Parts q4_parts(int n_seq, int n_q, int n_kv, int64_t n_static, int topk) {
+    const int heads = Q4_ATTEND_HEADS;
     Q4Parts p;
     p.tiles = (n_q / n_kv + heads - 1) / heads;
     p.spanG = Q4_PART;
@@ -568,10 +802,10 @@ static Q4Parts q4_parts(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t n_sta
     return p;
 }
 
-size_t ra_attend_q4_partial_floats(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N, int64_t Ng, int sink, int window, int topk) {
+size_t ra_attend_q4_partial_floats(ra_dtype, int n_seq, int n_q, int n_kv, int64_t N, int64_t Ng, int sink, int window, int topk) {
     int64_t s, w;
     q4_static(N, Ng, sink, window, &s, &w);
-    const Q4Parts p = q4_parts(dt, n_seq, n_q, n_kv, s + N - w, topk);
+    const Q4Parts p = q4_parts(n_seq, n_q, n_kv, s + N - w, topk);
     return (size_t)n_seq * n_q * (p.nS + p.nG) * Q4_REC;
 }
 
@@ -582,14 +816,14 @@ ra_status ra_launch_attend_q4(const void* q, ra_dtype dt, const Q4Cache& c, int 
                               hipStream_t st, float* out, float* lse, float* o_omega, float* lse_omega, float* o_w, float* lse_w) {
     int64_t s, w;
     q4_static(N, Ng, sink, window, &s, &w);
-    const Q4Parts p = q4_parts(dt, n_seq, n_q, n_kv, s + N - w, topk);
+    const Q4Parts p = q4_parts(n_seq, n_q, n_kv, s + N - w, topk);
     const int64_t blocks = (int64_t)n_seq * n_kv * (p.tiles * p.nS + n_q / n_kv * p.nG);
     if (blocks > (1 << 24) - 1) RA_FAIL(RA_EUNSUP, "too many heads for one launch");
     if ((int64_t)n_seq * n_q * (p.nS + p.nG) > Q4_TICKET_RECORDS) tickets = nullptr;
     const Q4Out o{tickets, out, lse, o_omega, lse_omega, o_w, lse_w};
-#define Q4_GO(DTV, TK)                                                                                                       \
-    hipLaunchKernelGGL((q4_attend_kernel<DTV, TK>), dim3((unsigned)blocks), dim3(Q4_THREADS), 0, st, q, c, n_q, n_kv, N, s, w, topk, ids, \
-                       p.nS, p.nG, p.spanS, p.spanG, p.tiles, partials, o)
+#define Q4_GO(DTV, TK)                                                                                                          \
+    hipLaunchKernelGGL((q4_attend_kernel<DTV, Q4_ATTEND_HEADS, TK>), dim3((unsigned)blocks), dim3(Q4_THREADS), 0, st, q, c, n_q, n_kv, N, s, w, \
+                       topk, ids, p.nS, p.nG, p.spanS, p.spanG, p.tiles, partials, o)
     if (dt == RA_BF16) { if (tickets) Q4_GO(RA_BF16, true); else Q4_GO(RA_BF16, false); }
     else { if (tickets) Q4_GO(RA_F32, true); else Q4_GO(RA_F32, false); }
 #undef Q4_GO

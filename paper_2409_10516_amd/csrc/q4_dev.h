@@ -3,7 +3,7 @@
 //
 // The part converts codes by itself: v_cvt_scalef32_pk_{f32,bf16}_fp4 turn the two codes of a byte into values
 // times a scale, of which only the exponent field counts, so a scale byte b goes in as b << 23 (255, in which form it is
-// an infinity, makes NaN; 0 makes 2^-127). v_cvt_scalef32_pk_fp4_f32 is the way back: values over scale, nearest, ties to even.
+// an infinity, makes NaN; 0 makes 2^-127), whatever else the word holds. v_cvt_scalef32_pk_fp4_f32 is the way back: values over scale, nearest, ties to even.
 #pragma once
 #include "common.h"
 
