@@ -51,21 +51,18 @@ struct Q4Wave {
     float m;
     uint32_t turn;              // by how much a word of four scale bytes turns for the lane's to lie at the exponent
 
-    // queries of heads 0 .. n - 1 of a tile, 128 values each; columns past them are zero
+    // queries of heads 0 .. n - 1 of a tile, 128 values each; columns past them are the first one's, and nobody asks for them
     __device__ __forceinline__ void start(const void* q0, int n, int lane) {
         const int kg = lane >> 4, h = (lane & 15) % HEADS;
-        const bool have = h < n;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const size_t at = (size_t)(have ? h : 0) * RA_D + 32 * kg + 8 * i;
+            const size_t at = (size_t)(h < n ? h : 0) * RA_D + 32 * kg + 8 * i;
             if constexpr (DT == RA_BF16) {
-                const uint4 u = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(q0) + at);
-                q[0][i] = __builtin_bit_cast(q4_bf16x8, have ? u : make_uint4(0u, 0u, 0u, 0u));
+                q[0][i] = __builtin_bit_cast(q4_bf16x8, *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(q0) + at));
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     float x = reinterpret_cast<const float*>(q0)[at + e];
-                    x = have ? x : 0.f;
 #pragma unroll
                     for (int t = 0; t < QTERMS; ++t) {
                         q[t][i][e] = (__bf16)x;
@@ -290,10 +287,25 @@ __device__ __forceinline__ void q4_close(Q4Wave<DT, HEADS>& s, Q4Lds& lds, int n
 // 128 (a chunk for each wavefront of a workgroup) or, for lists that would be too long for 32 bits, a power of two of these. Workgroups
 // take equal stretches of that list, whatever the lengths of the sequences are, and leave a record per job they touched, at place
 // (workgroup + job): going along the list, one or the other grows by one at a time.
+// Records lie per head of a tile, then place: sums [HEADS][places][128], then maxima and sums of weights [HEADS][places][2], so that
+// what is combined lies in a row.
 // A launch of as many workgroups as jobs (`whole`) gives each its job, and the workgroup writes the result.
 #define Q4_UNIT (Q4_WAVES * Q4_CHUNK)
 #define Q4_MOST_UNITS (1u << 21)    // times the workgroups, below 2^32
 #define Q4_LEAST_UNITS 2u           // units that are worth a workgroup
+// over the 64 lanes: the sum, in all of them, and the sums up to each
+__device__ __forceinline__ uint32_t q4_sum64(uint32_t x, int lane) {
+    x += lane_xor32<1>(x, lane); x += lane_xor32<2>(x, lane); x += lane_xor32<4>(x, lane);
+    x += lane_xor32<8>(x, lane); x += lane_xor32<16>(x, lane); x += lane_xor32<32>(x, lane);
+    return (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
+}
+__device__ __forceinline__ uint32_t q4_scan64(uint32_t x) {
+#define Q4_STEP(CTRL, ROWS) x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xF, ROWS == 0xF)
+    Q4_STEP(0x111, 0xF); Q4_STEP(0x112, 0xF); Q4_STEP(0x114, 0xF); Q4_STEP(0x118, 0xF);     // within rows of 16
+    Q4_STEP(0x142, 0xA); Q4_STEP(0x143, 0xC);           // the row before's last to every second row, then the half before's
+#undef Q4_STEP
+    return x;
+}
 struct Q4List {
     uint32_t units, first;          // of the whole list; before a sequence's jobs
     int n;                          // rows of the sequence
@@ -315,20 +327,18 @@ __device__ __forceinline__ Q4List q4_list(const int32_t* n_tokens, int n_seq, in
         x.first = q4_units(N, unit_log2) * seq * jobs;
         x.n = N;
     } else {
-        uint32_t all = 0, before = 0;
-        int mine = 0;
+        uint32_t all = 0, before = 0, mine = 0;
+        const int lane = threadIdx.x & 63;
         for (int s0 = 0; s0 < n_seq; s0 += RA_WAVE) {
-            const int s = s0 + (threadIdx.x & 63), rows = s < n_seq ? q4_rows_of(n_tokens, s, N) : 0;
+            const int s = s0 + lane, rows = s < n_seq ? q4_rows_of(n_tokens, s, N) : 0;
             const uint32_t u = q4_units(rows, unit_log2);
             all += u;
             before += s < seq ? u : 0u;
-            mine += s == seq ? rows : 0;
+            mine += s == seq ? (uint32_t)rows : 0u;
         }
-#pragma unroll
-        for (int d = 1; d < RA_WAVE; d <<= 1) { all += __shfl_xor(all, d); before += __shfl_xor(before, d); mine += __shfl_xor(mine, d); }
-        x.units = __builtin_amdgcn_readfirstlane(all) * jobs;
-        x.first = __builtin_amdgcn_readfirstlane(before) * jobs;
-        x.n = __builtin_amdgcn_readfirstlane(mine);
+        x.units = q4_sum64(all, lane) * jobs;
+        x.first = q4_sum64(before, lane) * jobs;
+        x.n = (int)q4_sum64(mine, lane);
     }
     const uint32_t most = (x.units + Q4_LEAST_UNITS - 1u) / Q4_LEAST_UNITS;
     x.workgroups = most < grid ? most : grid;
@@ -347,12 +357,7 @@ __device__ __forceinline__ int q4_seq_of(const int32_t* n_tokens, int n_seq, int
     for (int s0 = 0;; s0 += RA_WAVE) {
         const int s = s0 + lane;
         const uint32_t u = s < n_seq ? q4_units(q4_rows_of(n_tokens, s, N), unit_log2) : 0u;
-        uint32_t upto = u;
-#pragma unroll
-        for (int d = 1; d < RA_WAVE; d <<= 1) {
-            const uint32_t below = __shfl_up(upto, d);
-            upto += lane >= d ? below : 0u;
-        }
+        const uint32_t upto = q4_scan64(u);
         const unsigned long long past = __ballot(at + upto * jobs > unit);
         if (past != 0ull || s0 + RA_WAVE >= n_seq) {
             const int l = past != 0ull ? __ffsll(past) - 1 : 63;
@@ -431,12 +436,11 @@ __global__ __launch_bounds__(Q4_THREADS, 3) void q4_full_kernel(const void* __re
             q4_fetch_last(a, h, from + row, to, lane);
             s.template add<false>(a, q4_there(from + row, to, lane), lane);
         }
-        const size_t slot = ((size_t)wg + (size_t)seq * jobs + job) * HEADS;
+        const size_t places = (size_t)gridDim.x + (size_t)n_seq * jobs, place = (size_t)wg + (size_t)seq * jobs + job;
         q4_close<DT, HEADS>(s, lds, heads, tid, [&](int hd, int d, float sum, float mx, float l) {
             if (!whole) {
-                float* rec = partials + (slot + hd) * Q4_REC;
-                rec[d] = sum;
-                if (d == 0) { rec[RA_D] = mx; rec[RA_D + 1] = l; }
+                partials[(hd * places + place) * RA_D + d] = sum;
+                if (d == 0) reinterpret_cast<float2*>(partials + HEADS * places * RA_D)[hd * places + place] = make_float2(mx, l);
             } else {
                 out[(head0 + hd) * RA_D + d] = mx > -INFINITY ? sum / l : 0.f;
                 if (d == 0) lse[head0 + hd] = mx > -INFINITY ? mx * Q4_LN2 + logf(l) : -INFINITY;
@@ -448,8 +452,8 @@ __global__ __launch_bounds__(Q4_THREADS, 3) void q4_full_kernel(const void* __re
     }
 }
 
-// Where a head's records are, those of a row of workgroups: the first one, how many, and from one to the next.
-struct Q4Records { const float* rec; int have; size_t stride; };
+// A head's records, those of a row of workgroups: their sums, their maxima and sums of weights, and how many.
+struct Q4Records { const float* sums; const float2* ml; int have; };
 __device__ __forceinline__ Q4Records q4_records(const float* partials, size_t head, int n_seq, int n_q, int n_kv, int N,
                                                 const int32_t* n_tokens, int tiles, int unit_log2, int heads, int grid) {
     const int seq = (int)(head / n_q), group = n_q / n_kv, h = (int)(head % n_q), jobs = n_kv * tiles;
@@ -462,7 +466,8 @@ __device__ __forceinline__ Q4Records q4_records(const float* partials, size_t he
         wg0 = (int)x.owner(unit0);
         have = (int)x.owner(unit0 + units - 1) - wg0 + 1;
     }
-    return {partials + (((size_t)wg0 + (size_t)seq * jobs + job) * heads + h % group % heads) * Q4_REC, have, (size_t)heads * Q4_REC};
+    const size_t places = (size_t)grid + (size_t)n_seq * jobs, at = h % group % heads * places + (size_t)wg0 + (size_t)seq * jobs + job;
+    return {partials + at * RA_D, reinterpret_cast<const float2*>(partials + heads * places * RA_D) + at, have};
 }
 
 // The records of a head, few of them. grid: x = head; a thread per dimension, eight records on their way at a time.
@@ -478,10 +483,11 @@ __global__ __launch_bounds__(RA_D) void q4_full_merge_kernel(const float* __rest
         float m[FLY], l[FLY], a[FLY], mx = M;
 #pragma unroll
         for (int u = 0; u < FLY; ++u) {
-            const float* r = x.rec + (size_t)(i0 + u < x.have ? i0 + u : x.have - 1) * x.stride;
-            m[u] = r[RA_D];
-            l[u] = r[RA_D + 1];
-            a[u] = r[d];
+            const int i = i0 + u < x.have ? i0 + u : x.have - 1;
+            const float2 ml = x.ml[i];
+            m[u] = ml.x;
+            l[u] = ml.y;
+            a[u] = x.sums[(size_t)i * RA_D + d];
         }
 #pragma unroll
         for (int u = 0; u < FLY; ++u) mx = fmaxf(mx, m[u]);
@@ -501,8 +507,8 @@ __global__ __launch_bounds__(RA_D) void q4_full_merge_kernel(const float* __rest
     if (d == 0) lse[head] = M > -INFINITY ? M * Q4_LN2 + logf(L) : -INFINITY;
 }
 
-// The same for many. grid: x = a quarter of the dimensions of a head. 32 groups of threads take records in turn, FLY of each at a
-// time; the first ones are on their way before the weights are known.
+// The same for many. grid: x = a quarter of the dimensions of a head. 32 groups of threads take records in turn, all of which are
+// on their way before the weights are known.
 #define Q4_MERGE_THREADS 1024
 #define Q4_MERGE_DIMS 32
 #define Q4_MOST_WORKGROUPS 768      // three per compute unit, and the most records of a head
@@ -510,20 +516,19 @@ __global__ __launch_bounds__(Q4_MERGE_THREADS) void q4_full_merge_many_kernel(co
                                                                               int n_kv, int N, const int32_t* __restrict__ n_tokens,
                                                                               int tiles, int unit_log2, int heads, int grid,
                                                                               float* __restrict__ out, float* __restrict__ lse) {
-    constexpr int WAVES = Q4_MERGE_THREADS / RA_WAVE, SL = Q4_MERGE_THREADS / Q4_MERGE_DIMS, FLY = 8;
+    constexpr int WAVES = Q4_MERGE_THREADS / RA_WAVE, SL = Q4_MERGE_THREADS / Q4_MERGE_DIMS, FLY = Q4_MOST_WORKGROUPS / SL;
     static_assert(Q4_MOST_WORKGROUPS <= Q4_MERGE_THREADS, "a thread has the weight of a record");
     __shared__ float s_w[Q4_MERGE_THREADS], s_m[WAVES], s_l[WAVES], s_a[SL][Q4_MERGE_DIMS];
     const int tid = threadIdx.x, t = tid % Q4_MERGE_DIMS, slice = tid / Q4_MERGE_DIMS, lane = tid & 63;
     const size_t head = blockIdx.x / (RA_D / Q4_MERGE_DIMS);
     const int dim = blockIdx.x % (RA_D / Q4_MERGE_DIMS) * Q4_MERGE_DIMS + t;
     const Q4Records x = q4_records(partials, head, n_seq, n_q, n_kv, N, n_tokens, tiles, unit_log2, heads, grid);
-    const float* rec = x.rec;
-    const size_t stride = x.stride;
     const int have = x.have;
     float r[FLY];
 #pragma unroll
-    for (int u = 0; u < FLY; ++u) r[u] = slice + u * SL < have ? rec[(slice + u * SL) * stride + dim] : 0.f;
-    const float m = tid < have ? rec[tid * stride + RA_D] : -INFINITY, l = tid < have ? rec[tid * stride + RA_D + 1] : 0.f;
+    for (int u = 0; u < FLY; ++u) r[u] = slice + u * SL < have ? x.sums[(size_t)(slice + u * SL) * RA_D + dim] : 0.f;
+    const float2 ml = tid < have ? x.ml[tid] : make_float2(-INFINITY, 0.f);
+    const float m = ml.x, l = ml.y;
     float mx = m;
 #pragma unroll
     for (int d = 1; d < RA_WAVE; d <<= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
@@ -539,13 +544,9 @@ __global__ __launch_bounds__(Q4_MERGE_THREADS) void q4_full_merge_many_kernel(co
     if (lane == 0) s_l[tid / RA_WAVE] = ll;
     __syncthreads();
     float a = 0.f;
-    for (int i = slice; i < have; i += SL * FLY) {
 #pragma unroll
-        for (int u = 0; u < FLY; ++u)
-            if (i + u * SL < have) a = fmaf(r[u], s_w[i + u * SL], a);
-#pragma unroll
-        for (int u = 0; u < FLY; ++u) r[u] = i + (u + FLY) * SL < have ? rec[(i + (u + FLY) * SL) * stride + dim] : 0.f;
-    }
+    for (int u = 0; u < FLY; ++u)
+        if (slice + u * SL < have) a = fmaf(r[u], s_w[slice + u * SL], a);
     s_a[slice][t] = a;
     __syncthreads();
     if (slice) return;
@@ -748,7 +749,7 @@ static Q4Cut q4_cut(int n_seq, int n_q, int n_kv, int64_t N) {
 
 size_t ra_full_q4_partial_floats(ra_dtype, int n_seq, int n_q, int n_kv, int64_t N) {
     const Q4Cut x = q4_cut(n_seq, n_q, n_kv, N);
-    return x.whole ? 0 : ((size_t)x.workgroups + (size_t)n_seq * n_kv * x.tiles) * q4_heads(n_q / n_kv) * Q4_REC;
+    return x.whole ? 0 : ((size_t)x.workgroups + (size_t)n_seq * n_kv * x.tiles) * q4_heads(n_q / n_kv) * (RA_D + 2);
 }
 
 #define Q4_FEW_RECORDS 32
