@@ -192,11 +192,41 @@ def _here(*ts):
     return here
 
 
-def _ints(t: torch.Tensor, n_seq: int, name: str) -> int:
-    """The address of a vector of n_seq 32-bit integers."""
-    if t.dtype is not torch.int32 or t.shape != (n_seq,) or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 tensor [n_seq]")
+def _vector(t: torch.Tensor, n: int, dtype, here: int, name: str) -> int:
+    """The address of a vector of n elements."""
+    if t.dtype is not dtype or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor [{n}]")
+    if t.get_device() != here:
+        raise ValueError(f"{name} must live on the current GPU ({here}), not on {t.device}")
     return t.data_ptr()
+
+
+def _token_rows(t: torch.Tensor, n_seq: int, T: int, dtype, here: int):
+    """Heads of tokens [n_seq][T][heads][128] -> (address, heads, elements from token to token)."""
+    shape = t.shape
+    if len(shape) != 4 or shape[0] != n_seq or shape[1] != T or shape[3] != 128:
+        raise ValueError("q, k and v must be [n_seq][T][heads][128]")
+    if t.dtype is not dtype:
+        raise TypeError("q, k and v must share a dtype")
+    if t.get_device() != here:
+        raise ValueError(f"tensors must live on the current GPU ({here}), not on {t.device}")
+    seq, token, head, one = t.stride()
+    heads = shape[2]
+    # (the stride of a dimension of one element says nothing)
+    row = token if T > 1 else seq if n_seq > 1 else heads * 128
+    if one != 1 or (heads > 1 and head != 128) or (n_seq > 1 and seq != T * row):
+        raise ValueError("the heads of a token must lie side by side, and all tokens equally far apart")
+    return t.data_ptr(), heads, row
+
+
+def _cache_rows(t: torch.Tensor, n_seq: int, n_kv: int, dtype, here: int, room: int):
+    """A cache [n_seq][n_kv][capacity][128] -> (address, capacity); room: the capacity it must have, 0 for any."""
+    shape = t.shape
+    if t.dtype is not dtype:
+        raise TypeError("caches and inputs must share a dtype")
+    if len(shape) != 4 or shape != (n_seq, n_kv, room or shape[2], 128) or not t.is_contiguous() or t.get_device() != here:
+        raise ValueError("K and V must be contiguous [n_seq][n_kv][capacity][128], of one capacity and where the inputs are")
+    return t.data_ptr(), shape[2]
 
 
 def _kv4(x4, n_seq: int, n_kv: int, name: str, here: int, kv_stride: Optional[int] = None):
@@ -526,69 +556,48 @@ def ra_append_tokens(q, k, v, first, *, n_new=None, q_weight=None, k_weight=None
     some = q if q is not None else k if k is not None else v
     if some is None:
         raise ValueError("at least one of q, k and v is needed")
-    here = _here(q, k, v, first, n_new, q_weight, k_weight, inv_freq, q_out, K, V)
-    dtype = some.dtype
-    if some.dim() != 4:
+    here = torch.cuda.current_device()
+    dtype, shape = some.dtype, some.shape
+    if len(shape) != 4:
         raise ValueError("q, k and v must be [n_seq][T][heads][128]")
-    n_seq, T = some.shape[:2]
-
-    def rows(t):
-        """-> (address, heads, elements from token to token)"""
-        if t is None:
-            return None, 0, 0
-        shape = t.shape
-        if len(shape) != 4 or shape[0] != n_seq or shape[1] != T or shape[3] != 128:
-            raise ValueError("q, k and v must be [n_seq][T][heads][128]")
-        if t.dtype is not dtype:
-            raise TypeError("q, k and v must share a dtype")
-        seq, token, head, one = t.stride()
-        heads = shape[2]
-        # (the stride of a dimension of one element says nothing)
-        row = token if T > 1 else seq if n_seq > 1 else heads * 128
-        if one != 1 or (heads > 1 and head != 128) or (n_seq > 1 and seq != T * row):
-            raise ValueError("the heads of a token must lie side by side, and all tokens equally far apart")
-        return t.data_ptr(), heads, row
-
-    q_at, n_q, q_row = rows(q)
-    k_at, n_k, k_row = rows(k)
-    v_at, n_v, v_row = rows(v)
+    n_seq, T = shape[0], shape[1]
+    q_at, n_q, q_row = _token_rows(q, n_seq, T, dtype, here) if q is not None else (None, 0, 0)
+    k_at, n_k, k_row = _token_rows(k, n_seq, T, dtype, here) if k is not None else (None, 0, 0)
+    v_at, n_v, v_row = _token_rows(v, n_seq, T, dtype, here) if v is not None else (None, 0, 0)
     if n_k and n_v and n_k != n_v:
         raise ValueError("k and v must have the same number of heads")
     n_kv = n_k or n_v or 1
-    for w in (q_weight, k_weight):
-        if w is not None and (w.dtype is not dtype or w.shape != (128,) or not w.is_contiguous()):
-            raise ValueError("weights must be contiguous [128], of the dtype of q, k and v")
-    rot = 0
+    qw_at = _vector(q_weight, 128, dtype, here, "q_weight") if q_weight is not None else None
+    kw_at = _vector(k_weight, 128, dtype, here, "k_weight") if k_weight is not None else None
+    f_at, rot = None, 0
     if inv_freq is not None:
-        if inv_freq.dtype is not torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
-            raise ValueError("inv_freq must be a contiguous float32 tensor [rot_dim / 2]")
-        rot = 2 * inv_freq.shape[0]
+        rot = 2 * inv_freq.numel()
+        f_at = _vector(inv_freq, rot // 2, torch.float32, here, "inv_freq")
+    first_at = _vector(first, n_seq, torch.int32, here, "first") if first is not None else None
+    new_at = _vector(n_new, n_seq, torch.int32, here, "n_new") if n_new is not None else None
+    K_at = V_at = k4_at = k4s_at = v4_at = v4s_at = None
     room = room4 = 0
-    for t in (K, V):
-        if t is not None:
-            if t.dtype is not dtype:
-                raise TypeError("caches and inputs must share a dtype")
-            shape = t.shape
-            if len(shape) != 4 or shape != (n_seq, n_kv, room or shape[2], 128) or not t.is_contiguous():
-                raise ValueError("K and V must be contiguous [n_seq][n_kv][capacity][128], of one capacity")
-            room = shape[2]
-    k4_at = k4s_at = v4_at = v4s_at = None
+    if K is not None:
+        K_at, room = _cache_rows(K, n_seq, n_kv, dtype, here, 0)
+    if V is not None:
+        V_at, room = _cache_rows(V, n_seq, n_kv, dtype, here, room)
     if k4 is not None:
         k4_at, k4s_at, room4 = _kv4(k4, n_seq, n_kv, "k4", here)
     if v4 is not None:
         v4_at, v4s_at, room4 = _kv4(v4, n_seq, n_kv, "v4", here, room4 or None)
+    out_at = None
     if q is None:
         if q_out is not None:
             raise ValueError("q_out goes with q")
-    elif q_out is None:
-        q_out = (torch.empty if n_new is None else torch.zeros)((n_seq, n_q, T, 128), dtype=dtype, device=q.device)
-    elif q_out.dtype is not dtype or q_out.shape != (n_seq, n_q, T, 128) or not q_out.is_contiguous():
-        raise ValueError("q_out must be contiguous [n_seq][n_q][T][128], of the dtype of q")
-    _check(lib().ra_append_tokens(q_at, k_at, v_at, _dt(some), n_seq, n_q or n_kv, n_kv, T, 128, q_row, k_row, v_row, _ptr(q_weight),
-                                  _ptr(k_weight), eps, _ptr(inv_freq), rot, 1 if interleaved else 0,
-                                  None if first is None else _ints(first, n_seq, "first"),
-                                  None if n_new is None else _ints(n_new, n_seq, "n_new"), room, room4, _stream(stream), _ptr(q_out),
-                                  _ptr(K), _ptr(V), k4_at, k4s_at, v4_at, v4s_at))
+    else:
+        if q_out is None:
+            q_out = (torch.empty if n_new is None else torch.zeros)((n_seq, n_q, T, 128), dtype=dtype, device=q.device)
+        elif q_out.dtype is not dtype or q_out.shape != (n_seq, n_q, T, 128) or not q_out.is_contiguous() or q_out.get_device() != here:
+            raise ValueError("q_out must be contiguous [n_seq][n_q][T][128], of the dtype of q and where q is")
+        out_at = q_out.data_ptr()
+    _check(lib().ra_append_tokens(q_at, k_at, v_at, _dt(some), n_seq, n_q or n_kv, n_kv, T, 128, q_row, k_row, v_row, qw_at, kw_at, eps,
+                                  f_at, rot, 1 if interleaved else 0, first_at, new_at, room, room4, _stream(stream), out_at, K_at, V_at,
+                                  k4_at, k4s_at, v4_at, v4s_at))
     return q_out
 
 
@@ -597,7 +606,7 @@ def ra_quantize_kv4(X, first=None, n_new=None, out=None, stream=None):
     [n_seq][n_kv][capacity][4]). With out = (codes, scale) given, row t of sequence s goes to row first[s] + t of these (first: int32
     [n_seq] on the GPU; n_new likewise: only so many rows); without, they are new and hold T rows."""
     _dev(X)
-    here = _here(X, first, n_new)
+    here = _here(X)
     n_seq, n_kv, T, d = X.shape
     if out is None:
         if first is not None or n_new is not None:
@@ -605,15 +614,15 @@ def ra_quantize_kv4(X, first=None, n_new=None, out=None, stream=None):
         out = (torch.empty((n_seq, n_kv, T, 64), dtype=torch.uint8, device=X.device),
                torch.empty((n_seq, n_kv, T, 4), dtype=torch.uint8, device=X.device))
     codes, scale, room = _kv4(out, n_seq, n_kv, "out", here)
-    _check(lib().ra_quantize_kv4(X.data_ptr(), _dt(X), n_seq, n_kv, T, d, None if first is None else _ints(first, n_seq, "first"),
-                                 None if n_new is None else _ints(n_new, n_seq, "n_new"), room, _stream(stream), codes, scale))
+    _check(lib().ra_quantize_kv4(X.data_ptr(), _dt(X), n_seq, n_kv, T, d, None if first is None else _vector(first, n_seq, torch.int32, here, "first"),
+                                 None if n_new is None else _vector(n_new, n_seq, torch.int32, here, "n_new"), room, _stream(stream), codes, scale))
     return out
 
 
 def ra_dequantize_kv4(x4, dtype, first=None, rows: Optional[int] = None, out=None, stream=None):
     """Rows first[s] .. first[s] + rows (None: from 0, all) of a cache in 4 bits -> [n_seq][n_kv][rows][128] of the given dtype, the
     values they stand for."""
-    here = _here(first, out)
+    here = _here(out)
     n_seq, n_kv = x4[0].shape[:2]
     codes, scale, room = _kv4(x4, n_seq, n_kv, "x4", here)
     rows = room if rows is None else rows
@@ -621,22 +630,29 @@ def ra_dequantize_kv4(x4, dtype, first=None, rows: Optional[int] = None, out=Non
         out = torch.empty((n_seq, n_kv, rows, 128), dtype=dtype, device=x4[0].device)
     elif out.dtype is not dtype or out.shape != (n_seq, n_kv, rows, 128) or not out.is_contiguous():
         raise ValueError("out must be contiguous [n_seq][n_kv][rows][128], of the given dtype")
-    _check(lib().ra_dequantize_kv4(codes, scale, _dt(out), n_seq, n_kv, rows, 128, None if first is None else _ints(first, n_seq, "first"),
+    _check(lib().ra_dequantize_kv4(codes, scale, _dt(out), n_seq, n_kv, rows, 128, None if first is None else _vector(first, n_seq, torch.int32, here, "first"),
                                    room, _stream(stream), out.data_ptr()))
     return out
 
 
-def _results(n_seq, n_q, d, device, out, lse):
+def _results(n_seq, n_q, d, here, out, lse):
     """out [n_seq][n_q][d] and lse [n_seq][n_q], the given ones or new ones."""
     if out is None:
-        out = torch.empty((n_seq, n_q, d), dtype=torch.float32, device=device)
-    elif out.dtype is not torch.float32 or out.shape != (n_seq, n_q, d) or not out.is_contiguous():
-        raise ValueError("out must be contiguous float32 [n_seq][n_q][128]")
+        out = torch.empty((n_seq, n_q, d), dtype=torch.float32, device=here)
+    elif out.dtype is not torch.float32 or out.shape != (n_seq, n_q, d) or not out.is_contiguous() or out.get_device() != here:
+        raise ValueError("out must be contiguous float32 [n_seq][n_q][128] on the current GPU")
     if lse is None:
-        lse = torch.empty((n_seq, n_q), dtype=torch.float32, device=device)
-    elif lse.dtype is not torch.float32 or lse.shape != (n_seq, n_q) or not lse.is_contiguous():
-        raise ValueError("lse must be contiguous float32 [n_seq][n_q]")
+        lse = torch.empty((n_seq, n_q), dtype=torch.float32, device=here)
+    elif lse.dtype is not torch.float32 or lse.shape != (n_seq, n_q) or not lse.is_contiguous() or lse.get_device() != here:
+        raise ValueError("lse must be contiguous float32 [n_seq][n_q] on the current GPU")
     return out, lse
+
+
+def _query(q, here: int):
+    """Checks q [n_seq][n_q][d] -> its address and sizes."""
+    if q.dim() != 3 or not q.is_contiguous() or q.get_device() != here:
+        raise ValueError("q must be contiguous [n_seq][n_q][128] on the current GPU")
+    return q.data_ptr(), *q.shape
 
 
 @functools.lru_cache(maxsize=256)
@@ -648,9 +664,8 @@ def _full_q4_room(dt: int, n_seq: int, n_q: int, n_kv: int, N: int) -> int:
 def ra_full_attention_q4(q, k4, v4, n_tokens=None, N: Optional[int] = None, stream=None, workspace=None, out=None, lse=None):
     """Eq. 1 over the first n_tokens[s] rows (int32 [n_seq] on the GPU, at most N; None: N, by default the capacity) of a cache
     in 4 bits -> (out float32 [n_seq][n_q][128], lse float32 [n_seq][n_q])."""
-    _dev(q, workspace)
-    here = _here(q, n_tokens, workspace, out, lse)
-    n_seq, n_q, d = q.shape
+    here = torch.cuda.current_device()
+    q_at, n_seq, n_q, d = _query(q, here)
     n_kv = k4[0].shape[1]
     K4, K4s, room = _kv4(k4, n_seq, n_kv, "k4", here)
     V4, V4s, _ = _kv4(v4, n_seq, n_kv, "v4", here, room)
@@ -658,13 +673,15 @@ def ra_full_attention_q4(q, k4, v4, n_tokens=None, N: Optional[int] = None, stre
     N = room if N is None else N
     if workspace is None:
         have = _full_q4_room(dt, n_seq, n_q, n_kv, N)
-        workspace = torch.empty(have, dtype=torch.uint8, device=q.device)
+        workspace = torch.empty(have, dtype=torch.uint8, device=here)
     else:
+        _dev(workspace)
+        _here(workspace)
         have = workspace.numel() * workspace.element_size()
-    out, lse = _results(n_seq, n_q, d, q.device, out, lse)
-    _check(lib().ra_full_attention_q4(q.data_ptr(), dt, K4, K4s, V4, V4s, n_seq, n_q, n_kv, N, room, d,
-                                      None if n_tokens is None else _ints(n_tokens, n_seq, "n_tokens"), workspace.data_ptr(), have,
-                                      _stream(stream), out.data_ptr(), lse.data_ptr()))
+    out, lse = _results(n_seq, n_q, d, here, out, lse)
+    _check(lib().ra_full_attention_q4(q_at, dt, K4, K4s, V4, V4s, n_seq, n_q, n_kv, N, room, d,
+                                      None if n_tokens is None else _vector(n_tokens, n_seq, torch.int32, here, "n_tokens"),
+                                      workspace.data_ptr(), have, _stream(stream), out.data_ptr(), lse.data_ptr()))
     return out, lse
 
 
@@ -672,23 +689,23 @@ def ra_attend_q4(q, idx: Index, k4, v4, sink: int, window: int, ids: torch.Tenso
                  partials: bool = False, out=None, lse=None):
     """ra_attend over a cache in 4 bits that holds N >= idx.N tokens (by default as many as its capacity); tokens behind the
     index's are static. -> (out, lse) or, with partials=True, (out, lse, o_omega, lse_omega, o_w, lse_w)."""
-    _dev(q, ids)
-    here = _here(q, ids, out, lse)
-    n_seq, n_q, d = q.shape
-    n_kv = k4[0].shape[1]
+    here = torch.cuda.current_device()
+    q_at, n_seq, n_q, d = _query(q, here)
+    n_kv, shape = k4[0].shape[1], ids.shape
     if (n_seq, n_q, n_kv) != idx.heads or d != 128:
         raise ValueError("q must be [n_seq][n_q][128], and its heads and the cache's those of the index")
-    if ids.dtype is not torch.int32 or ids.dim() != 3 or ids.shape[:2] != (n_seq, n_q):
-        raise ValueError("ids must be int32 [n_seq][n_q][topk]")
+    if ids.dtype is not torch.int32 or len(shape) != 3 or shape[0] != n_seq or shape[1] != n_q or not ids.is_contiguous() \
+            or ids.get_device() != here:
+        raise ValueError("ids must be contiguous int32 [n_seq][n_q][topk] on the current GPU")
     K4, K4s, room = _kv4(k4, n_seq, n_kv, "k4", here)
     V4, V4s, _ = _kv4(v4, n_seq, n_kv, "v4", here, room)
-    out, lse = _results(n_seq, n_q, d, q.device, out, lse)
+    out, lse = _results(n_seq, n_q, d, here, out, lse)
     extra = ()
     if partials:
         f = dict(dtype=torch.float32, device=q.device)
         extra = (torch.empty((n_seq, n_q, d), **f), torch.empty((n_seq, n_q), **f),
                  torch.empty((n_seq, n_q, d), **f), torch.empty((n_seq, n_q), **f))
-    _check(_room(lib().ra_attend_q4, q.data_ptr(), idx.handle, _dt(q), K4, K4s, V4, V4s, room if N is None else N, room, sink, window,
-                 ids.shape[-1], ids.data_ptr(), _stream(stream), out.data_ptr(), lse.data_ptr(),
+    _check(_room(lib().ra_attend_q4, q_at, idx.handle, _dt(q), K4, K4s, V4, V4s, room if N is None else N, room, sink, window, shape[2],
+                 ids.data_ptr(), _stream(stream), out.data_ptr(), lse.data_ptr(),
                  *([t.data_ptr() for t in extra] or (None, None, None, None))))
     return (out, lse, *extra) if partials else (out, lse)

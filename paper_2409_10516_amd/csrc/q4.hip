@@ -183,8 +183,11 @@ struct Q4Wave {
 };
 
 // Rows of one head from `first` on, read through buffer descriptors: a lane's places in a chunk never change, and what moves
-// from chunk to chunk is one scalar, so that no vector instruction is spent on addresses.
+// from chunk to chunk is one scalar, so that no vector instruction is spent on addresses. Codes of keys are non-temporal: of a
+// cache that is read again before long, or is larger than what the memory side keeps, the values' half stays (three caches of 131072 rows
+// in turn 37.9 -> 33.1 us a call, of 303 MB 63.2 -> 61.5; both halves 35.5 and 59.6).
 #define Q4_RSRC 0x00020000          // raw buffer, no format
+#define Q4_NT 2                     // non-temporal
 struct Q4Stream {
     __amdgpu_buffer_rsrc_t k, ks, v, vs;
     int at_k, at_ks, at_v, at_vs;
@@ -202,7 +205,7 @@ struct Q4Stream {
         const int by = row * Q4_ROW, bys = row * Q4_BLOCKS;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            c.k[t] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(k, at_k, by + 16 * t * Q4_ROW, 0));
+            c.k[t] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(k, at_k, by + 16 * t * Q4_ROW, Q4_NT));
             c.ks[t] = __builtin_amdgcn_raw_buffer_load_b8(ks, at_ks, bys + 16 * t * Q4_BLOCKS, 0);
         }
 #pragma unroll
@@ -310,6 +313,7 @@ struct Q4List {
     uint32_t units, first;          // of the whole list; before a sequence's jobs
     int n;                          // rows of the sequence
     uint32_t workgroups;            // that have a stretch
+    int rows;                       // rows of sequence `lane`
 
     __device__ __forceinline__ uint32_t from(uint32_t wg) const { return units * wg / workgroups; }
     __device__ __forceinline__ uint32_t owner(uint32_t unit) const { return ((unit + 1) * workgroups - 1) / units; }
@@ -322,6 +326,7 @@ __device__ __forceinline__ uint32_t q4_units(int rows, int unit_log2) { return (
 // the list, and where sequence `seq`'s part of it begins; called by whole wavefronts, the same in all lanes
 __device__ __forceinline__ Q4List q4_list(const int32_t* n_tokens, int n_seq, int seq, int N, int unit_log2, uint32_t jobs, uint32_t grid) {
     Q4List x;
+    x.rows = N;
     if (!n_tokens) {
         x.units = q4_units(N, unit_log2) * n_seq * jobs;
         x.first = q4_units(N, unit_log2) * seq * jobs;
@@ -332,6 +337,7 @@ __device__ __forceinline__ Q4List q4_list(const int32_t* n_tokens, int n_seq, in
         for (int s0 = 0; s0 < n_seq; s0 += RA_WAVE) {
             const int s = s0 + lane, rows = s < n_seq ? q4_rows_of(n_tokens, s, N) : 0;
             const uint32_t u = q4_units(rows, unit_log2);
+            if (s0 == 0) x.rows = rows;
             all += u;
             before += s < seq ? u : 0u;
             mine += s == seq ? (uint32_t)rows : 0u;
@@ -345,8 +351,8 @@ __device__ __forceinline__ Q4List q4_list(const int32_t* n_tokens, int n_seq, in
     return x;
 }
 // the sequence that has unit `unit` (one of the list's), and where its part begins
-__device__ __forceinline__ int q4_seq_of(const int32_t* n_tokens, int n_seq, int N, int unit_log2, uint32_t jobs, uint32_t unit,
-                                         uint32_t* first) {
+__device__ __forceinline__ int q4_seq_of(const Q4List& x, const int32_t* n_tokens, int n_seq, int N, int unit_log2, uint32_t jobs,
+                                         uint32_t unit, uint32_t* first) {
     if (!n_tokens) {
         const uint32_t per = q4_units(N, unit_log2) * jobs, seq = unit / per;
         *first = seq * per;
@@ -356,7 +362,7 @@ __device__ __forceinline__ int q4_seq_of(const int32_t* n_tokens, int n_seq, int
     uint32_t at = 0;
     for (int s0 = 0;; s0 += RA_WAVE) {
         const int s = s0 + lane;
-        const uint32_t u = s < n_seq ? q4_units(q4_rows_of(n_tokens, s, N), unit_log2) : 0u;
+        const uint32_t u = q4_units(s0 == 0 ? x.rows : s < n_seq ? q4_rows_of(n_tokens, s, N) : 0, unit_log2);
         const uint32_t upto = q4_scan64(u);
         const unsigned long long past = __ballot(at + upto * jobs > unit);
         if (past != 0ull || s0 + RA_WAVE >= n_seq) {
@@ -377,19 +383,20 @@ __global__ __launch_bounds__(Q4_THREADS, 3) void q4_full_kernel(const void* __re
     const int jobs = n_kv * tiles, group = n_q / n_kv, wg = blockIdx.x;
     uint32_t at = 0, end = 1, first = 0;
     int seq = wg / jobs;
+    Q4List x;
     if (!whole) {
-        const Q4List x = q4_list(n_tokens, n_seq, 0, N, unit_log2, jobs, gridDim.x);
+        x = q4_list(n_tokens, n_seq, 0, N, unit_log2, jobs, gridDim.x);
         if ((uint32_t)wg >= x.workgroups) return;
         at = x.from(wg);
         end = x.from(wg + 1);
-        seq = q4_seq_of(n_tokens, n_seq, N, unit_log2, jobs, at, &first);
+        seq = q4_seq_of(x, n_tokens, n_seq, N, unit_log2, jobs, at, &first);
     }
     while (at < end) {
         // (what depends on the thread alone is worked out anew for each job: kept over the loop it takes 80 registers)
         int tid = threadIdx.x;
         asm volatile("" : "+v"(tid));
         const int lane = tid & 63, wv = tid / RA_WAVE;
-        const int n = q4_rows_of(n_tokens, seq, N);
+        const int n = whole || seq >= RA_WAVE ? q4_rows_of(n_tokens, seq, N) : __builtin_amdgcn_readlane(x.rows, seq);
         const uint32_t units = q4_units(n, unit_log2);
         int job = wg % jobs;
         uint32_t unit0 = 0, unit1 = units;
@@ -418,15 +425,15 @@ __global__ __launch_bounds__(Q4_THREADS, 3) void q4_full_kernel(const void* __re
         Q4Chunk a, b;
         s.start(reinterpret_cast<const char*>(q) + head0 * RA_D * (DT == RA_BF16 ? 2 : 4), heads, lane);
         if (row + Q4_CHUNK <= rows) {
-            Q4Stream x;
-            x.start(h, from, rows, lane);
-            x.fetch(a, row);
+            Q4Stream rd;
+            rd.start(h, from, rows, lane);
+            rd.fetch(a, row);
             while (true) {
-                x.fetch(b, row + step < last ? row + step : last);
+                rd.fetch(b, row + step < last ? row + step : last);
                 s.template add<true>(a, 255u, lane);
                 row += step;
                 if (row > last) break;
-                x.fetch(a, row + step < last ? row + step : last);
+                rd.fetch(a, row + step < last ? row + step : last);
                 s.template add<true>(b, 255u, lane);
                 row += step;
                 if (row > last) break;
@@ -670,7 +677,7 @@ __device__ __forceinline__ void q4_finish(const float* rec, int nS, int nG, size
 // the parts of the static set per tile of heads. `spanS`, `spanG`: rows of a part. TICKETS: the workgroup that stores a head's last
 // record combines them all (ticket.h), which saves a launch.
 template <int DT, int HEADS, bool TICKETS>
-__global__ __launch_bounds__(Q4_THREADS) void q4_attend_kernel(const void* __restrict__ q, Q4Cache c, int n_q, int n_kv, int64_t N,
+__global__ __launch_bounds__(Q4_THREADS, 3) void q4_attend_kernel(const void* __restrict__ q, Q4Cache c, int n_q, int n_kv, int64_t N,
                                                                int64_t s, int64_t w, int topk, const int32_t* __restrict__ ids, int nS,
                                                                int nG, int spanS, int spanG, int tiles, float* partials, Q4Out o) {
     __shared__ Q4Lds lds;
@@ -693,7 +700,14 @@ __global__ __launch_bounds__(Q4_THREADS) void q4_attend_kernel(const void* __res
     st.start(reinterpret_cast<const char*>(q) + head0 * RA_D * (DT == RA_BF16 ? 2 : 4), heads, lane);
     for (int at = from + wv * Q4_CHUNK; at < to; at += Q4_WAVES * Q4_CHUNK) {
         Q4Chunk ch;
-        const uint32_t there = q4_gather(ch, h, src, at, lane);
+        uint32_t there = 255u;
+        if (!om && at >= s && at + Q4_CHUNK <= to) {         // (rows side by side)
+            Q4Stream rd;
+            rd.start(h, w - s + at, Q4_CHUNK, lane);
+            rd.fetch(ch, 0);
+        } else {
+            there = q4_gather(ch, h, src, at, lane);
+        }
         st.template add<false>(ch, there, lane);
     }
     q4_close<DT, HEADS>(st, lds, heads, tid, [&](int hd, int d, float sum, float mx, float l) {
@@ -731,7 +745,9 @@ static int q4_heads(int group) { return group <= 4 ? 4 : group <= 8 ? 8 : 16; }
     } while (0)
 
 // How a call is cut: tiles of query heads per KV head, workgroups, and whether each has a job of its own. That is so where the jobs are
-// many, or all of a head's rows are few units.
+// many, or all of a head's rows are few units. Otherwise three workgroups fit a compute unit; where few jobs share them, two
+// leave fewer records to combine (us, two and three: 8 jobs of 131072 rows 37.1, 38.0, one of a million 39.4, 40.5, 64 of 20011
+// 33.9, 34.3, 128 of up to 32768 64.2, 62.6).
 struct Q4Cut { int tiles, workgroups, unit_log2; bool whole; };
 static Q4Cut q4_cut(int n_seq, int n_q, int n_kv, int64_t N) {
     Q4Cut x;
@@ -743,7 +759,8 @@ static Q4Cut q4_cut(int n_seq, int n_q, int n_kv, int64_t N) {
     static_assert(Q4_UNIT == 1 << 7, "rows of a unit");
     auto units = [&] { return jobs * ((N + ((int64_t)1 << x.unit_log2) - 1) >> x.unit_log2); };
     while (!x.whole && units() > Q4_MOST_UNITS) ++x.unit_log2;
-    x.workgroups = (int)(x.whole ? (jobs < (1 << 24) ? jobs : 1 << 24) : units() < Q4_MOST_WORKGROUPS ? units() : Q4_MOST_WORKGROUPS);
+    const int most = jobs <= 64 ? Q4_MOST_WORKGROUPS / 3 * 2 : Q4_MOST_WORKGROUPS;
+    x.workgroups = (int)(x.whole ? (jobs < (1 << 24) ? jobs : 1 << 24) : units() < most ? units() : most);
     return x;
 }
 
@@ -792,8 +809,9 @@ static Q4Parts q4_parts(int n_seq, int n_q, int n_kv, int64_t n_static, int topk
     Q4Parts p;
     p.tiles = (n_q / n_kv + heads - 1) / heads;
     p.spanG = Q4_PART;
+    while (p.spanG < topk && (int64_t)n_seq * n_q * ((topk + p.spanG - 1) / p.spanG) > 2048) p.spanG *= 2;
     p.nG = (topk + p.spanG - 1) / p.spanG;
-    int64_t most = 2048 / ((int64_t)n_seq * n_kv * p.tiles);
+    int64_t most = 512 / ((int64_t)n_seq * n_kv * p.tiles);
     if (most < 1) most = 1;
     int64_t nS = (n_static + Q4_PART - 1) / Q4_PART;
     if (nS > most) nS = most;
@@ -810,7 +828,7 @@ size_t ra_attend_q4_partial_floats(ra_dtype, int n_seq, int n_q, int n_kv, int64
     return (size_t)n_seq * n_q * (p.nS + p.nG) * Q4_REC;
 }
 
-#define Q4_TICKET_RECORDS 512
+#define Q4_TICKET_RECORDS 1024
 
 ra_status ra_launch_attend_q4(const void* q, ra_dtype dt, const Q4Cache& c, int n_seq, int n_q, int n_kv, int64_t N, int64_t Ng,
                               int sink, int window, int topk, const int32_t* ids, float* partials, uint32_t* tickets,
