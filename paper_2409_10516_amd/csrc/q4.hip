@@ -42,9 +42,9 @@ struct Q4Chunk {
     uint32_t ks[2], v[8], vs[8];
 };
 
-template <int DT, int HEADS>
+template <int DT, int HEADS, int TERMS>
 struct Q4Wave {
-    static constexpr int TERMS = DT == RA_BF16 ? 2 : 3, QTERMS = DT == RA_BF16 ? 1 : 3;
+    static constexpr int QTERMS = DT == RA_BF16 ? 1 : 3;
     static constexpr int SHARES = 16 / HEADS, MINE = 8 / SHARES;        // groups of columns; rows of a lane's 8 that are its own
     q4_bf16x8 q[QTERMS][4];
     q4_f32x4 acc[8], sum;       // weighted sums, and the sum of the weights as they went in, the same in all rows
@@ -81,7 +81,8 @@ struct Q4Wave {
     // `there`: bit j says whether the lane's row j is one (rows 4 kg + j of the first half, j < 4, then of the second); ALL: all are
     template <bool ALL>
     __device__ __forceinline__ void add(const Q4Chunk& c, uint32_t there, int lane) {
-        q4_f32x4 S[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        // (the lesser terms of a float32 query have a sum of their own, so that the first one's is rounded four times, not twelve)
+        q4_f32x4 S[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}, less[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const float unit = q4_unit(c.ks[t]);
@@ -94,9 +95,11 @@ struct Q4Wave {
                 b.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], unit, 2));
                 b.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], unit, 3));
 #pragma unroll
-                for (int x = QTERMS - 1; x >= 0; --x)       // (the smallest term first)
-                    S[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(q4_bf16x8, b), q[x][i], S[t], 0, 0, 0);
+                for (int x = QTERMS - 1; x >= 1; --x)
+                    less[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(q4_bf16x8, b), q[x][i], less[t], 0, 0, 0);
+                S[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(q4_bf16x8, b), q[0][i], S[t], 0, 0, 0);
             }
+            if (QTERMS > 1) S[t] += less[t];
         }
         // the lane's own rows: MINE from g MINE on
         const int g = (lane & 15) / HEADS;
@@ -249,8 +252,8 @@ struct Q4Lds { float a[Q4_WAVES][16][Q4_PAD], m[Q4_WAVES][16], l[Q4_WAVES][16]; 
 
 // The states of the wavefronts' columns -> one per head: f(head of the tile, dimension, sum, maximum, sum of weights), called by
 // one thread for each; a head without rows has the maximum -infinity.
-template <int DT, int HEADS, class Fn>
-__device__ __forceinline__ void q4_close(Q4Wave<DT, HEADS>& s, Q4Lds& lds, int n, int tid, Fn f) {
+template <int DT, int HEADS, int TERMS, class Fn>
+__device__ __forceinline__ void q4_close(Q4Wave<DT, HEADS, TERMS>& s, Q4Lds& lds, int n, int tid, Fn f) {
     constexpr int SHARES = 16 / HEADS;
     const int wv = tid / RA_WAVE, lane = tid & 63, kg = lane >> 4, col = lane & 15;
     const float l = s.sum[0];
@@ -421,7 +424,7 @@ __global__ __launch_bounds__(Q4_THREADS, 3) void q4_full_kernel(const void* __re
         const int step = Q4_UNIT, rows = (int)(to - from);
         int row = __builtin_amdgcn_readfirstlane(wv) * Q4_CHUNK;
         const int last = row + (rows - Q4_CHUNK - row) / step * step;
-        Q4Wave<DT, HEADS> s;
+        Q4Wave<DT, HEADS, DT == RA_BF16 ? 2 : 3> s;
         Q4Chunk a, b;
         s.start(reinterpret_cast<const char*>(q) + head0 * RA_D * (DT == RA_BF16 ? 2 : 4), heads, lane);
         if (row + Q4_CHUNK <= rows) {
@@ -444,7 +447,7 @@ __global__ __launch_bounds__(Q4_THREADS, 3) void q4_full_kernel(const void* __re
             s.template add<false>(a, q4_there(from + row, to, lane), lane);
         }
         const size_t places = (size_t)gridDim.x + (size_t)n_seq * jobs, place = (size_t)wg + (size_t)seq * jobs + job;
-        q4_close<DT, HEADS>(s, lds, heads, tid, [&](int hd, int d, float sum, float mx, float l) {
+        q4_close(s, lds, heads, tid, [&](int hd, int d, float sum, float mx, float l) {
             if (!whole) {
                 partials[(hd * places + place) * RA_D + d] = sum;
                 if (d == 0) reinterpret_cast<float2*>(partials + HEADS * places * RA_D)[hd * places + place] = make_float2(mx, l);
@@ -696,7 +699,7 @@ __global__ __launch_bounds__(Q4_THREADS, 3) void q4_attend_kernel(const void* __
                     c.vs + kv_head * c.kv_stride * Q4_BLOCKS, c.kv_stride};
     const Q4Rows src = om ? Q4Rows{ids + head0 * topk, N, 0, 0, topk} : Q4Rows{nullptr, N, s, w, (int)(s + N - w)};
     const int span = om ? spanG : spanS, from = part * span, to = from + span < src.count ? from + span : src.count;
-    Q4Wave<DT, HEADS> st;
+    Q4Wave<DT, HEADS, 3> st;
     st.start(reinterpret_cast<const char*>(q) + head0 * RA_D * (DT == RA_BF16 ? 2 : 4), heads, lane);
     for (int at = from + wv * Q4_CHUNK; at < to; at += Q4_WAVES * Q4_CHUNK) {
         Q4Chunk ch;
@@ -710,7 +713,7 @@ __global__ __launch_bounds__(Q4_THREADS, 3) void q4_attend_kernel(const void* __
         }
         st.template add<false>(ch, there, lane);
     }
-    q4_close<DT, HEADS>(st, lds, heads, tid, [&](int hd, int d, float sum, float mx, float l) {
+    q4_close(st, lds, heads, tid, [&](int hd, int d, float sum, float mx, float l) {
         float* rec = partials + ((head0 + hd) * P + slot) * Q4_REC;
         q4_store<TICKETS>(rec + d, sum);
         if (d == 0) { q4_store<TICKETS>(rec + RA_D, mx); q4_store<TICKETS>(rec + RA_D + 1, l); }
