@@ -341,8 +341,10 @@ ra_status ra_full_attention_q4(const void* q, ra_dtype dt, const uint8_t* K4, co
 /* ra_attend over a cache in 4 bits (what follows ra_search or ra_search_q8 where no other cache is kept): Eq. 2 over Omega = ids
  * and over W, their combination by Eq. 4-5 into out/lse, and the four partial outputs, each of which may be NULL. N >= the
  * index's N tokens are in the cache, N <= kv_stride; as in ra_decode_step_grown W = [0, sink) u [min(N - window, N_index), N).
- * ids must not contain members of W; -1 and ids >= N are skipped. Weights have 24 bits for both types. Errors as for ra_attend. Calls on one handle share its workspace:
- * calls that overlap in time on one handle race. */
+ * ids must not contain members of W; -1 and ids >= N are skipped. Weights have 24 bits for both types. Errors as for ra_attend.
+ * Calls on one handle share its workspace: calls that overlap in time on one handle race. The workspace grows with the sizes of the
+ * calls, which cannot be done under capture: make a call of these sizes or larger before. A captured call stays good for
+ * as long as the handle lives, whatever later calls need. */
 ra_status ra_attend_q4(const void* q, const ra_index* idx, ra_dtype dt, const uint8_t* K4, const uint8_t* K4s,
                        const uint8_t* V4, const uint8_t* V4s, int64_t N, int64_t kv_stride, int sink, int window, int topk,
                        const int32_t* ids, void* stream, float* out, float* lse, float* o_omega, float* lse_omega,

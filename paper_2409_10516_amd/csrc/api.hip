@@ -170,6 +170,8 @@ extern "C" void ra_index_free(ra_index* ix) {
     if (!ix) return;
     if (ix->adj) (void)hipFree(ix->adj);                 // (and what lies behind the graphs)
     if (ix->partials) (void)hipFree(ix->partials);
+    if (ix->q4_ws) (void)hipFree(ix->q4_ws);
+    for (int i = 0; i < ix->q4_olds; ++i) (void)hipFree(ix->q4_old[i]);
     if (ix->ids_ws) (void)hipFree(ix->ids_ws);
     if (ix->bitset) (void)hipFree(ix->bitset);
     if (ix->seeds) (void)hipFree(ix->seeds);
@@ -274,7 +276,7 @@ extern "C" int64_t ra_index_info(const ra_index* ix, int what) {
         case 4: return ix->deg;
         case 5: return (int64_t)(ix->graph_bytes + (size_t)ix->n_seq * ix->n_q * 4 +
                                  ix->partials_bytes + ix->ids_bytes + ix->bitset_bytes + coop_bytes(ix) +
-                                 ix->seedx_bytes + ix->walk_bytes +
+                                 ix->seedx_bytes + ix->walk_bytes + ix->q4_ws_bytes + ix->q4_old_bytes +
                                  (size_t)ix->n_seq * ix->n_q * (ix->root_cap + ix->seed_cap) * sizeof(int32_t));
         case 6: {
             if (ix->coop_mode != RA_HELPERS_ON || ix->coop_silent) return 0;
@@ -907,7 +909,18 @@ extern "C" ra_status ra_attend_q4(const void* q, const ra_index* idx, ra_dtype d
     RA_TRY(check_aligned(q, 16, "q"));
     ra_index* ix = const_cast<ra_index*>(idx);
     const size_t need = ra_attend_q4_partial_floats(dt, ix->n_seq, ix->n_q, ix->n_kv, N, ix->N, sink, window, topk) * sizeof(float);
-    RA_TRY(grow((void**)&ix->partials, &ix->partials_bytes, need));
+    if (need > ix->q4_ws_bytes) {
+        const size_t bytes = need > 2 * ix->q4_ws_bytes ? need : 2 * ix->q4_ws_bytes;
+        void* p = nullptr;
+        if (ix->q4_olds >= (int)(sizeof(ix->q4_old) / sizeof(ix->q4_old[0]))) RA_FAIL(RA_ENOMEM, "the handle's workspace has grown too often");
+        RA_HIP(hipMalloc(&p, bytes));
+        if (ix->q4_ws) {
+            ix->q4_old[ix->q4_olds++] = ix->q4_ws;
+            ix->q4_old_bytes += ix->q4_ws_bytes;
+        }
+        ix->q4_ws = reinterpret_cast<float*>(p);
+        ix->q4_ws_bytes = bytes;
+    }
     return ra_launch_attend_q4(q, dt, Q4Cache{K4, K4s, V4, V4s, kv_stride}, ix->n_seq, ix->n_q, ix->n_kv, N, ix->N, sink, window, topk,
-                               ids, ix->partials, attend_tickets(ix), (hipStream_t)stream, out, lse, o_omega, lse_omega, o_w, lse_w);
+                               ids, ix->q4_ws, attend_tickets(ix), (hipStream_t)stream, out, lse, o_omega, lse_omega, o_w, lse_w);
 }

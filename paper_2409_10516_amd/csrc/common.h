@@ -60,6 +60,12 @@ struct ra_index {
     // decode workspace, grown on demand (never shrinks)
     float* partials;    // attention partial records
     size_t partials_bytes;
+    // the same of ra_attend_q4, and the smaller ones it had before, which calls in captured graphs still write to: each at least
+    // twice its predecessor, freed with the handle
+    float* q4_ws;
+    size_t q4_ws_bytes, q4_old_bytes;
+    void* q4_old[48];
+    int q4_olds;
     int32_t* ids_ws;    // [n_seq*n_q][topk] when the caller passes ids == NULL
     size_t ids_bytes;
     uint32_t* bitset;   // global visited bitsets for contexts too long for LDS

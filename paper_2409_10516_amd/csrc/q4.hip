@@ -22,10 +22,11 @@
 //   sums    O[dimension][column] += V^T P. The lane's weights of the two halves are 8 consecutive slots of the contraction, so
 //           they go in as they come out; V^T wants for them, per dimension, the same 8 rows. Lane (kg, r) reads codes 8 r .. 8 r + 7 of
 //           these rows, four bytes each (16 lanes read a row): instruction m takes the m-th of each, dimension 8 r + m.
-// Codes become bfloat16 exactly. A float32 weight goes in as terms of bfloat16, the first as rounded, the next what the rounding left, an
-// instruction for each: 2 (16 bits) for bfloat16, 3 (24 bits) for float32, whose queries are three terms too. The sum of the
-// weights is that of the terms (an instruction with a row of ones), so that what their rounding does to a weight that has nearly
-// everything cancels.
+// Codes become bfloat16 exactly. A float32 weight goes in as TERMS terms of bfloat16, the first as rounded, the next what the rounding
+// left, an instruction for each: 2 (16 bits) for bfloat16 over all tokens, else 3 (24 bits). Sparse sets are a few rows with all the
+// weight: with 16 bits their outputs were up to 1.2e-6 off (2-norm), with 24 bits 0.2e-6, for 2 % of the time; over all tokens 16 bits are
+// 0.7e-6 off, and 24 would be 2 to 7 % of the time. Float32 queries are three terms too. The sum of the weights is that of the terms (an
+// instruction with a row of ones), so that what their rounding does to a weight that has nearly everything cancels.
 // Columns are heads, HEADS of them; where that is 8 or 4, two or four groups of columns have the same heads, and a lane makes the weights of
 // half or a quarter of its rows only (the others are zero): exponentials and splits are what vector instructions are short of,
 // not matrix instructions. Every column has a maximum and sums of its own; they are put together at the end.
@@ -751,32 +752,34 @@ static int q4_heads(int group) { return group <= 4 ? 4 : group <= 8 ? 8 : 16; }
 // many, or all of a head's rows are few units. Otherwise three workgroups fit a compute unit; where few jobs share them, two
 // leave fewer records to combine (us, two and three: 8 jobs of 131072 rows 37.1, 38.0, one of a million 39.4, 40.5, 64 of 20011
 // 33.9, 34.3, 128 of up to 32768 64.2, 62.6).
-struct Q4Cut { int tiles, workgroups, unit_log2; bool whole; };
+#define Q4_MOST_WHOLE (1 << 24)     // rows whose codes a stretch reaches with 32 bits
+struct Q4Cut { int tiles, workgroups, unit_log2; bool whole, refused; };
 static Q4Cut q4_cut(int n_seq, int n_q, int n_kv, int64_t N) {
     Q4Cut x;
     const int heads = q4_heads(n_q / n_kv);
     x.tiles = (n_q / n_kv + heads - 1) / heads;
     const int64_t jobs = (int64_t)n_seq * n_kv * x.tiles;
-    x.whole = jobs >= 2048 || N <= Q4_LEAST_UNITS * Q4_UNIT;
+    x.whole = (jobs >= 2048 && N <= Q4_MOST_WHOLE) || N <= Q4_LEAST_UNITS * Q4_UNIT;
     x.unit_log2 = 7;
     static_assert(Q4_UNIT == 1 << 7, "rows of a unit");
     auto units = [&] { return jobs * ((N + ((int64_t)1 << x.unit_log2) - 1) >> x.unit_log2); };
-    while (!x.whole && units() > Q4_MOST_UNITS) ++x.unit_log2;
+    while (!x.whole && jobs <= Q4_MOST_UNITS && units() > Q4_MOST_UNITS) ++x.unit_log2;
+    x.refused = (x.whole ? jobs : 0) >= 1 << 24 || (!x.whole && jobs > Q4_MOST_UNITS);
     const int most = jobs <= 64 ? Q4_MOST_WORKGROUPS / 3 * 2 : Q4_MOST_WORKGROUPS;
-    x.workgroups = (int)(x.whole ? (jobs < (1 << 24) ? jobs : 1 << 24) : units() < most ? units() : most);
+    x.workgroups = (int)(x.whole ? (x.refused ? 0 : jobs) : units() < most ? units() : most);
     return x;
 }
 
 size_t ra_full_q4_partial_floats(ra_dtype, int n_seq, int n_q, int n_kv, int64_t N) {
     const Q4Cut x = q4_cut(n_seq, n_q, n_kv, N);
-    return x.whole ? 0 : ((size_t)x.workgroups + (size_t)n_seq * n_kv * x.tiles) * q4_heads(n_q / n_kv) * (RA_D + 2);
+    return x.whole || x.refused ? 0 : ((size_t)x.workgroups + (size_t)n_seq * n_kv * x.tiles) * q4_heads(n_q / n_kv) * (RA_D + 2);
 }
 
 #define Q4_FEW_RECORDS 32
 ra_status ra_launch_full_q4(const void* q, ra_dtype dt, const Q4Cache& c, int n_seq, int n_q, int n_kv, int64_t N,
                             const int32_t* n_tokens, float* partials, hipStream_t st, float* out, float* lse) {
     const Q4Cut x = q4_cut(n_seq, n_q, n_kv, N);
-    if (x.workgroups >= 1 << 24) RA_FAIL(RA_EUNSUP, "too many (sequence, KV head) pairs for one launch");
+    if (x.refused) RA_FAIL(RA_EUNSUP, "too many heads for one launch");
 #define Q4_GO(DTV, HV)                                                                                                         \
     hipLaunchKernelGGL((q4_full_kernel<DTV, HV>), dim3(x.workgroups), dim3(Q4_THREADS), 0, st, q, c, n_seq, n_q, n_kv, (int)N, n_tokens, \
                        x.tiles, x.unit_log2, (int)x.whole, partials, out, lse)

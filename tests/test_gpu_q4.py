@@ -104,6 +104,46 @@ def test_full_attention_of_any_length(dtype, N):
             _check(out[s, h], lse[s, h], to_np(q[s, h]), K[s, 0], V[s, 0], np.arange(n), dtype)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n_seq,n_q,n_kv,N", [(130, 4, 1, 700), (67, 1, 1, 300), (2100, 1, 1, 300), (1030, 2, 2, 257), (2, 40, 1, 3000), (1, 2, 1, 20001),
+                                             (1, 17, 1, 40000), (3, 3, 1, 9999)])
+def test_full_attention_of_many_sequences_heads_and_records(dtype, n_seq, n_q, n_kv, N):
+    """More sequences than lanes, more jobs than are cut, tiles of heads, more records of a head than one thread per dimension
+    combines; lengths of zero, one and anything, some of them in a row."""
+    rng = np.random.default_rng(N)
+    lens = rng.integers(0, N + 1, n_seq)
+    lens[rng.random(n_seq) < 0.3] = 0
+    lens[-1] = N
+    if n_seq > 4:
+        lens[1], lens[2], lens[n_seq // 2:n_seq // 2 + 3] = 1, 129, 0
+    k4, v4, K, V = _cache(1, n_kv, N, seed=N)                # (the same rows for all sequences)
+    k4, v4 = (tuple(t.expand(n_seq, -1, -1, -1).contiguous() for t in x) for x in (k4, v4))
+    q = _queries(n_seq, n_q, dtype, N)
+    out, lse = ra.ra_full_attention_q4(q.to(DEV), k4, v4, torch.from_numpy(lens.astype(np.int32)).to(DEV))
+    out, lse = out.cpu().numpy(), lse.cpu().numpy()
+    assert (out[lens == 0] == 0).all() and np.isneginf(lse[lens == 0]).all() and np.isfinite(lse[lens > 0]).all()
+    some = {0, 1, 2, n_seq - 1} | set(rng.integers(0, n_seq, 6).tolist())
+    for s in sorted(x for x in some if x < n_seq):
+        for h in sorted({0, n_q // 2, n_q - 1}):
+            g = h // (n_q // n_kv)
+            _check(out[s, h], lse[s, h], to_np(q[s, h]), K[0, g], V[0, g], np.arange(lens[s]), dtype)
+
+
+def test_a_capacity_of_hundreds_of_millions():
+    """The list of rows is counted in larger units then; most of the capacity is not used."""
+    cap, T = 300_000_000, 6001
+    k4, v4 = ((torch.empty((1, 1, cap, 64), dtype=torch.uint8, device=DEV), torch.empty((1, 1, cap, 4), dtype=torch.uint8, device=DEV))
+              for _ in range(2))
+    a4, b4, K, V = _cache(1, 1, T, seed=4)
+    for x, y in ((k4, a4), (v4, b4)):
+        for s, t in zip(x, y):
+            s[:, :, :T] = t
+    q = _queries(1, 3, torch.bfloat16, 4)
+    out, lse = ra.ra_full_attention_q4(q.to(DEV), k4, v4, torch.tensor([T], dtype=torch.int32, device=DEV))
+    for h in range(3):
+        _check(out[0, h].cpu().numpy(), float(lse[0, h]), to_np(q[0, h]), K[0, 0], V[0, 0], np.arange(T), torch.bfloat16)
+
+
 def test_lengths_outside_the_cache_are_cut():
     k4, v4, K, V = _cache(3, 2, 90, seed=1)
     q = _queries(3, 4, torch.float32, 1)
@@ -377,6 +417,32 @@ def test_captured_token_replays_as_positions_advance():
             assert all(torch.equal(c, d) for c, d in zip(a, b))
     idx.free()
     ref_idx.free()
+
+
+def test_a_captured_call_outlives_the_growth_of_its_workspace():
+    """A larger call on the handle takes a larger workspace; a graph captured before goes on with its own."""
+    k4, v4, _, _ = _cache(1, 1, 3000, seed=31)
+    idx = _handle(1, 4, 1, 3000)
+    q = _queries(1, 4, torch.bfloat16, 31).to(DEV)
+    ids = torch.randint(10, 2000, (1, 4, 300), dtype=torch.int32, device=DEV)
+    ref = [t.clone() for t in ra.ra_attend_q4(q, idx, k4, v4, 4, 100, ids)]
+    out, lse = torch.empty_like(ref[0]), torch.empty_like(ref[1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ra.ra_attend_q4(q, idx, k4, v4, 4, 100, ids, out=out, lse=lse)
+    before = idx.device_bytes
+    big = [t.clone() for t in ra.ra_attend_q4(q, idx, k4, v4, 4, 2500, ids[..., :200].contiguous())]
+    assert idx.device_bytes > before
+    keep = torch.full((1 << 20,), 3.0, device=DEV)
+    for _ in range(4):
+        out.fill_(float("nan"))
+        lse.fill_(float("nan"))
+        graph.replay()
+        again = ra.ra_attend_q4(q, idx, k4, v4, 4, 2500, ids[..., :200].contiguous())
+        torch.cuda.synchronize()
+        assert torch.equal(out, ref[0]) and torch.equal(lse, ref[1])
+        assert torch.equal(again[0], big[0]) and (keep == 3.0).all()
+    idx.free()
 
 
 def test_calls_on_their_own_streams():
