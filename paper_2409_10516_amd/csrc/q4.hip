@@ -335,6 +335,10 @@ __device__ __forceinline__ Q4List q4_list(const int32_t* n_tokens, int n_seq, in
         x.units = q4_units(N, unit_log2) * n_seq * jobs;
         x.first = q4_units(N, unit_log2) * seq * jobs;
         x.n = N;
+    } else if (n_seq == 1) {        // (a scalar load, and nothing to add up)
+        x.n = x.rows = q4_rows_of(n_tokens, 0, N);
+        x.units = q4_units(x.n, unit_log2) * jobs;
+        x.first = 0;
     } else {
         uint32_t all = 0, before = 0, mine = 0;
         const int lane = threadIdx.x & 63;
@@ -357,6 +361,10 @@ __device__ __forceinline__ Q4List q4_list(const int32_t* n_tokens, int n_seq, in
 // the sequence that has unit `unit` (one of the list's), and where its part begins
 __device__ __forceinline__ int q4_seq_of(const Q4List& x, const int32_t* n_tokens, int n_seq, int N, int unit_log2, uint32_t jobs,
                                          uint32_t unit, uint32_t* first) {
+    if (n_seq == 1) {
+        *first = 0;
+        return 0;
+    }
     if (!n_tokens) {
         const uint32_t per = q4_units(N, unit_log2) * jobs, seq = unit / per;
         *first = seq * per;
@@ -379,7 +387,7 @@ __device__ __forceinline__ int q4_seq_of(const Q4List& x, const int32_t* n_token
 }
 
 template <int DT, int HEADS>
-__global__ __launch_bounds__(Q4_THREADS, 3) void q4_full_kernel(const void* __restrict__ q, Q4Cache c, int n_seq, int n_q,
+__global__ __launch_bounds__(Q4_THREADS, DT == RA_BF16 ? 3 : 2) void q4_full_kernel(const void* __restrict__ q, Q4Cache c, int n_seq, int n_q,
                                                                                   int n_kv, int N, const int32_t* __restrict__ n_tokens,
                                                                                   int tiles, int unit_log2, int whole, float* __restrict__ partials,
                                                                                   float* __restrict__ out, float* __restrict__ lse) {
@@ -749,36 +757,37 @@ static int q4_heads(int group) { return group <= 4 ? 4 : group <= 8 ? 8 : 16; }
     } while (0)
 
 // How a call is cut: tiles of query heads per KV head, workgroups, and whether each has a job of its own. That is so where the jobs are
-// many, or all of a head's rows are few units. Otherwise three workgroups fit a compute unit; where few jobs share them, two
+// many, or a head's rows few: shared out, 512 rows of 8 jobs take 8.7 us and by themselves 6.9, 1000 rows 8.9 and 9.5 (and a launch less on
+// the host's side), 2000 rows 8.9 and 14.0; 128 jobs of 1000 rows 12.8 and 10.4, of 2000 16.8 and 15.4, of 4000 21.7 and 24.3. Otherwise three workgroups of bfloat16 fit a compute unit, two of float32; where few jobs share them, two
 // leave fewer records to combine (us, two and three: 8 jobs of 131072 rows 37.1, 38.0, one of a million 39.4, 40.5, 64 of 20011
 // 33.9, 34.3, 128 of up to 32768 64.2, 62.6).
 #define Q4_MOST_WHOLE (1 << 24)     // rows whose codes a stretch reaches with 32 bits
 struct Q4Cut { int tiles, workgroups, unit_log2; bool whole, refused; };
-static Q4Cut q4_cut(int n_seq, int n_q, int n_kv, int64_t N) {
+static Q4Cut q4_cut(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N) {
     Q4Cut x;
     const int heads = q4_heads(n_q / n_kv);
     x.tiles = (n_q / n_kv + heads - 1) / heads;
     const int64_t jobs = (int64_t)n_seq * n_kv * x.tiles;
-    x.whole = (jobs >= 2048 && N <= Q4_MOST_WHOLE) || N <= Q4_LEAST_UNITS * Q4_UNIT;
+    x.whole = (jobs >= 2048 && N <= Q4_MOST_WHOLE) || N <= (jobs >= 128 ? 2048 : 1024);
     x.unit_log2 = 7;
     static_assert(Q4_UNIT == 1 << 7, "rows of a unit");
     auto units = [&] { return jobs * ((N + ((int64_t)1 << x.unit_log2) - 1) >> x.unit_log2); };
     while (!x.whole && jobs <= Q4_MOST_UNITS && units() > Q4_MOST_UNITS) ++x.unit_log2;
     x.refused = (x.whole ? jobs : 0) >= 1 << 24 || (!x.whole && jobs > Q4_MOST_UNITS);
-    const int most = jobs <= 64 ? Q4_MOST_WORKGROUPS / 3 * 2 : Q4_MOST_WORKGROUPS;
+    const int most = jobs <= 64 || dt == RA_F32 ? Q4_MOST_WORKGROUPS / 3 * 2 : Q4_MOST_WORKGROUPS;
     x.workgroups = (int)(x.whole ? (x.refused ? 0 : jobs) : units() < most ? units() : most);
     return x;
 }
 
-size_t ra_full_q4_partial_floats(ra_dtype, int n_seq, int n_q, int n_kv, int64_t N) {
-    const Q4Cut x = q4_cut(n_seq, n_q, n_kv, N);
+size_t ra_full_q4_partial_floats(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N) {
+    const Q4Cut x = q4_cut(dt, n_seq, n_q, n_kv, N);
     return x.whole || x.refused ? 0 : ((size_t)x.workgroups + (size_t)n_seq * n_kv * x.tiles) * q4_heads(n_q / n_kv) * (RA_D + 2);
 }
 
 #define Q4_FEW_RECORDS 32
 ra_status ra_launch_full_q4(const void* q, ra_dtype dt, const Q4Cache& c, int n_seq, int n_q, int n_kv, int64_t N,
                             const int32_t* n_tokens, float* partials, hipStream_t st, float* out, float* lse) {
-    const Q4Cut x = q4_cut(n_seq, n_q, n_kv, N);
+    const Q4Cut x = q4_cut(dt, n_seq, n_q, n_kv, N);
     if (x.refused) RA_FAIL(RA_EUNSUP, "too many heads for one launch");
 #define Q4_GO(DTV, HV)                                                                                                         \
     hipLaunchKernelGGL((q4_full_kernel<DTV, HV>), dim3(x.workgroups), dim3(Q4_THREADS), 0, st, q, c, n_seq, n_q, n_kv, (int)N, n_tokens, \
