@@ -118,12 +118,14 @@ __device__ __forceinline__ void turn_halves(float (&v)[8], const float2* cs, boo
 }
 
 // A workgroup takes a token, or with few tokens, one of `split` parts of its heads: the sines and cosines of the token's angles, one
-// per lane of its first wavefront, then the heads' rows, one per 16 lanes. The first rows are asked for before the angles are
-// worked on. What this is bound by is how many rows are in flight: registers for eight wavefronts per SIMD.
-// A 32K prompt of 32 + 8 + 8 heads, us: with four tokens per workgroup, their factors and the weights in registers, and one row
-// asked for ahead 303; the same with one token 285.
-template <int DT>
-__global__ __launch_bounds__(KV_THREADS) void append_kernel(AppendArgs a, int split) {
+// per lane of its first wavefront, then the heads' rows, one per 16 lanes. What bounds it is how many rows are on their way, and
+// that tokens side by side are written together: registers for eight wavefronts per SIMD, and nothing asked for ahead.
+// A 32K prompt of 32 + 8 + 8 heads, 192 us (4.2 TB/s): with four tokens per workgroup, their factors and the weights in registers, and one
+// row asked for ahead 303; with the first rows asked for before the angles are worked on 250; with three rows on their way 222; with 16 heads, 32
+// or all of a token in a workgroup of 256, 512 or 768 threads, so that it has fewer turns, 281, 249, 298; with 8 heads at a time 200. Workgroups that go
+// through the rows of several tokens, so that their last turn is full: 8 + 8 + 8 heads 130 -> 148, 6 + 2 + 2 43 -> 48.
+template <int DT, int THREADS>
+__global__ __launch_bounds__(THREADS) void append_kernel(AppendArgs a, int split) {
     __shared__ float2 s_cs[RA_D / 2];
     __shared__ float4 s_w[2][RA_D / 4];
     const int tid = threadIdx.x, lane = tid & (RA_WAVE - 1), l16 = tid & 15, grp = tid >> 4;
@@ -132,7 +134,7 @@ __global__ __launch_bounds__(KV_THREADS) void append_kernel(AppendArgs a, int sp
     if (a.n_new && t >= a.n_new[seq]) return;                       // (uniform)
     const int64_t pos = (int64_t)(a.first ? a.first[seq] : 0) + t;
     const bool there[2] = {pos >= 0 && pos < a.stride[0], pos >= 0 && pos < a.stride[1]};
-    const int n_rows = a.n_q + 2 * a.n_kv, step = KV_GROUPS * split, rot = a.rot, half = rot / 2;
+    const int n_rows = a.n_q + 2 * a.n_kv, step = THREADS / 16 * split, rot = a.rot, half = rot / 2;
     // a row's input; none where there is no such row, no input, or no cache that has the row
     auto row_of = [&](int r) __attribute__((always_inline)) -> const char* {
         if (r >= n_rows) return nullptr;
@@ -142,20 +144,18 @@ __global__ __launch_bounds__(KV_THREADS) void append_kernel(AppendArgs a, int sp
         return reinterpret_cast<const char*>(a.in[which]) + ((size_t)tok * a.row[which] + (size_t)h * RA_D) * esz;
     };
     if (tid < half) s_cs[tid] = cos_sin64((double)pos * (double)a.inv_freq[tid]);
-    if (tid >= KV_THREADS - RA_D) {                                // (other wavefronts than those of the angles)
-        const int d = tid - (KV_THREADS - RA_D);
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (a.weight[i])
+    for (int i = 0; i < 2; ++i)
+        if (a.weight[i])                                           // (the last wavefronts first: the angles are the first one's)
+            for (int d = THREADS - 1 - tid; d < RA_D; d += THREADS)
                 reinterpret_cast<float*>(s_w[i])[d] = DT == RA_BF16 ? bf16_lo(reinterpret_cast<const uint16_t*>(a.weight[i])[d])
                                                                     : reinterpret_cast<const float*>(a.weight[i])[d];
-    }
     __syncthreads();
     const int near = half / 8;                                     // lanes of a half
     const bool low = l16 < near, in_rot = l16 < 2 * near;
     const int from = (lane & ~15) + (low ? l16 + near : in_rot ? l16 - near : l16);
     const float2* cs = s_cs + (!in_rot ? 0 : a.interleaved ? 4 * l16 : 8 * (low ? l16 : l16 - near));
-    for (int r = grp + (int)(blockIdx.x % split) * KV_GROUPS; r < n_rows; r += step) {
+    for (int r = grp + (int)(blockIdx.x % split) * (THREADS / 16); r < n_rows; r += step) {
         const char* in = row_of(r);
         if (!in) continue;
         const int which = r < a.n_q ? 0 : r < a.n_q + a.n_kv ? 1 : 2;
@@ -204,8 +204,16 @@ ra_status ra_launch_append(const AppendArgs& a, ra_dtype dt, hipStream_t st) {
     const int heads = a.n_q + 2 * a.n_kv, split = tokens <= 128 ? (heads + KV_GROUPS - 1) / KV_GROUPS : 1;
     const int64_t blocks = tokens * split;
     if (blocks > (1 << 24) - 1) RA_FAIL(RA_EUNSUP, "too many heads for one launch");
-#define KV_GO(DTV) hipLaunchKernelGGL(append_kernel<DTV>, dim3((unsigned)blocks), dim3(KV_THREADS), 0, st, a, split)
+#define KV_GO_T(DTV, THREADS) hipLaunchKernelGGL((append_kernel<DTV, THREADS>), dim3((unsigned)blocks), dim3(THREADS), 0, st, a, split)
+    // (tokens of few rows: 100000 of 1 + 1 + 1 heads 127 us with 256 threads, 82 with 64; 5000 of 4 + 1 + 1 12.1 and with 128 10.5)
+#define KV_GO(DTV)                                  \
+    do {                                            \
+        if (heads <= 4) KV_GO_T(DTV, 64);           \
+        else if (heads <= 8) KV_GO_T(DTV, 128);     \
+        else KV_GO_T(DTV, KV_THREADS);              \
+    } while (0)
     if (dt == RA_BF16) KV_GO(RA_BF16); else KV_GO(RA_F32);
+#undef KV_GO_T
 #undef KV_GO
     RA_HIP(hipGetLastError());
     return RA_OK;
