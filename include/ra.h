@@ -283,8 +283,8 @@ ra_status ra_decode_step_q8(const void* q, const ra_index* idx, const void* K, c
  *     codes  [n_seq][n_kv_heads][kv_stride][64] uint8, 16-byte aligned; dimension 2 i in the low half of byte i,
  *     scale  [n_seq][n_kv_heads][kv_stride][4]  uint8, 4-byte aligned;
  * a code is a sign (bit 3) and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6, a scale byte b stands for 2^(b - 127), 255 for NaN
- * (the E2M1 and E8M0 formats of the OCP microscaling specification, which the matrix part of a compute unit converts
- * by itself). kv_stride is the capacity: rows from one head to the next.
+ * (the E2M1 and E8M0 formats of the OCP microscaling specification, which a compute unit converts by itself; values past
+ * float32, from scale bytes that nothing here writes, are infinite, and NaN in an attention's sums). kv_stride is the capacity: rows from one head to the next.
  * Written here, the scale of a block is the least power of two with which no value exceeds 6 (at least 2^-125), and a
  * value becomes the nearest code, ties to the even one. A block with a NaN, an infinity or a magnitude of 2^127 or more
  * has scale byte 255 and codes of zero: all its values read as NaN.

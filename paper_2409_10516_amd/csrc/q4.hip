@@ -2,7 +2,7 @@
 // Sec. 3.3 with their combination by Eq. 4-5 (ra_attend_q4).
 //
 // Rows are cut into parts; a workgroup turns one part into a record (128 weighted sums, the running maximum of
-// z log2(e), the sum of weights), and a second kernel combines a head's records. Weights are powers of two,
+// z log2(e), the sum of weights), and a head's records are combined by a second kernel or by whoever stores the last. Weights are powers of two,
 // p = 2^(c <q, k> - m) with c = log2(e) / sqrt(d): one multiply-add and one instruction each.
 #include "q4_dev.h"
 #include "ticket.h"
@@ -757,10 +757,11 @@ static int q4_heads(int group) { return group <= 4 ? 4 : group <= 8 ? 8 : 16; }
     } while (0)
 
 // How a call is cut: tiles of query heads per KV head, workgroups, and whether each has a job of its own. That is so where the jobs are
-// many, or a head's rows few: shared out, 512 rows of 8 jobs take 8.7 us and by themselves 6.9, 1000 rows 8.9 and 9.5 (and a launch less on
-// the host's side), 2000 rows 8.9 and 14.0; 128 jobs of 1000 rows 12.8 and 10.4, of 2000 16.8 and 15.4, of 4000 21.7 and 24.3. Otherwise three workgroups of bfloat16 fit a compute unit, two of float32; where few jobs share them, two
-// leave fewer records to combine (us, two and three: 8 jobs of 131072 rows 37.1, 38.0, one of a million 39.4, 40.5, 64 of 20011
-// 33.9, 34.3, 128 of up to 32768 64.2, 62.6).
+// many, or a head's rows few: shared out, 512 rows of 8 jobs take 8.7 us and by themselves 6.9, 1000 rows 8.9 and 9.5 (and a launch
+// less on the host's side), 2000 rows 8.9 and 14.0; 128 jobs of 1000 rows 12.8 and 10.4, of 2000 16.8 and 15.4, of 4000 21.7 and 24.3.
+// Otherwise three workgroups of bfloat16 fit a compute unit, two of float32; where few jobs share them, two leave fewer records to
+// combine (us, two and three: 8 jobs of 131072 rows 37.1, 38.0, one of a million 39.4, 40.5, 64 of 20011 33.9, 34.3, 128 of up to
+// 32768 64.2, 62.6).
 #define Q4_MOST_WHOLE (1 << 24)     // rows whose codes a stretch reaches with 32 bits
 struct Q4Cut { int tiles, workgroups, unit_log2; bool whole, refused; };
 static Q4Cut q4_cut(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N) {
