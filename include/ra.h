@@ -330,6 +330,8 @@ ra_status ra_dequantize_kv4(const uint8_t* codes, const uint8_t* scale, ra_dtype
  * min(n_tokens[s], N) (device int32; NULL: N for every sequence). A sequence without rows gets out = 0 and lse = -inf. Rows
  * from n on are not looked at. float32 accumulation; the weights of the softmax meet the values with 16 bits (dt = bfloat16)
  * or 24 (float32) of mantissa, and their sum is taken of what remains.
+ * RA_EUNSUP where a workgroup's part of one head would pass 2^24 rows (hundreds of query heads per KV head over tens of millions of
+ * tokens), and past 2^21 tiles of up to 16 query heads.
  * workspace: device memory of at least ra_full_attention_q4_workspace_bytes(...) bytes, 16-byte aligned, which nothing else may use
  * until the call has run; it needs no initialisation. */
 size_t ra_full_attention_q4_workspace_bytes(ra_dtype dt, int n_seq, int n_q_heads, int n_kv_heads, int64_t N);

@@ -7,6 +7,7 @@ if the library is missing, loading fails with an error.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import functools
 import os
@@ -190,6 +191,19 @@ def _here(*ts):
         if t is not None and t.get_device() != here:
             raise ValueError(f"tensors must live on the current GPU ({here}), not on {t.device}")
     return here
+
+
+_CURRENT = contextlib.nullcontext()
+
+
+def _for(stream, here: int):
+    """Where a call on `stream` allocates: there, or what it drops at its end (a workspace) would be another stream's while the
+    call still runs, and zeroes could come after its results."""
+    if stream is None:
+        return _CURRENT
+    if stream.device_index != here:
+        raise ValueError(f"stream must be one of the current GPU ({here})")
+    return torch.cuda.stream(stream)
 
 
 def _vector(t: torch.Tensor, n: int, dtype, here: int, name: str) -> int:
@@ -557,6 +571,7 @@ def ra_append_tokens(q, k, v, first, *, n_new=None, q_weight=None, k_weight=None
     if some is None:
         raise ValueError("at least one of q, k and v is needed")
     here = torch.cuda.current_device()
+    room_for = _for(stream, here)
     dtype, shape = some.dtype, some.shape
     if len(shape) != 4:
         raise ValueError("q, k and v must be [n_seq][T][heads][128]")
@@ -591,7 +606,8 @@ def ra_append_tokens(q, k, v, first, *, n_new=None, q_weight=None, k_weight=None
             raise ValueError("q_out goes with q")
     else:
         if q_out is None:
-            q_out = (torch.empty if n_new is None else torch.zeros)((n_seq, n_q, T, 128), dtype=dtype, device=q.device)
+            with room_for:
+                q_out = (torch.empty if n_new is None else torch.zeros)((n_seq, n_q, T, 128), dtype=dtype, device=here)
         elif q_out.dtype is not dtype or q_out.shape != (n_seq, n_q, T, 128) or not q_out.is_contiguous() or q_out.get_device() != here:
             raise ValueError("q_out must be contiguous [n_seq][n_q][T][128], of the dtype of q and where q is")
         out_at = q_out.data_ptr()
@@ -607,12 +623,14 @@ def ra_quantize_kv4(X, first=None, n_new=None, out=None, stream=None):
     [n_seq] on the GPU; n_new likewise: only so many rows); without, they are new and hold T rows."""
     _dev(X)
     here = _here(X)
+    room_for = _for(stream, here)
     n_seq, n_kv, T, d = X.shape
     if out is None:
         if first is not None or n_new is not None:
             raise ValueError("first and n_new go with out")
-        out = (torch.empty((n_seq, n_kv, T, 64), dtype=torch.uint8, device=X.device),
-               torch.empty((n_seq, n_kv, T, 4), dtype=torch.uint8, device=X.device))
+        with room_for:
+            out = (torch.empty((n_seq, n_kv, T, 64), dtype=torch.uint8, device=here),
+                   torch.empty((n_seq, n_kv, T, 4), dtype=torch.uint8, device=here))
     codes, scale, room = _kv4(out, n_seq, n_kv, "out", here)
     _check(lib().ra_quantize_kv4(X.data_ptr(), _dt(X), n_seq, n_kv, T, d, None if first is None else _vector(first, n_seq, torch.int32, here, "first"),
                                  None if n_new is None else _vector(n_new, n_seq, torch.int32, here, "n_new"), room, _stream(stream), codes, scale))
@@ -623,11 +641,13 @@ def ra_dequantize_kv4(x4, dtype, first=None, rows: Optional[int] = None, out=Non
     """Rows first[s] .. first[s] + rows (None: from 0, all) of a cache in 4 bits -> [n_seq][n_kv][rows][128] of the given dtype, the
     values they stand for."""
     here = _here(out)
+    room_for = _for(stream, here)
     n_seq, n_kv = x4[0].shape[:2]
     codes, scale, room = _kv4(x4, n_seq, n_kv, "x4", here)
     rows = room if rows is None else rows
     if out is None:
-        out = torch.empty((n_seq, n_kv, rows, 128), dtype=dtype, device=x4[0].device)
+        with room_for:
+            out = torch.empty((n_seq, n_kv, rows, 128), dtype=dtype, device=here)
     elif out.dtype is not dtype or out.shape != (n_seq, n_kv, rows, 128) or not out.is_contiguous():
         raise ValueError("out must be contiguous [n_seq][n_kv][rows][128], of the given dtype")
     _check(lib().ra_dequantize_kv4(codes, scale, _dt(out), n_seq, n_kv, rows, 128, None if first is None else _vector(first, n_seq, torch.int32, here, "first"),
@@ -665,6 +685,7 @@ def ra_full_attention_q4(q, k4, v4, n_tokens=None, N: Optional[int] = None, stre
     """Eq. 1 over the first n_tokens[s] rows (int32 [n_seq] on the GPU, at most N; None: N, by default the capacity) of a cache
     in 4 bits -> (out float32 [n_seq][n_q][128], lse float32 [n_seq][n_q])."""
     here = torch.cuda.current_device()
+    room_for = _for(stream, here)
     q_at, n_seq, n_q, d = _query(q, here)
     n_kv = k4[0].shape[1]
     K4, K4s, room = _kv4(k4, n_seq, n_kv, "k4", here)
@@ -673,12 +694,14 @@ def ra_full_attention_q4(q, k4, v4, n_tokens=None, N: Optional[int] = None, stre
     N = room if N is None else N
     if workspace is None:
         have = _full_q4_room(dt, n_seq, n_q, n_kv, N)
-        workspace = torch.empty(have, dtype=torch.uint8, device=here)
+        with room_for:
+            workspace = torch.empty(have, dtype=torch.uint8, device=here)
     else:
         _dev(workspace)
         _here(workspace)
         have = workspace.numel() * workspace.element_size()
-    out, lse = _results(n_seq, n_q, d, here, out, lse)
+    with room_for:
+        out, lse = _results(n_seq, n_q, d, here, out, lse)
     _check(lib().ra_full_attention_q4(q_at, dt, K4, K4s, V4, V4s, n_seq, n_q, n_kv, N, room, d,
                                       None if n_tokens is None else _vector(n_tokens, n_seq, torch.int32, here, "n_tokens"),
                                       workspace.data_ptr(), have, _stream(stream), out.data_ptr(), lse.data_ptr()))
@@ -690,6 +713,7 @@ def ra_attend_q4(q, idx: Index, k4, v4, sink: int, window: int, ids: torch.Tenso
     """ra_attend over a cache in 4 bits that holds N >= idx.N tokens (by default as many as its capacity); tokens behind the
     index's are static. -> (out, lse) or, with partials=True, (out, lse, o_omega, lse_omega, o_w, lse_w)."""
     here = torch.cuda.current_device()
+    room_for = _for(stream, here)
     q_at, n_seq, n_q, d = _query(q, here)
     n_kv, shape = k4[0].shape[1], ids.shape
     if (n_seq, n_q, n_kv) != idx.heads or d != 128:
@@ -699,12 +723,13 @@ def ra_attend_q4(q, idx: Index, k4, v4, sink: int, window: int, ids: torch.Tenso
         raise ValueError("ids must be contiguous int32 [n_seq][n_q][topk] on the current GPU")
     K4, K4s, room = _kv4(k4, n_seq, n_kv, "k4", here)
     V4, V4s, _ = _kv4(v4, n_seq, n_kv, "v4", here, room)
-    out, lse = _results(n_seq, n_q, d, here, out, lse)
     extra = ()
-    if partials:
-        f = dict(dtype=torch.float32, device=q.device)
-        extra = (torch.empty((n_seq, n_q, d), **f), torch.empty((n_seq, n_q), **f),
-                 torch.empty((n_seq, n_q, d), **f), torch.empty((n_seq, n_q), **f))
+    with room_for:
+        out, lse = _results(n_seq, n_q, d, here, out, lse)
+        if partials:
+            f = dict(dtype=torch.float32, device=here)
+            extra = (torch.empty((n_seq, n_q, d), **f), torch.empty((n_seq, n_q), **f),
+                     torch.empty((n_seq, n_q, d), **f), torch.empty((n_seq, n_q), **f))
     _check(_room(lib().ra_attend_q4, q_at, idx.handle, _dt(q), K4, K4s, V4, V4s, room if N is None else N, room, sink, window, shape[2],
                  ids.data_ptr(), _stream(stream), out.data_ptr(), lse.data_ptr(),
                  *([t.data_ptr() for t in extra] or (None, None, None, None))))

@@ -762,14 +762,14 @@ static int q4_heads(int group) { return group <= 4 ? 4 : group <= 8 ? 8 : 16; }
 // Otherwise three workgroups of bfloat16 fit a compute unit, two of float32; where few jobs share them, two leave fewer records to
 // combine (us, two and three: 8 jobs of 131072 rows 37.1, 38.0, one of a million 39.4, 40.5, 64 of 20011 33.9, 34.3, 128 of up to
 // 32768 64.2, 62.6).
-#define Q4_MOST_WHOLE (1 << 24)     // rows whose codes a stretch reaches with 32 bits
+#define Q4_MOST_ROWS (1 << 24)      // of one job in a stretch: places in its codes fit 31 bits
 struct Q4Cut { int tiles, workgroups, unit_log2; bool whole, refused; };
 static Q4Cut q4_cut(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N) {
     Q4Cut x;
     const int heads = q4_heads(n_q / n_kv);
     x.tiles = (n_q / n_kv + heads - 1) / heads;
     const int64_t jobs = (int64_t)n_seq * n_kv * x.tiles;
-    x.whole = (jobs >= 2048 && N <= Q4_MOST_WHOLE) || N <= (jobs >= 128 ? 2048 : 1024);
+    x.whole = (jobs >= 2048 && N <= Q4_MOST_ROWS) || N <= (jobs >= 128 ? 2048 : 1024);
     x.unit_log2 = 7;
     static_assert(Q4_UNIT == 1 << 7, "rows of a unit");
     auto units = [&] { return jobs * ((N + ((int64_t)1 << x.unit_log2) - 1) >> x.unit_log2); };
@@ -777,6 +777,8 @@ static Q4Cut q4_cut(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N) {
     x.refused = (x.whole ? jobs : 0) >= 1 << 24 || (!x.whole && jobs > Q4_MOST_UNITS);
     const int most = jobs <= 64 || dt == RA_F32 ? Q4_MOST_WORKGROUPS / 3 * 2 : Q4_MOST_WORKGROUPS;
     x.workgroups = (int)(x.whole ? (x.refused ? 0 : jobs) : units() < most ? units() : most);
+    // (a stretch is longest with all sequences at their longest; only very many query heads of one KV head get here)
+    if (!x.whole && !x.refused && N > Q4_MOST_ROWS) x.refused = ((units() / x.workgroups + 1) << x.unit_log2) > Q4_MOST_ROWS;
     return x;
 }
 

@@ -276,3 +276,16 @@ def test_refusals():
         ra.ra_append_tokens(qkv.expand(1, 4, 2, 128)[:, :1].expand(1, 4, 2, 128).cpu(), None, None, None)
     with pytest.raises(ra.RaError):
         ra.ra_append_tokens(qkv[:, :1].expand(1, 4, 2, 128), None, None, None)               # tokens on top of each other
+
+
+def test_rows_behind_the_last_token_are_zero_on_another_stream():
+    """The zeroes of a q_out that the call makes come before its rows, whatever the current stream is waiting for."""
+    x = torch.randn((2, 9, 4, 128), device=DEV)
+    n_new = torch.tensor([9, 4], dtype=torch.int32, device=DEV)
+    ref = ra.ra_append_tokens(x, None, None, None, n_new=n_new)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    torch.cuda._sleep(20_000_000)
+    got = ra.ra_append_tokens(x, None, None, None, n_new=n_new, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(got, ref) and (got[1, :, 4:] == 0).all() and torch.equal(got[1, :, :4], x[1, :4].transpose(0, 1))

@@ -464,6 +464,39 @@ def test_calls_on_their_own_streams():
             assert torch.equal(turn[i][0], refs[i][0]) and torch.equal(turn[i][1], refs[i][1])
 
 
+def test_calls_on_a_stream_allocate_there():
+    """A workspace that a call drops when it returns is not handed to the current stream while the call waits on its own."""
+    k4, v4, _, _ = _cache(2, 2, 5000, seed=22)
+    q = _queries(2, 8, torch.bfloat16, 33).to(DEV)
+    ref = ra.ra_full_attention_q4(q, k4, v4)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    need = B.lib().ra_full_attention_q4_workspace_bytes(B.RA_BF16, 2, 8, 2, 5000)
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+    got = ra.ra_full_attention_q4(q, k4, v4, stream=side)
+    for _ in range(400):                                     # (work on the current stream, in memory of the workspace's size)
+        torch.full((need // 4,), float("nan"), device=DEV)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
+
+
+class _Elsewhere:
+    """What a stream of another device looks like."""
+    cuda_stream, device_index = 0, 7
+
+
+def test_streams_of_another_device_are_refused():
+    k4, v4, _, _ = _cache(1, 1, 40, seed=23)
+    q = _queries(1, 4, torch.bfloat16, 34).to(DEV)
+    for call in (lambda st: ra.ra_full_attention_q4(q, k4, v4, stream=st),
+                 lambda st: ra.ra_append_tokens(q[:, None], None, None, None, stream=st),
+                 lambda st: ra.ra_quantize_kv4(torch.zeros(1, 1, 4, 128, device=DEV), stream=st),
+                 lambda st: ra.ra_dequantize_kv4(k4, torch.float32, stream=st)):
+        with pytest.raises(ValueError, match="current GPU"):
+            call(_Elsewhere())
+
+
 def test_oracle_decode_step_is_what_the_parts_make():
     """On rows that 4 bits hold exactly, ids from the walk over the keys and ra_attend_q4 are the fused decode step."""
     w = synth.make_llama_layer(61, N=500, M=200, T=1, n_q=4, n_kv=2, ef=40, topk=12, window=40, deg=10, knn=10)

@@ -72,6 +72,14 @@ def test_full_attention_refuses(change, status, needle):
     assert needle in L.ra_last_error().decode()
 
 
+@pytest.mark.parametrize("N,n_q,needle", [((1 << 24) + 1, 16 * 1024, "too many heads"), ((1 << 30) - 1, 16 * 2047, "too many heads")])
+def test_full_attention_refuses_stretches_past_31_bits(N, n_q, needle):
+    """Rows that a workgroup would take of one head, with 64 bytes of codes each."""
+    L = ra.lib()
+    assert L.ra_full_attention_q4(*(FULL | dict(n_q=n_q, n_kv=1, N=N, stride=N)).values()) == 6
+    assert needle in L.ra_last_error().decode()
+
+
 def test_workspace_sizes():
     L = ra.lib()
     size = L.ra_full_attention_q4_workspace_bytes
