@@ -173,17 +173,20 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
+_RAW = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream) -> int:
     """The stream's handle; by default the current device's current stream. torch's own accessor of the
     raw handle is used where it exists: building a Stream object costs as much as the rest of a call."""
     if stream is not None:
         return stream.cuda_stream
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return torch.cuda.current_stream().cuda_stream if raw is None else raw(torch.cuda.current_device())
+    return torch.cuda.current_stream().cuda_stream if _RAW is None else _RAW(torch.cuda.current_device())
 
 
 # The calls around a 4-bit cache take many tensors and are made once per token and layer: their checks read every attribute once
-# and build nothing (a tensor's attribute is some 0.1 us, a ctypes call with 20 arguments 2 us, a launch 2 us).
+# and build nothing (us: a tensor's attribute 0.05, a shape 0.1, the C entry's checks 0.6, a launch 3.4, a tensor made of sizes given one by
+# one 1.3, as a tuple 1.7).
 def _here(*ts):
     """The given tensors live on the current device, where the call is launched -> its index."""
     here = torch.cuda.current_device()
@@ -191,6 +194,11 @@ def _here(*ts):
         if t is not None and t.get_device() != here:
             raise ValueError(f"tensors must live on the current GPU ({here}), not on {t.device}")
     return here
+
+
+def _handle(stream, here: int) -> int:
+    """_stream, where the current device is known."""
+    return _stream(stream) if stream is not None or _RAW is None else _RAW(here)
 
 
 _CURRENT = contextlib.nullcontext()
@@ -607,12 +615,12 @@ def ra_append_tokens(q, k, v, first, *, n_new=None, q_weight=None, k_weight=None
     else:
         if q_out is None:
             with room_for:
-                q_out = (torch.empty if n_new is None else torch.zeros)((n_seq, n_q, T, 128), dtype=dtype, device=here)
+                q_out = (torch.empty if n_new is None else torch.zeros)(n_seq, n_q, T, 128, dtype=dtype, device=here)
         elif q_out.dtype is not dtype or q_out.shape != (n_seq, n_q, T, 128) or not q_out.is_contiguous() or q_out.get_device() != here:
             raise ValueError("q_out must be contiguous [n_seq][n_q][T][128], of the dtype of q and where q is")
         out_at = q_out.data_ptr()
     _check(lib().ra_append_tokens(q_at, k_at, v_at, _dt(some), n_seq, n_q or n_kv, n_kv, T, 128, q_row, k_row, v_row, qw_at, kw_at, eps,
-                                  f_at, rot, 1 if interleaved else 0, first_at, new_at, room, room4, _stream(stream), out_at, K_at, V_at,
+                                  f_at, rot, 1 if interleaved else 0, first_at, new_at, room, room4, _handle(stream, here), out_at, K_at, V_at,
                                   k4_at, k4s_at, v4_at, v4s_at))
     return q_out
 
@@ -633,7 +641,7 @@ def ra_quantize_kv4(X, first=None, n_new=None, out=None, stream=None):
                    torch.empty((n_seq, n_kv, T, 4), dtype=torch.uint8, device=here))
     codes, scale, room = _kv4(out, n_seq, n_kv, "out", here)
     _check(lib().ra_quantize_kv4(X.data_ptr(), _dt(X), n_seq, n_kv, T, d, None if first is None else _vector(first, n_seq, torch.int32, here, "first"),
-                                 None if n_new is None else _vector(n_new, n_seq, torch.int32, here, "n_new"), room, _stream(stream), codes, scale))
+                                 None if n_new is None else _vector(n_new, n_seq, torch.int32, here, "n_new"), room, _handle(stream, here), codes, scale))
     return out
 
 
@@ -647,22 +655,22 @@ def ra_dequantize_kv4(x4, dtype, first=None, rows: Optional[int] = None, out=Non
     rows = room if rows is None else rows
     if out is None:
         with room_for:
-            out = torch.empty((n_seq, n_kv, rows, 128), dtype=dtype, device=here)
+            out = torch.empty(n_seq, n_kv, rows, 128, dtype=dtype, device=here)
     elif out.dtype is not dtype or out.shape != (n_seq, n_kv, rows, 128) or not out.is_contiguous():
         raise ValueError("out must be contiguous [n_seq][n_kv][rows][128], of the given dtype")
     _check(lib().ra_dequantize_kv4(codes, scale, _dt(out), n_seq, n_kv, rows, 128, None if first is None else _vector(first, n_seq, torch.int32, here, "first"),
-                                   room, _stream(stream), out.data_ptr()))
+                                   room, _handle(stream, here), out.data_ptr()))
     return out
 
 
 def _results(n_seq, n_q, d, here, out, lse):
     """out [n_seq][n_q][d] and lse [n_seq][n_q], the given ones or new ones."""
     if out is None:
-        out = torch.empty((n_seq, n_q, d), dtype=torch.float32, device=here)
+        out = torch.empty(n_seq, n_q, d, dtype=torch.float32, device=here)
     elif out.dtype is not torch.float32 or out.shape != (n_seq, n_q, d) or not out.is_contiguous() or out.get_device() != here:
         raise ValueError("out must be contiguous float32 [n_seq][n_q][128] on the current GPU")
     if lse is None:
-        lse = torch.empty((n_seq, n_q), dtype=torch.float32, device=here)
+        lse = torch.empty(n_seq, n_q, dtype=torch.float32, device=here)
     elif lse.dtype is not torch.float32 or lse.shape != (n_seq, n_q) or not lse.is_contiguous() or lse.get_device() != here:
         raise ValueError("lse must be contiguous float32 [n_seq][n_q] on the current GPU")
     return out, lse
@@ -704,7 +712,7 @@ def ra_full_attention_q4(q, k4, v4, n_tokens=None, N: Optional[int] = None, stre
         out, lse = _results(n_seq, n_q, d, here, out, lse)
     _check(lib().ra_full_attention_q4(q_at, dt, K4, K4s, V4, V4s, n_seq, n_q, n_kv, N, room, d,
                                       None if n_tokens is None else _vector(n_tokens, n_seq, torch.int32, here, "n_tokens"),
-                                      workspace.data_ptr(), have, _stream(stream), out.data_ptr(), lse.data_ptr()))
+                                      workspace.data_ptr(), have, _handle(stream, here), out.data_ptr(), lse.data_ptr()))
     return out, lse
 
 
@@ -731,6 +739,6 @@ def ra_attend_q4(q, idx: Index, k4, v4, sink: int, window: int, ids: torch.Tenso
             extra = (torch.empty((n_seq, n_q, d), **f), torch.empty((n_seq, n_q), **f),
                      torch.empty((n_seq, n_q, d), **f), torch.empty((n_seq, n_q), **f))
     _check(_room(lib().ra_attend_q4, q_at, idx.handle, _dt(q), K4, K4s, V4, V4s, room if N is None else N, room, sink, window, shape[2],
-                 ids.data_ptr(), _stream(stream), out.data_ptr(), lse.data_ptr(),
+                 ids.data_ptr(), _handle(stream, here), out.data_ptr(), lse.data_ptr(),
                  *([t.data_ptr() for t in extra] or (None, None, None, None))))
     return (out, lse, *extra) if partials else (out, lse)
