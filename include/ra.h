@@ -301,7 +301,7 @@ ra_status ra_decode_step_q8(const void* q, const ra_index* idx, const void* K, c
  *               i < rot_dim / 2: (n_j, n_k) becomes (n_j cos a_i - n_k sin a_i, n_k cos a_i + n_j sin a_i) for the pair
  *               (j, k) = (i, i + rot_dim / 2), or with `interleaved` (2 i, 2 i + 1)
  * and one rounding to dt. Values are copied. The mean is taken in 64 bits and angles, their sines and cosines are computed in 64
- * bits (a position of a million times a frequency in 32 bits is off by a tenth of a radian); what follows is float32.
+ * bits (a position of a million times a frequency is rounded by up to 0.03 radians in 32); what follows is float32.
  *   q_in, k_in, v_in  [n_seq][T][heads][128] of type dt, the heads of a token side by side, tokens q_row, k_row and v_row
  *                     elements apart (the three may be parts of one buffer); each may be NULL with its outputs
  *   inv_freq          device float32 [rot_dim / 2], NULL with rot_dim 0
