@@ -102,18 +102,21 @@ __device__ __forceinline__ float2 cos_sin64(double x) {
     return make_float2(k == 1 || k == 2 ? -fc : fc, k & 2 ? -fs : fs);
 }
 
-// the value that the lane `step` further in the row's rotated part holds for the lower half, `step` back for the upper
+// Rotation of a row: a value times its cosine plus its pair's other value times its sine, which is negative for a pair's first. The other
+// value is in the same lane for neighbouring pairs, else STEP lanes away (0: in lane `from`).
 template <int STEP>
-__device__ __forceinline__ float other_half(float v, int lane, int from) {
-    if constexpr (STEP == 0) return __shfl(v, from);
-    else return __uint_as_float(lane_xor32<STEP>(__float_as_uint(v), lane));
-}
-template <int STEP>
-__device__ __forceinline__ void turn_halves(float (&v)[8], const float2* cs, bool in_rot, bool low, int lane, int from) {
+__device__ __forceinline__ void turn(float (&v)[8], const float2 (&cs)[8], bool in_rot, int lane, int from) {
+    float other[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const float other = other_half<STEP>(v[e], lane, from);
-        if (in_rot) v[e] = v[e] * cs[e].x + (low ? -other : other) * cs[e].y;
+        if constexpr (STEP < 0) other[e] = v[e ^ 1];
+        else if constexpr (STEP == 0) other[e] = __shfl(v[e], from);
+        else other[e] = __uint_as_float(lane_xor32<STEP>(__float_as_uint(v[e]), lane));
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float x = v[e] * cs[e].x + other[e] * cs[e].y;
+        v[e] = in_rot ? x : v[e];
     }
 }
 
@@ -125,7 +128,7 @@ __device__ __forceinline__ void turn_halves(float (&v)[8], const float2* cs, boo
 // or all of a token in a workgroup of 256, 512 or 768 threads, so that it has fewer turns, 281, 249, 298; with 8 heads at a time 200. Workgroups that go
 // through the rows of several tokens, so that their last turn is full: 8 + 8 + 8 heads 130 -> 148, 6 + 2 + 2 43 -> 48.
 template <int DT, int THREADS>
-__global__ __launch_bounds__(THREADS) void append_kernel(AppendArgs a, int split) {
+__global__ __launch_bounds__(THREADS, 8) void append_kernel(AppendArgs a, int split) {
     __shared__ float2 s_cs[RA_D / 2];
     __shared__ float4 s_w[2][RA_D / 4];
     const int tid = threadIdx.x, lane = tid & (RA_WAVE - 1), l16 = tid & 15, grp = tid >> 4;
@@ -135,14 +138,12 @@ __global__ __launch_bounds__(THREADS) void append_kernel(AppendArgs a, int split
     const int64_t pos = (int64_t)(a.first ? a.first[seq] : 0) + t;
     const bool there[2] = {pos >= 0 && pos < a.stride[0], pos >= 0 && pos < a.stride[1]};
     const int n_rows = a.n_q + 2 * a.n_kv, step = THREADS / 16 * split, rot = a.rot, half = rot / 2;
-    // a row's input; none where there is no such row, no input, or no cache that has the row
-    auto row_of = [&](int r) __attribute__((always_inline)) -> const char* {
-        if (r >= n_rows) return nullptr;
-        const int which = r < a.n_q ? 0 : r < a.n_q + a.n_kv ? 1 : 2;
-        if (!a.in[which] || (which && !there[0] && !there[1])) return nullptr;
-        const int h = which == 0 ? r : which == 1 ? r - a.n_q : r - a.n_q - a.n_kv;
-        return reinterpret_cast<const char*>(a.in[which]) + ((size_t)tok * a.row[which] + (size_t)h * RA_D) * esz;
-    };
+    // where the token's rows are, head 0's (none: no such input or output)
+    auto at = [&](const void* p, size_t row) { return p ? reinterpret_cast<char*>(const_cast<void*>(p)) + row * esz : nullptr; };
+    const char *in_q = at(a.in[0], tok * a.row[0]), *in_k = at(a.in[1], tok * a.row[1]), *in_v = at(a.in[2], tok * a.row[2]);
+    char* out_q = at(a.out[0], ((size_t)seq * a.n_q * T + t) * RA_D);
+    const size_t row0 = (size_t)seq * a.n_kv * a.stride[0] + pos, head4 = (size_t)seq * a.n_kv * a.stride[1] + pos;
+    char *out_k = at(a.out[1], row0 * RA_D), *out_v = at(a.out[2], row0 * RA_D);
     if (tid < half) s_cs[tid] = cos_sin64((double)pos * (double)a.inv_freq[tid]);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -154,14 +155,22 @@ __global__ __launch_bounds__(THREADS) void append_kernel(AppendArgs a, int split
     const int near = half / 8;                                     // lanes of a half
     const bool low = l16 < near, in_rot = l16 < 2 * near;
     const int from = (lane & ~15) + (low ? l16 + near : in_rot ? l16 - near : l16);
-    const float2* cs = s_cs + (!in_rot ? 0 : a.interleaved ? 4 * l16 : 8 * (low ? l16 : l16 - near));
+    float2 cs[8];                                                  // of the lane's dimensions, whatever the row
+    if (rot) {
+        const float2* at = s_cs + (!in_rot ? 0 : a.interleaved ? 4 * l16 : 8 * (low ? l16 : l16 - near));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            cs[e] = at[a.interleaved ? e / 2 : e];
+            if (a.interleaved ? !(e & 1) : low) cs[e].y = -cs[e].y;
+        }
+    }
     for (int r = grp + (int)(blockIdx.x % split) * (THREADS / 16); r < n_rows; r += step) {
-        const char* in = row_of(r);
-        if (!in) continue;
         const int which = r < a.n_q ? 0 : r < a.n_q + a.n_kv ? 1 : 2;
         const int h = which == 0 ? r : which == 1 ? r - a.n_q : r - a.n_q - a.n_kv;
+        const char* in = which == 0 ? in_q : which == 1 ? in_k : in_v;
+        if (!in || (which && !there[0] && !there[1])) continue;
         float v[8];
-        kv_floats<DT>(kv_load8<DT>(in, l16), v);
+        kv_floats<DT>(kv_load8<DT>(in + (uint64_t)(uint32_t)h * (RA_D * esz), l16), v);
         if (which < 2) {
             if (a.weight[which]) {
                 double sum = 0.;
@@ -173,26 +182,24 @@ __global__ __launch_bounds__(THREADS) void append_kernel(AppendArgs a, int split
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = v[e] * rinv * w[e];
             }
-            if (a.interleaved) {
-                if (in_rot)
-#pragma unroll
-                    for (int e = 0; e < 8; e += 2) {
-                        const float x = v[e], y = v[e + 1];
-                        v[e] = x * cs[e / 2].x - y * cs[e / 2].y;
-                        v[e + 1] = y * cs[e / 2].x + x * cs[e / 2].y;
-                    }
-            } else if (near == 8) turn_halves<8>(v, cs, in_rot, low, lane, from);
-            else if (near == 4) turn_halves<4>(v, cs, in_rot, low, lane, from);
-            else if (near) turn_halves<0>(v, cs, in_rot, low, lane, from);
+            if (rot) {
+                if (a.interleaved) turn<-1>(v, cs, in_rot, lane, from);
+                else if (near == 8) turn<8>(v, cs, in_rot, lane, from);
+                else if (near == 4) turn<4>(v, cs, in_rot, lane, from);
+                else turn<0>(v, cs, in_rot, lane, from);
+            }
             kv_round8<DT>(v);
         }
         if (which == 0) {
-            kv_store8<DT>(reinterpret_cast<char*>(a.out[0]) + (((size_t)seq * a.n_q + h) * T + t) * RA_D * esz, l16, v);
+            kv_store8<DT>(out_q + (uint64_t)(uint32_t)h * (uint32_t)T * (RA_D * esz), l16, v);
         } else {
-            const size_t head = (size_t)seq * a.n_kv + h, row = head * a.stride[0] + pos, row4 = head * a.stride[1] + pos;
-            if (a.out[which] && there[0]) kv_store8<DT>(reinterpret_cast<char*>(a.out[which]) + row * RA_D * esz, l16, v);
-            if (a.codes[which - 1] && there[1])
+            // (capacities are below 2^30 rows)
+            char* out = which == 1 ? out_k : out_v;
+            if (out && there[0]) kv_store8<DT>(out + (uint64_t)(uint32_t)h * (uint32_t)a.stride[0] * (RA_D * esz), l16, v);
+            if (a.codes[which - 1] && there[1]) {
+                const uint64_t row4 = head4 + (uint64_t)(uint32_t)h * (uint32_t)a.stride[1];
                 kv_store4(a.codes[which - 1] + row4 * Q4_ROW, a.scale[which - 1] + row4 * Q4_BLOCKS, l16, lane, v);
+            }
         }
     }
 }
