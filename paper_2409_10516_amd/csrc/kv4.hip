@@ -28,27 +28,26 @@ __device__ __forceinline__ void kv_floats(const KvRaw<DT>& x, float (&v)[8]) {
     }
 }
 typedef __bf16 kv_bf16x8 __attribute__((ext_vector_type(8)));
-// stores them, rounded to DT; v becomes what was stored
+// rounded to DT
 template <int DT>
-__device__ __forceinline__ void kv_round8(float (&v)[8]) {
-    if constexpr (DT == RA_BF16)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = (float)(__bf16)v[e];
-}
-template <int DT>
-__device__ __forceinline__ void kv_store8(void* row, int l16, const float (&v)[8]) {
-    kv_u32x4* to = reinterpret_cast<kv_u32x4*>(row);
+__device__ __forceinline__ KvRaw<DT> kv_pack(const float (&v)[8]) {
+    KvRaw<DT> x;
     if constexpr (DT == RA_BF16) {
         kv_bf16x8 b;
 #pragma unroll
         for (int e = 0; e < 8; ++e) b[e] = (__bf16)v[e];
-        __builtin_nontemporal_store(__builtin_bit_cast(kv_u32x4, b), to + l16);
+        x.a[0] = __builtin_bit_cast(kv_u32x4, b);
     } else {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            __builtin_nontemporal_store(kv_u32x4{__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]),
-                                                 __float_as_uint(v[4 * i + 3])}, to + 2 * l16 + i);
+        for (int e = 0; e < 8; ++e) x.a[e / 4][e & 3] = __float_as_uint(v[e]);
     }
+    return x;
+}
+template <int DT>
+__device__ __forceinline__ void kv_store8(void* row, int l16, const KvRaw<DT>& x) {
+    constexpr int W = DT == RA_BF16 ? 1 : 2;
+#pragma unroll
+    for (int i = 0; i < W; ++i) __builtin_nontemporal_store(x.a[i], reinterpret_cast<kv_u32x4*>(row) + W * l16 + i);
 }
 // A row of 16 lanes x 8 values into 4 bits. Called by whole groups of 16 lanes.
 __device__ __forceinline__ void kv_store4(uint8_t* codes, uint8_t* scale, int l16, int lane, const float (&v)[8]) {
@@ -115,7 +114,8 @@ __device__ __forceinline__ void turn(float (&v)[8], const float2 (&cs)[8], bool 
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const float x = v[e] * cs[e].x + other[e] * cs[e].y;
+        float x = v[e] * cs[e].x + other[e] * cs[e].y;
+        asm("" : "+v"(x));                                         // (not to be worked out behind a branch)
         v[e] = in_rot ? x : v[e];
     }
 }
@@ -169,9 +169,10 @@ __global__ __launch_bounds__(THREADS, 8) void append_kernel(AppendArgs a, int sp
         const int h = which == 0 ? r : which == 1 ? r - a.n_q : r - a.n_q - a.n_kv;
         const char* in = which == 0 ? in_q : which == 1 ? in_k : in_v;
         if (!in || (which && !there[0] && !there[1])) continue;
-        float v[8];
-        kv_floats<DT>(kv_load8<DT>(in + (uint64_t)(uint32_t)h * (RA_D * esz), l16), v);
+        KvRaw<DT> row = kv_load8<DT>(in + (uint64_t)(uint32_t)h * (RA_D * esz), l16);
         if (which < 2) {
+            float v[8];
+            kv_floats<DT>(row, v);
             if (a.weight[which]) {
                 double sum = 0.;
 #pragma unroll
@@ -188,15 +189,17 @@ __global__ __launch_bounds__(THREADS, 8) void append_kernel(AppendArgs a, int sp
                 else if (near == 4) turn<4>(v, cs, in_rot, lane, from);
                 else turn<0>(v, cs, in_rot, lane, from);
             }
-            kv_round8<DT>(v);
+            row = kv_pack<DT>(v);
         }
         if (which == 0) {
-            kv_store8<DT>(out_q + (uint64_t)(uint32_t)h * (uint32_t)T * (RA_D * esz), l16, v);
+            kv_store8<DT>(out_q + (uint64_t)(uint32_t)h * (uint32_t)T * (RA_D * esz), l16, row);
         } else {
             // (capacities are below 2^30 rows)
             char* out = which == 1 ? out_k : out_v;
-            if (out && there[0]) kv_store8<DT>(out + (uint64_t)(uint32_t)h * (uint32_t)a.stride[0] * (RA_D * esz), l16, v);
+            if (out && there[0]) kv_store8<DT>(out + (uint64_t)(uint32_t)h * (uint32_t)a.stride[0] * (RA_D * esz), l16, row);
             if (a.codes[which - 1] && there[1]) {
+                float v[8];
+                kv_floats<DT>(row, v);
                 const uint64_t row4 = head4 + (uint64_t)(uint32_t)h * (uint32_t)a.stride[1];
                 kv_store4(a.codes[which - 1] + row4 * Q4_ROW, a.scale[which - 1] + row4 * Q4_BLOCKS, l16, lane, v);
             }
@@ -282,7 +285,7 @@ __global__ __launch_bounds__(KV_THREADS) void dequantize_kv4_kernel(const uint8_
         if (t >= T) continue;
         float v[8];
         q4_values(there[u] ? c[u] : 0u, q4_unit(there[u] ? b[u] : 127u), v);
-        kv_store8<DT>(reinterpret_cast<char*>(X) + (head * T + t) * RA_D * (DT == RA_BF16 ? 2 : 4), l16, v);
+        kv_store8<DT>(reinterpret_cast<char*>(X) + (head * T + t) * RA_D * (DT == RA_BF16 ? 2 : 4), l16, kv_pack<DT>(v));
     }
 }
 
