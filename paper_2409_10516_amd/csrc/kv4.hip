@@ -121,12 +121,12 @@ __device__ __forceinline__ void turn(float (&v)[8], const float2 (&cs)[8], bool 
 }
 
 // A workgroup takes a token, or with few tokens, one of `split` parts of its heads: the sines and cosines of the token's angles, one
-// per lane of its first wavefront, then the heads' rows, one per 16 lanes. What bounds it is how many rows are on their way, and
-// that tokens side by side are written together: registers for eight wavefronts per SIMD, and nothing asked for ahead.
-// A 32K prompt of 32 + 8 + 8 heads, 192 us (4.2 TB/s): with four tokens per workgroup, their factors and the weights in registers, and one
-// row asked for ahead 303; with the first rows asked for before the angles are worked on 250; with three rows on their way 222; with 16 heads, 32
-// or all of a token in a workgroup of 256, 512 or 768 threads, so that it has fewer turns, 281, 249, 298; with 8 heads at a time 200. Workgroups that go
-// through the rows of several tokens, so that their last turn is full: 8 + 8 + 8 heads 130 -> 148, 6 + 2 + 2 43 -> 48.
+// per lane of its first wavefront, then the heads' rows, one per 16 lanes. What bounds it is how many rows are on their way, hence
+// registers for eight wavefronts per SIMD and nothing asked for ahead, and next the vector instructions of a row.
+// A 32K prompt of 32 + 8 + 8 normed heads, 150 us (5.4 TB/s; without norm and rotation 145). Held to seven wavefronts, six, five or four
+// 206, 223, 248, 283 of then 192; that 192 had a branch and a wait for shared memory per rotated value, with a branch around
+// both sides of a rotation it was 165. Two, four, eight or 16 tokens side by side in a workgroup 197, 200, 200, 205 of 192. With 512
+// threads 211, 768 273 (a turn that is not full is a longer one).
 template <int DT, int THREADS>
 __global__ __launch_bounds__(THREADS, 8) void append_kernel(AppendArgs a, int split) {
     __shared__ float2 s_cs[RA_D / 2];
@@ -215,12 +215,16 @@ ra_status ra_launch_append(const AppendArgs& a, ra_dtype dt, hipStream_t st) {
     const int64_t blocks = tokens * split;
     if (blocks > (1 << 24) - 1) RA_FAIL(RA_EUNSUP, "too many heads for one launch");
 #define KV_GO_T(DTV, THREADS) hipLaunchKernelGGL((append_kernel<DTV, THREADS>), dim3((unsigned)blocks), dim3(THREADS), 0, st, a, split)
-    // (tokens of few rows: 100000 of 1 + 1 + 1 heads 127 us with 256 threads, 82 with 64; 5000 of 4 + 1 + 1 12.1 and with 128 10.5)
-#define KV_GO(DTV)                                  \
-    do {                                            \
-        if (heads <= 4) KV_GO_T(DTV, 64);           \
-        else if (heads <= 8) KV_GO_T(DTV, 128);     \
-        else KV_GO_T(DTV, KV_THREADS);              \
+    // Tokens of little data want small workgroups, which wait for less at a time, where there are enough of them to fill the part (us
+    // with 64, 128 and 256 threads, bfloat16: 20000 of 6 + 2 + 2 heads 30, 35, 45; 16384 of 16 + 2 + 2 36, 39, 47; 32768 of 28 + 4 + 4
+    // 123, 113, 125; 16384 of 64 + 8 + 8 135, 129, 122; float32, 16384 of 8 + 8 + 8 93, 90, 85; 2500 of 16 + 2 + 2 11.7, 10.8, 11.6;
+    // 1000 of 32 + 8 + 8 17.5, 11.5, 9.4, of 4 + 1 + 1 6.1, 5.0, 5.4).
+    const int64_t bytes = (int64_t)heads * RA_D * (dt == RA_BF16 ? 2 : 4);
+#define KV_GO(DTV)                                                                                    \
+    do {                                                                                              \
+        if (heads <= 4 || (tokens >= 8192 && bytes <= 6144)) KV_GO_T(DTV, 64);                        \
+        else if (heads <= 8 || (tokens >= 2048 && bytes <= 10240)) KV_GO_T(DTV, 128);                 \
+        else KV_GO_T(DTV, KV_THREADS);                                                                \
     } while (0)
     if (dt == RA_BF16) KV_GO(RA_BF16); else KV_GO(RA_F32);
 #undef KV_GO_T
