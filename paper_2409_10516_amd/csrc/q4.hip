@@ -829,7 +829,11 @@ static Q4Parts q4_parts(int n_seq, int n_q, int n_kv, int64_t n_static, int topk
     p.spanG = Q4_PART;
     while (p.spanG < topk && (int64_t)n_seq * n_q * ((topk + p.spanG - 1) / p.spanG) > 2048) p.spanG *= 2;
     p.nG = (topk + p.spanG - 1) / p.spanG;
-    int64_t most = 512 / ((int64_t)n_seq * n_kv * p.tiles);
+    // Of the static set so many that all workgroups are there at once, three per compute unit, where Omega's leave room for some (us, 16
+    // sequences of 32 + 8 heads, 8 static parts of 512 rows each in 128: 512 workgroups at most 18.4 float32, 14.7 bfloat16, the rest of 768 15.6
+    // and 14.5; where Omega leaves none, one part 26.5, up to 512 workgroups 23.4).
+    const int64_t jobs = (int64_t)n_seq * n_kv * p.tiles, rest = (768 - (int64_t)n_seq * n_q * p.nG) / jobs;
+    int64_t most = rest >= 1 && rest < 512 / jobs ? rest : 512 / jobs;
     if (most < 1) most = 1;
     int64_t nS = (n_static + Q4_PART - 1) / Q4_PART;
     if (nS > most) nS = most;
