@@ -300,6 +300,7 @@ __device__ __forceinline__ void q4_close(Q4Wave<DT, HEADS, TERMS>& s, Q4Lds& lds
 #define Q4_UNIT (Q4_WAVES * Q4_CHUNK)
 #define Q4_MOST_UNITS (1u << 21)    // times the workgroups, below 2^32
 #define Q4_LEAST_UNITS 2u           // units that are worth a workgroup
+#define Q4_MOST_WORKGROUPS 768      // three per compute unit
 // over the 64 lanes: the sum, in all of them, and the sums up to each
 __device__ __forceinline__ uint32_t q4_sum64(uint32_t x, int lane) {
     x += lane_xor32<1>(x, lane); x += lane_xor32<2>(x, lane); x += lane_xor32<4>(x, lane);
@@ -489,91 +490,93 @@ __device__ __forceinline__ Q4Records q4_records(const float* partials, size_t he
     return {partials + at * RA_D, reinterpret_cast<const float2*>(partials + heads * places * RA_D) + at, have};
 }
 
-// The records of a head, few of them. grid: x = head; a thread per dimension, eight records on their way at a time.
-__global__ __launch_bounds__(RA_D) void q4_full_merge_kernel(const float* __restrict__ partials, int n_seq, int n_q, int n_kv, int N,
-                                                             const int32_t* __restrict__ n_tokens, int tiles, int unit_log2, int heads,
-                                                             int grid, float* __restrict__ out, float* __restrict__ lse) {
-    const size_t head = blockIdx.x;
-    const int d = threadIdx.x;
-    const Q4Records x = q4_records(partials, head, n_seq, n_q, n_kv, N, n_tokens, tiles, unit_log2, heads, grid);
-    float M = -INFINITY, L = 0.f, A = 0.f;
-    constexpr int FLY = 8;
-    for (int i0 = 0; i0 < x.have; i0 += FLY) {
-        float m[FLY], l[FLY], a[FLY], mx = M;
-#pragma unroll
-        for (int u = 0; u < FLY; ++u) {
-            const int i = i0 + u < x.have ? i0 + u : x.have - 1;
-            const float2 ml = x.ml[i];
-            m[u] = ml.x;
-            l[u] = ml.y;
-            a[u] = x.sums[(size_t)i * RA_D + d];
-        }
-#pragma unroll
-        for (int u = 0; u < FLY; ++u) mx = fmaxf(mx, m[u]);
-        if (mx == -INFINITY) continue;
-        const float corr = __builtin_amdgcn_exp2f(M - mx);
-        A *= corr;
-        L *= corr;
-#pragma unroll
-        for (int u = 0; u < FLY; ++u) {
-            const float w = i0 + u < x.have ? __builtin_amdgcn_exp2f(m[u] - mx) : 0.f;
-            A = fmaf(a[u], w, A);
-            L = fmaf(l[u], w, L);
-        }
-        M = mx;
-    }
-    out[head * RA_D + d] = M > -INFINITY ? A / L : 0.f;
-    if (d == 0) lse[head] = M > -INFINITY ? M * Q4_LN2 + logf(L) : -INFINITY;
-}
-
-// The same for many. grid: x = a quarter of the dimensions of a head. 32 groups of threads take records in turn, all of which are
-// on their way before the weights are known.
-#define Q4_MERGE_THREADS 1024
-#define Q4_MERGE_DIMS 32
-#define Q4_MOST_WORKGROUPS 768      // three per compute unit, and the most records of a head
-__global__ __launch_bounds__(Q4_MERGE_THREADS) void q4_full_merge_many_kernel(const float* __restrict__ partials, int n_seq, int n_q,
-                                                                              int n_kv, int N, const int32_t* __restrict__ n_tokens,
-                                                                              int tiles, int unit_log2, int heads, int grid,
-                                                                              float* __restrict__ out, float* __restrict__ lse) {
-    constexpr int WAVES = Q4_MERGE_THREADS / RA_WAVE, SL = Q4_MERGE_THREADS / Q4_MERGE_DIMS, FLY = Q4_MOST_WORKGROUPS / SL;
-    static_assert(Q4_MOST_WORKGROUPS <= Q4_MERGE_THREADS, "a thread has the weight of a record");
-    __shared__ float s_w[Q4_MERGE_THREADS], s_m[WAVES], s_l[WAVES], s_a[SL][Q4_MERGE_DIMS];
-    const int tid = threadIdx.x, t = tid % Q4_MERGE_DIMS, slice = tid / Q4_MERGE_DIMS, lane = tid & 63;
-    const size_t head = blockIdx.x / (RA_D / Q4_MERGE_DIMS);
-    const int dim = blockIdx.x % (RA_D / Q4_MERGE_DIMS) * Q4_MERGE_DIMS + t;
+// What is combined: grid: x = DIMS dimensions of a head. One record or a few (of most heads, in a batch): a thread per dimension, all records on their
+// way at once. More: groups of DIMS threads take records in turn, the first of which are on their way before the weights are known.
+// Workgroups of 32 dimensions where few heads have many records each (131072 tokens of 8 KV heads: with 1024 threads 32.5 us a
+// call, 512 31.9, 256 32.0), else of all 128.
+#define Q4_MERGE_THREADS 512
+#define Q4_MERGE_FEW 16
+template <int DIMS>
+__global__ __launch_bounds__(Q4_MERGE_THREADS) void q4_full_merge_kernel(const float* __restrict__ partials, int n_seq, int n_q, int n_kv,
+                                                                         int N, const int32_t* __restrict__ n_tokens, int tiles,
+                                                                         int unit_log2, int heads, int grid, float* __restrict__ out,
+                                                                         float* __restrict__ lse) {
+    constexpr int WAVES = Q4_MERGE_THREADS / RA_WAVE, SL = Q4_MERGE_THREADS / DIMS, FLY = DIMS == RA_D ? 16 : 32;
+    constexpr int MOST = DIMS == RA_D ? Q4_MOST_WORKGROUPS : Q4_MOST_WORKGROUPS / 3 * 2;       // records of a head
+    constexpr int MINE = (MOST + Q4_MERGE_THREADS - 1) / Q4_MERGE_THREADS;                     // that a thread makes the weight of
+    __shared__ float s_w[MINE * Q4_MERGE_THREADS], s_m[WAVES], s_l[WAVES], s_a[SL][DIMS];
+    const int tid = threadIdx.x, t = tid % DIMS, slice = tid / DIMS, lane = tid & 63;
+    const size_t head = blockIdx.x / (RA_D / DIMS);
+    const int dim = blockIdx.x % (RA_D / DIMS) * DIMS + t;
     const Q4Records x = q4_records(partials, head, n_seq, n_q, n_kv, N, n_tokens, tiles, unit_log2, heads, grid);
     const int have = x.have;
-    float r[FLY];
+    float mx = -INFINITY, ll = 0.f, a = 0.f;
+    if (DIMS == RA_D && have <= Q4_MERGE_FEW) {
+        if (slice) return;
+        float m[Q4_MERGE_FEW], l[Q4_MERGE_FEW], r[Q4_MERGE_FEW];
 #pragma unroll
-    for (int u = 0; u < FLY; ++u) r[u] = slice + u * SL < have ? x.sums[(size_t)(slice + u * SL) * RA_D + dim] : 0.f;
-    const float2 ml = tid < have ? x.ml[tid] : make_float2(-INFINITY, 0.f);
-    const float m = ml.x, l = ml.y;
-    float mx = m;
+        for (int u = 0; u < Q4_MERGE_FEW; ++u) {
+            const bool is = u < have;
+            const float2 ml = is ? x.ml[u] : make_float2(-INFINITY, 0.f);
+            m[u] = ml.x;
+            l[u] = ml.y;
+            r[u] = is ? x.sums[(size_t)u * RA_D + dim] : 0.f;
+        }
 #pragma unroll
-    for (int d = 1; d < RA_WAVE; d <<= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
-    if (lane == 0) s_m[tid / RA_WAVE] = mx;
-    __syncthreads();
+        for (int u = 0; u < Q4_MERGE_FEW; ++u) mx = fmaxf(mx, m[u]);
+        const float base = mx > -INFINITY ? mx : 0.f;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) mx = fmaxf(mx, s_m[w]);
-    const float w = mx > -INFINITY ? __builtin_amdgcn_exp2f(m - mx) : 0.f;
-    s_w[tid] = w;
-    float ll = l * w;
+        for (int u = 0; u < Q4_MERGE_FEW; ++u) {
+            const float w = __builtin_amdgcn_exp2f(m[u] - base);
+            a = fmaf(r[u], w, a);
+            ll = fmaf(l[u], w, ll);
+        }
+    } else {
+        float r[FLY], m[MINE], l[MINE];
 #pragma unroll
-    for (int d = 1; d < RA_WAVE; d <<= 1) ll += __shfl_xor(ll, d);
-    if (lane == 0) s_l[tid / RA_WAVE] = ll;
-    __syncthreads();
-    float a = 0.f;
+        for (int u = 0; u < FLY; ++u) r[u] = slice + u * SL < have ? x.sums[(size_t)(slice + u * SL) * RA_D + dim] : 0.f;
 #pragma unroll
-    for (int u = 0; u < FLY; ++u)
-        if (slice + u * SL < have) a = fmaf(r[u], s_w[slice + u * SL], a);
-    s_a[slice][t] = a;
-    __syncthreads();
-    if (slice) return;
-    ll = 0.f;
+        for (int i = 0; i < MINE; ++i) {
+            const int rec = tid + i * Q4_MERGE_THREADS;
+            const float2 ml = rec < have ? x.ml[rec] : make_float2(-INFINITY, 0.f);
+            m[i] = ml.x;
+            l[i] = ml.y;
+            mx = fmaxf(mx, m[i]);
+        }
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) ll += s_l[w];
+        for (int d = 1; d < RA_WAVE; d <<= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
+        if (lane == 0) s_m[tid / RA_WAVE] = mx;
+        __syncthreads();
 #pragma unroll
-    for (int s = 1; s < SL; ++s) a += s_a[s][t];
+        for (int w = 0; w < WAVES; ++w) mx = fmaxf(mx, s_m[w]);
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) {
+            const float w = mx > -INFINITY ? __builtin_amdgcn_exp2f(m[i] - mx) : 0.f;
+            s_w[tid + i * Q4_MERGE_THREADS] = w;
+            ll = fmaf(l[i], w, ll);
+        }
+#pragma unroll
+        for (int d = 1; d < RA_WAVE; d <<= 1) ll += __shfl_xor(ll, d);
+        if (lane == 0) s_l[tid / RA_WAVE] = ll;
+        __syncthreads();
+        for (int first = slice;;) {
+#pragma unroll
+            for (int u = 0; u < FLY; ++u)
+                if (first + u * SL < have) a = fmaf(r[u], s_w[first + u * SL], a);
+            first += FLY * SL;
+            if (FLY * SL >= MOST || first - slice >= have) break;
+#pragma unroll
+            for (int u = 0; u < FLY; ++u) r[u] = first + u * SL < have ? x.sums[(size_t)(first + u * SL) * RA_D + dim] : 0.f;
+        }
+        s_a[slice][t] = a;
+        __syncthreads();
+        if (slice) return;
+        ll = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) ll += s_l[w];
+#pragma unroll
+        for (int i = 1; i < SL; ++i) a += s_a[i][t];
+    }
     out[head * RA_D + dim] = mx > -INFINITY ? a / ll : 0.f;
     if (dim == 0) lse[head] = mx > -INFINITY ? mx * Q4_LN2 + logf(ll) : -INFINITY;
 }
@@ -799,12 +802,12 @@ ra_status ra_launch_full_q4(const void* q, ra_dtype dt, const Q4Cache& c, int n_
 #undef Q4_GO
     RA_HIP(hipGetLastError());
     if (x.whole) return RA_OK;
-#define Q4_MERGE(KERNEL, GRID, THREADS)                                                                                                 \
-    hipLaunchKernelGGL(KERNEL, dim3(GRID), dim3(THREADS), 0, st, partials, n_seq, n_q, n_kv, (int)N, n_tokens, x.tiles, x.unit_log2,  \
-                       q4_heads(n_q / n_kv), x.workgroups, out, lse)
+#define Q4_MERGE(DIMS)                                                                                                                  \
+    hipLaunchKernelGGL((q4_full_merge_kernel<DIMS>), dim3(n_seq * n_q * (RA_D / DIMS)), dim3(Q4_MERGE_THREADS), 0, st, partials, n_seq, n_q, n_kv, \
+                       (int)N, n_tokens, x.tiles, x.unit_log2, q4_heads(n_q / n_kv), x.workgroups, out, lse)
     // records per head, were all sequences as long as the longest
-    if (x.workgroups / (n_seq * n_kv * x.tiles) <= Q4_FEW_RECORDS) Q4_MERGE(q4_full_merge_kernel, n_seq * n_q, RA_D);
-    else Q4_MERGE(q4_full_merge_many_kernel, n_seq * n_q * (RA_D / Q4_MERGE_DIMS), Q4_MERGE_THREADS);
+    if (x.workgroups / (n_seq * n_kv * x.tiles) <= Q4_FEW_RECORDS) Q4_MERGE(RA_D);
+    else Q4_MERGE(32);
 #undef Q4_MERGE
     RA_HIP(hipGetLastError());
     return RA_OK;
