@@ -129,6 +129,24 @@ def test_full_attention_of_many_sequences_heads_and_records(dtype, n_seq, n_q, n
             _check(out[s, h], lse[s, h], to_np(q[s, h]), K[0, g], V[0, g], np.arange(lens[s]), dtype)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n_seq,n_q,n_kv,N", [(20, 2, 1, 9000), (40, 17, 1, 40001), (10, 4, 2, 50000), (66, 4, 1, 200003)])
+def test_full_attention_of_one_long_sequence_in_a_batch(dtype, n_seq, n_q, n_kv, N):
+    """The long one's heads have nearly all the records there are: more than a thread per dimension, than the groups of a workgroup in
+    one go, and than a workgroup has threads; the others have one, or none."""
+    lens = np.full(n_seq, 200, np.int32)
+    lens[1], lens[2], lens[n_seq // 2] = 0, 1, N
+    k4, v4, K, V = _cache(1, n_kv, N, seed=N)
+    k4, v4 = (tuple(t.expand(n_seq, -1, -1, -1).contiguous() for t in x) for x in (k4, v4))
+    q = _queries(n_seq, n_q, dtype, N)
+    out, lse = ra.ra_full_attention_q4(q.to(DEV), k4, v4, torch.from_numpy(lens).to(DEV))
+    out, lse = out.cpu().numpy(), lse.cpu().numpy()
+    for s in (0, 1, 2, n_seq // 2, n_seq - 1):
+        for h in sorted({0, n_q // 2, n_q - 1}):
+            g = h // (n_q // n_kv)
+            _check(out[s, h], lse[s, h], to_np(q[s, h]), K[0, g], V[0, g], np.arange(lens[s]), dtype)
+
+
 def test_a_capacity_of_hundreds_of_millions():
     """The list of rows is counted in larger units then; most of the capacity is not used."""
     cap, T = 300_000_000, 6001
