@@ -490,21 +490,21 @@ __device__ __forceinline__ Q4Records q4_records(const float* partials, size_t he
     return {partials + at * RA_D, reinterpret_cast<const float2*>(partials + heads * places * RA_D) + at, have};
 }
 
-// What is combined: grid: x = DIMS dimensions of a head. One record or a few (of most heads, in a batch): a thread per dimension, all records on their
-// way at once. More: groups of DIMS threads take records in turn, the first of which are on their way before the weights are known.
+// What is combined: grid: x = DIMS dimensions of a head. One record or a few (of most heads, in a batch): a thread per dimension, all records
+// on their way at once. More: groups of DIMS threads take records in turn, the first of which are on their way before the weights are known.
 // Workgroups of 32 dimensions where few heads have many records each (131072 tokens of 8 KV heads: with 1024 threads 32.5 us a
-// call, 512 31.9, 256 32.0), else of all 128.
-#define Q4_MERGE_THREADS 512
+// call, 512 31.9, 256 32.0), else of all 128: of 512 threads, for a batch's one long sequence (32 of one KV head, one of 262144 tokens and the
+// others 500: with 128 threads 61 us, 512 32), and where the heads are many, of 128 (1024 jobs of 2500 rows: with 512 threads 69, 128 61).
 #define Q4_MERGE_FEW 16
-template <int DIMS>
-__global__ __launch_bounds__(Q4_MERGE_THREADS) void q4_full_merge_kernel(const float* __restrict__ partials, int n_seq, int n_q, int n_kv,
+template <int THREADS, int DIMS>
+__global__ __launch_bounds__(THREADS) void q4_full_merge_kernel(const float* __restrict__ partials, int n_seq, int n_q, int n_kv,
                                                                          int N, const int32_t* __restrict__ n_tokens, int tiles,
                                                                          int unit_log2, int heads, int grid, float* __restrict__ out,
                                                                          float* __restrict__ lse) {
-    constexpr int WAVES = Q4_MERGE_THREADS / RA_WAVE, SL = Q4_MERGE_THREADS / DIMS, FLY = DIMS == RA_D ? 16 : 32;
+    constexpr int WAVES = THREADS / RA_WAVE, SL = THREADS / DIMS, FLY = DIMS == RA_D ? 16 : 32;
     constexpr int MOST = DIMS == RA_D ? Q4_MOST_WORKGROUPS : Q4_MOST_WORKGROUPS / 3 * 2;       // records of a head
-    constexpr int MINE = (MOST + Q4_MERGE_THREADS - 1) / Q4_MERGE_THREADS;                     // that a thread makes the weight of
-    __shared__ float s_w[MINE * Q4_MERGE_THREADS], s_m[WAVES], s_l[WAVES], s_a[SL][DIMS];
+    constexpr int MINE = (MOST + THREADS - 1) / THREADS;                     // that a thread makes the weight of
+    __shared__ float s_w[MINE * THREADS], s_m[WAVES], s_l[WAVES], s_a[SL][DIMS];
     const int tid = threadIdx.x, t = tid % DIMS, slice = tid / DIMS, lane = tid & 63;
     const size_t head = blockIdx.x / (RA_D / DIMS);
     const int dim = blockIdx.x % (RA_D / DIMS) * DIMS + t;
@@ -537,7 +537,7 @@ __global__ __launch_bounds__(Q4_MERGE_THREADS) void q4_full_merge_kernel(const f
         for (int u = 0; u < FLY; ++u) r[u] = slice + u * SL < have ? x.sums[(size_t)(slice + u * SL) * RA_D + dim] : 0.f;
 #pragma unroll
         for (int i = 0; i < MINE; ++i) {
-            const int rec = tid + i * Q4_MERGE_THREADS;
+            const int rec = tid + i * THREADS;
             const float2 ml = rec < have ? x.ml[rec] : make_float2(-INFINITY, 0.f);
             m[i] = ml.x;
             l[i] = ml.y;
@@ -552,7 +552,7 @@ __global__ __launch_bounds__(Q4_MERGE_THREADS) void q4_full_merge_kernel(const f
 #pragma unroll
         for (int i = 0; i < MINE; ++i) {
             const float w = mx > -INFINITY ? __builtin_amdgcn_exp2f(m[i] - mx) : 0.f;
-            s_w[tid + i * Q4_MERGE_THREADS] = w;
+            s_w[tid + i * THREADS] = w;
             ll = fmaf(l[i], w, ll);
         }
 #pragma unroll
@@ -759,9 +759,11 @@ static int q4_heads(int group) { return group <= 4 ? 4 : group <= 8 ? 8 : 16; }
         else GO(DTV, 16);                               \
     } while (0)
 
-// How a call is cut: tiles of query heads per KV head, workgroups, and whether each has a job of its own. That is so where the jobs are
-// many, or a head's rows few: shared out, 512 rows of 8 jobs take 8.7 us and by themselves 6.9, 1000 rows 8.9 and 9.5 (and a launch
-// less on the host's side), 2000 rows 8.9 and 14.0; 128 jobs of 1000 rows 12.8 and 10.4, of 2000 16.8 and 15.4, of 4000 21.7 and 24.3.
+// How a call is cut: tiles of query heads per KV head, workgroups, and whether each has a job of its own. That is so where a head's rows are
+// few or the jobs many: shared out, 512 rows of 8 jobs take 8.7 us and by themselves 6.9, 1000 rows 8.9 and 9.5 (and a launch less on the host's
+// side), 2000 rows 8.9 and 14.0; 128 jobs of 2000 rows 16.8 and 15.4, of 4000 21.7 and 24.3; 512 of 8000 79 and 75, of 0 to 8000 70 and 54, one
+// of 8000 and 504 of 200 17 and 46; 1024 of 16000 288 and 275, of 0 to 16000 189 and 160; 2048 of 20000 711 and 655. A job of its own costs what
+// the longest takes alone, 5 ns a row, hence the limit however many there are.
 // Otherwise three workgroups of bfloat16 fit a compute unit, two of float32; where few jobs share them, two leave fewer records to
 // combine (us, two and three: 8 jobs of 131072 rows 37.1, 38.0, one of a million 39.4, 40.5, 64 of 20011 33.9, 34.3, 128 of up to
 // 32768 64.2, 62.6).
@@ -772,7 +774,7 @@ static Q4Cut q4_cut(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N) {
     const int heads = q4_heads(n_q / n_kv);
     x.tiles = (n_q / n_kv + heads - 1) / heads;
     const int64_t jobs = (int64_t)n_seq * n_kv * x.tiles;
-    x.whole = (jobs >= 2048 && N <= Q4_MOST_ROWS) || N <= (jobs >= 128 ? 2048 : 1024);
+    x.whole = N <= 1024 || N <= (jobs < 2048 ? 16 * jobs : 32768) || (jobs > Q4_MOST_UNITS && N <= Q4_MOST_ROWS);
     x.unit_log2 = 7;
     static_assert(Q4_UNIT == 1 << 7, "rows of a unit");
     auto units = [&] { return jobs * ((N + ((int64_t)1 << x.unit_log2) - 1) >> x.unit_log2); };
@@ -802,12 +804,13 @@ ra_status ra_launch_full_q4(const void* q, ra_dtype dt, const Q4Cache& c, int n_
 #undef Q4_GO
     RA_HIP(hipGetLastError());
     if (x.whole) return RA_OK;
-#define Q4_MERGE(DIMS)                                                                                                                  \
-    hipLaunchKernelGGL((q4_full_merge_kernel<DIMS>), dim3(n_seq * n_q * (RA_D / DIMS)), dim3(Q4_MERGE_THREADS), 0, st, partials, n_seq, n_q, n_kv, \
+#define Q4_MERGE(THREADS, DIMS)                                                                                                                  \
+    hipLaunchKernelGGL((q4_full_merge_kernel<THREADS, DIMS>), dim3(n_seq * n_q * (RA_D / DIMS)), dim3(THREADS), 0, st, partials, n_seq, n_q, n_kv, \
                        (int)N, n_tokens, x.tiles, x.unit_log2, q4_heads(n_q / n_kv), x.workgroups, out, lse)
     // records per head, were all sequences as long as the longest
-    if (x.workgroups / (n_seq * n_kv * x.tiles) <= Q4_FEW_RECORDS) Q4_MERGE(RA_D);
-    else Q4_MERGE(32);
+    if (x.workgroups / (n_seq * n_kv * x.tiles) > Q4_FEW_RECORDS) Q4_MERGE(512, 32);
+    else if ((int64_t)n_seq * n_q <= 1024) Q4_MERGE(512, RA_D);
+    else Q4_MERGE(128, RA_D);
 #undef Q4_MERGE
     RA_HIP(hipGetLastError());
     return RA_OK;
