@@ -289,3 +289,50 @@ def test_rows_behind_the_last_token_are_zero_on_another_stream():
     got = ra.ra_append_tokens(x, None, None, None, n_new=n_new, stream=side)
     torch.cuda.synchronize()
     assert torch.equal(got, ref) and (got[1, :, 4:] == 0).all() and torch.equal(got[1, :, :4], x[1, :4].transpose(0, 1))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n_q,n_kv,T,rot,inter", [(1, 1, 9001, 128, False), (6, 2, 8209, 64, True), (16, 2, 8200, 128, True), (28, 4, 2100, 96, False),
+                                                 (32, 8, 2049, 128, False), (5, 5, 2500, 16, False), (64, 8, 300, 64, False)])
+def test_append_of_many_tokens(dtype, n_q, n_kv, T, rot, inter):
+    """As many tokens as change the workgroups' size: every copied row, and normed and rotated rows of some tokens."""
+    g = torch.Generator(device=DEV).manual_seed(T)
+    heads = n_q + 2 * n_kv
+    x = torch.randn((2, T, heads, 128), generator=g, device=DEV).to(dtype)
+    q, k, v = x.split((n_q, n_kv, n_kv), dim=2)
+    w = [(1 + 0.3 * torch.randn(128, generator=g, device=DEV)).to(dtype) for _ in range(2)]
+    f = _inv_freq(rot)
+    first, n_new = [5, 0], [T, T - 37]
+    dev = lambda a: torch.tensor(a, dtype=torch.int32, device=DEV)  # noqa: E731
+    K, V = (torch.full((2, n_kv, T + 9, 128), 3.0, dtype=dtype, device=DEV) for _ in range(2))
+    k4 = (torch.full((2, n_kv, T + 9, 64), 7, dtype=torch.uint8, device=DEV), torch.full((2, n_kv, T + 9, 4), 7, dtype=torch.uint8, device=DEV))
+    out = ra.ra_append_tokens(q, k, v, dev(first), n_new=dev(n_new), q_weight=w[0], k_weight=w[1], inv_freq=torch.from_numpy(f).to(DEV),
+                              interleaved=inter, K=K, V=V, k4=k4)
+    for s in range(2):
+        a, n = first[s], n_new[s]
+        assert torch.equal(V[s, :, a:a + n], v[s, :n].transpose(0, 1))
+        for c in (K, V):
+            assert (c[s, :, :a] == 3.0).all() and (c[s, :, a + n:] == 3.0).all()
+        assert (out[s, :, n:] == 0).all()
+        whole = ra.ra_quantize_kv4(K[s:s + 1, :, a:a + n].contiguous())
+        assert all(torch.equal(c[s, :, a:a + n], e[0]) for c, e in zip(k4, whole))
+        assert all((c[s, :, :a] == 7).all() and (c[s, :, a + n:] == 7).all() for c in k4)
+        some = np.unique(np.concatenate([[0, 1, n - 1], np.random.default_rng(T).integers(0, n, 13)]))
+        for rows, got, weight in ((q, out[s][:, some], w[0]), (k, K[s][:, a + some], w[1])):
+            ref, size = OK.head_rows(_np(rows[s, some]), a + some, _np(weight), 1e-6, f, inter)
+            _row_close(_np(got).transpose(1, 0, 2), ref, size, dtype)
+
+
+def test_rows_past_four_gigabytes():
+    """The second head's rows start 5 GB into the caches and 4.6 GB into q_out."""
+    cap, T = 20_000_000, 140_000
+    g = torch.Generator(device=DEV).manual_seed(3)
+    K, V = (torch.empty((1, 2, cap, 128), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    k, v = (torch.randn((1, 40, 2, 128), generator=g, device=DEV).to(torch.bfloat16) for _ in range(2))
+    end = torch.tensor([cap - 40], dtype=torch.int32, device=DEV)
+    ra.ra_append_tokens(None, k, v, end, K=K, V=V)
+    assert torch.equal(K[0, :, cap - 40:], k[0].transpose(0, 1)) and torch.equal(V[0, :, cap - 40:], v[0].transpose(0, 1))
+    del K, V
+    q = torch.randint(-999, 999, (1, T, 130, 128), generator=g, device=DEV, dtype=torch.int16).to(torch.bfloat16)
+    out = ra.ra_append_tokens(q, None, None, None)
+    assert torch.equal(out[0], q[0].transpose(0, 1))

@@ -106,7 +106,7 @@ def test_full_attention_of_any_length(dtype, N):
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("n_seq,n_q,n_kv,N", [(130, 4, 1, 700), (67, 1, 1, 300), (2100, 1, 1, 300), (1030, 2, 2, 257), (2, 40, 1, 3000), (1, 2, 1, 20001),
-                                             (1, 17, 1, 40000), (3, 3, 1, 9999)])
+                                             (1, 17, 1, 40000), (3, 3, 1, 9999), (300, 8, 4, 2500), (2060, 1, 1, 33001)])
 def test_full_attention_of_many_sequences_heads_and_records(dtype, n_seq, n_q, n_kv, N):
     """More sequences than lanes, more jobs than are cut, tiles of heads, more records of a head than one thread per dimension
     combines; lengths of zero, one and anything, some of them in a row."""
