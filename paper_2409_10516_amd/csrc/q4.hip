@@ -636,56 +636,63 @@ __device__ __forceinline__ float q4_load(const float* p) {
     return COHERENT ? __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : *p;
 }
 
-// Dimension d of a head from its records, nS of the static set and nG of Omega: Eq. 4 for each, Eq. 5 for both.
+// Dimension d of a head's records [first, last), every `by`th: their maximum, sum of weights and weighted sum.
+struct Q4Sum { float m, l, a; };
 template <bool COHERENT>
-__device__ __forceinline__ void q4_finish(const float* rec, int nS, int nG, size_t head, int d, const Q4Out& o) {
-    float M[2] = {-INFINITY, -INFINITY}, L[2] = {0.f, 0.f}, A[2] = {0.f, 0.f};
+__device__ __forceinline__ Q4Sum q4_add_up(const float* rec, int first, int last, int by, int d) {
     constexpr int FLY = 8;
+    Q4Sum x{-INFINITY, 0.f, 0.f};
+    for (int i0 = first; i0 < last; i0 += FLY * by) {
+        float m[FLY], l[FLY], a[FLY], mx = x.m;
 #pragma unroll
-    for (int set = 0; set < 2; ++set) {
-        const int first = set ? nS : 0, last = set ? nS + nG : nS;
-        for (int i0 = first; i0 < last; i0 += FLY) {
-            float m[FLY], l[FLY], a[FLY];
-#pragma unroll
-            for (int u = 0; u < FLY; ++u) {
-                const float* x = rec + (size_t)(i0 + u < last ? i0 + u : last - 1) * Q4_REC;
-                m[u] = q4_load<COHERENT>(x + RA_D);
-                l[u] = q4_load<COHERENT>(x + RA_D + 1);
-                a[u] = q4_load<COHERENT>(x + d);
-            }
-            float mx = M[set];
-#pragma unroll
-            for (int u = 0; u < FLY; ++u) mx = fmaxf(mx, m[u]);
-            if (mx == -INFINITY) continue;
-            const float corr = __builtin_amdgcn_exp2f(M[set] - mx);
-            A[set] *= corr;
-            L[set] *= corr;
-#pragma unroll
-            for (int u = 0; u < FLY; ++u) {
-                const float w = i0 + u < last ? __builtin_amdgcn_exp2f(m[u] - mx) : 0.f;
-                A[set] = fmaf(a[u], w, A[set]);
-                L[set] = fmaf(l[u], w, L[set]);
-            }
-            M[set] = mx;
+        for (int u = 0; u < FLY; ++u) {
+            const float* y = rec + (size_t)(i0 + u * by < last ? i0 + u * by : i0) * Q4_REC;
+            m[u] = q4_load<COHERENT>(y + RA_D);
+            l[u] = q4_load<COHERENT>(y + RA_D + 1);
+            a[u] = q4_load<COHERENT>(y + d);
         }
+#pragma unroll
+        for (int u = 0; u < FLY; ++u) mx = fmaxf(mx, m[u]);
+        if (mx == -INFINITY) continue;
+        const float corr = __builtin_amdgcn_exp2f(x.m - mx);
+        x.a *= corr;
+        x.l *= corr;
+#pragma unroll
+        for (int u = 0; u < FLY; ++u) {
+            const float w = i0 + u * by < last ? __builtin_amdgcn_exp2f(m[u] - mx) : 0.f;
+            x.a = fmaf(a[u], w, x.a);
+            x.l = fmaf(l[u], w, x.l);
+        }
+        x.m = mx;
     }
+    return x;
+}
+// Eq. 4 for the static set and for Omega, Eq. 5 for both
+__device__ __forceinline__ void q4_write(const Q4Sum (&set)[2], size_t head, int d, const Q4Out& o) {
     float* o_set[2] = {o.o_w, o.o_om};
     float* l_set[2] = {o.lse_w, o.lse_om};
 #pragma unroll
-    for (int set = 0; set < 2; ++set) {
-        const bool empty = M[set] == -INFINITY;
-        if (o_set[set]) o_set[set][head * RA_D + d] = empty ? 0.f : A[set] / L[set];
-        if (l_set[set] && d == 0) l_set[set][head] = empty ? -INFINITY : M[set] * Q4_LN2 + logf(L[set]);
+    for (int i = 0; i < 2; ++i) {
+        const bool empty = set[i].m == -INFINITY;
+        if (o_set[i]) o_set[i][head * RA_D + d] = empty ? 0.f : set[i].a / set[i].l;
+        if (l_set[i] && d == 0) l_set[i][head] = empty ? -INFINITY : set[i].m * Q4_LN2 + logf(set[i].l);
     }
-    const float mx = fmaxf(M[0], M[1]);
+    const float mx = fmaxf(set[0].m, set[1].m);
     float out = 0.f, lse = -INFINITY;
     if (mx > -INFINITY) {
-        const float e0 = __builtin_amdgcn_exp2f(M[0] - mx), e1 = __builtin_amdgcn_exp2f(M[1] - mx), l = L[0] * e0 + L[1] * e1;
-        out = (A[0] * e0 + A[1] * e1) / l;
+        const float e0 = __builtin_amdgcn_exp2f(set[0].m - mx), e1 = __builtin_amdgcn_exp2f(set[1].m - mx);
+        const float l = set[0].l * e0 + set[1].l * e1;
+        out = (set[0].a * e0 + set[1].a * e1) / l;
         lse = mx * Q4_LN2 + logf(l);
     }
     o.out[head * RA_D + d] = out;
     if (d == 0) o.lse[head] = lse;
+}
+// dimension d of a head from its records, nS of the static set and nG of Omega
+template <bool COHERENT>
+__device__ __forceinline__ void q4_finish(const float* rec, int nS, int nG, size_t head, int d, const Q4Out& o) {
+    const Q4Sum set[2] = {q4_add_up<COHERENT>(rec, 0, nS, 1, d), q4_add_up<COHERENT>(rec, nS, nS + nG, 1, d)};
+    q4_write(set, head, d, o);
 }
 
 // grid: per (sequence, KV head) the parts of each of its query heads' Omega (their loads wait for ids, so they start first), then
@@ -713,16 +720,36 @@ __global__ __launch_bounds__(Q4_THREADS, 3) void q4_attend_kernel(const void* __
     const int span = om ? spanG : spanS, from = part * span, to = from + span < src.count ? from + span : src.count;
     Q4Wave<DT, HEADS, 3> st;
     st.start(reinterpret_cast<const char*>(q) + head0 * RA_D * (DT == RA_BF16 ? 2 : 4), heads, lane);
-    for (int at = from + wv * Q4_CHUNK; at < to; at += Q4_WAVES * Q4_CHUNK) {
-        Q4Chunk ch;
-        uint32_t there = 255u;
-        if (!om && at >= s && at + Q4_CHUNK <= to) {         // (rows side by side)
+    // Whole chunks of W's rows behind the sink lie side by side, [lo, hi) in steps, and are read as over all tokens, the next one always on
+    // its way; then all others (us, one sequence of 32 + 8 heads with 8644, 30644 and 100644 static rows 15.0, 19.9, 36 without, 11.4, 14.6, 28).
+    const int step = Q4_WAVES * Q4_CHUNK, mine = from + wv * Q4_CHUNK;
+    int lo = mine, hi = mine;
+    if (!om) {
+        if (lo < s) lo += ((int)s - lo + step - 1) / step * step;
+        hi = lo;
+        if (lo + Q4_CHUNK <= to) {
+            Q4Chunk a, b;
             Q4Stream rd;
-            rd.start(h, w - s + at, Q4_CHUNK, lane);
-            rd.fetch(ch, 0);
-        } else {
-            there = q4_gather(ch, h, src, at, lane);
+            const int last = (to - Q4_CHUNK - lo) / step * step;
+            rd.start(h, w - s + lo, last + Q4_CHUNK, lane);
+            hi = lo + last + step;
+            int row = 0;
+            rd.fetch(a, 0);
+            while (true) {
+                rd.fetch(b, row + step < last ? row + step : last);
+                st.template add<true>(a, 255u, lane);
+                row += step;
+                if (row > last) break;
+                rd.fetch(a, row + step < last ? row + step : last);
+                st.template add<true>(b, 255u, lane);
+                row += step;
+                if (row > last) break;
+            }
         }
+    }
+    for (int at = mine == lo ? hi : mine; at < to; at = at + step == lo ? hi : at + step) {
+        Q4Chunk ch;
+        const uint32_t there = q4_gather(ch, h, src, at, lane);
         st.template add<false>(ch, there, lane);
     }
     q4_close(st, lds, heads, tid, [&](int hd, int d, float sum, float mx, float l) {
@@ -743,10 +770,37 @@ __global__ __launch_bounds__(Q4_THREADS, 3) void q4_attend_kernel(const void* __
     }
 }
 
-// grid: x = head (with its sequence)
-__global__ __launch_bounds__(RA_D) void q4_merge_kernel(const float* __restrict__ partials, int nS, int nG, Q4Out o) {
+// grid: x = head (with its sequence); SLICES threads per dimension take the records in turn
+template <int SLICES>
+__global__ __launch_bounds__(RA_D * SLICES) void q4_merge_kernel(const float* __restrict__ partials, int nS, int nG, Q4Out o) {
     const size_t head = blockIdx.x;
-    q4_finish<false>(partials + head * (nS + nG) * Q4_REC, nS, nG, head, threadIdx.x, o);
+    const float* rec = partials + head * (nS + nG) * Q4_REC;
+    const int d = threadIdx.x % RA_D, slice = threadIdx.x / RA_D;
+    if constexpr (SLICES == 1) {
+        q4_finish<false>(rec, nS, nG, head, d, o);
+    } else {
+        __shared__ Q4Sum s_part[SLICES][2][RA_D];
+        s_part[slice][0][d] = q4_add_up<false>(rec, slice, nS, SLICES, d);
+        s_part[slice][1][d] = q4_add_up<false>(rec, nS + slice, nS + nG, SLICES, d);
+        __syncthreads();
+        if (slice) return;
+        Q4Sum set[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            Q4Sum x{-INFINITY, 0.f, 0.f};
+#pragma unroll
+            for (int y = 0; y < SLICES; ++y) x.m = fmaxf(x.m, s_part[y][i][d].m);
+            const float base = x.m > -INFINITY ? x.m : 0.f;
+#pragma unroll
+            for (int y = 0; y < SLICES; ++y) {
+                const float w = __builtin_amdgcn_exp2f(s_part[y][i][d].m - base);
+                x.a = fmaf(s_part[y][i][d].a, w, x.a);
+                x.l = fmaf(s_part[y][i][d].l, w, x.l);
+            }
+            set[i] = x;
+        }
+        q4_write(set, head, d, o);
+    }
 }
 
 // query heads of a tile (columns of the matrix instructions)
@@ -843,7 +897,7 @@ static Q4Parts q4_parts(int n_seq, int n_q, int n_kv, int64_t n_static, int topk
     if (most < 1) most = 1;
     int64_t nS = (n_static + Q4_PART - 1) / Q4_PART;
     if (nS > most) nS = most;
-    if (nS < 1) nS = n_static > 0;
+    if (nS < (n_static + Q4_MOST_ROWS - 1) / Q4_MOST_ROWS) nS = (n_static + Q4_MOST_ROWS - 1) / Q4_MOST_ROWS;
     p.spanS = nS ? (int)((n_static + nS - 1) / nS + Q4_PART - 1) / Q4_PART * Q4_PART : Q4_PART;
     p.nS = (int)((n_static + p.spanS - 1) / p.spanS);
     return p;
@@ -876,7 +930,10 @@ ra_status ra_launch_attend_q4(const void* q, ra_dtype dt, const Q4Cache& c, int 
 #undef Q4_GO
     RA_HIP(hipGetLastError());
     if (tickets) return RA_OK;
-    hipLaunchKernelGGL(q4_merge_kernel, dim3(n_seq * n_q), dim3(RA_D), 0, st, partials, p.nS, p.nG, o);
+    // (eight records are on their way at a time. 16 heads of one KV head, 100640 static rows in 394 records: 44 us with one thread per
+    // dimension, 19 with eight; 24 records 26.7 and 27.3)
+    if ((p.nS + 7) / 8 + (p.nG + 7) / 8 <= 3) hipLaunchKernelGGL(q4_merge_kernel<1>, dim3(n_seq * n_q), dim3(RA_D), 0, st, partials, p.nS, p.nG, o);
+    else hipLaunchKernelGGL(q4_merge_kernel<8>, dim3(n_seq * n_q), dim3(RA_D * 8), 0, st, partials, p.nS, p.nG, o);
     RA_HIP(hipGetLastError());
     return RA_OK;
 }

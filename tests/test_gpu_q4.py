@@ -252,6 +252,13 @@ ATTEND = [
     (1, 5, 1, 1500, 1500, 1500, 0, 0, 200),       # nothing static
     (4, 16, 2, 260, 200, 264, 1, 31, 64),
     (1, 20, 1, 4000, 4000, 4000, 128, 1400, 300),
+    # long static sets: several chunks of a wavefront side by side, sinks that end inside one, many records of a head, one record
+    (1, 16, 1, 40001, 3001, 40003, 4, 640, 100),
+    (2, 8, 2, 9001, 2000, 9001, 4, 500, 40),
+    (5, 20, 2, 5003, 900, 5003, 700, 31, 64),
+    (1, 4, 1, 20011, 500, 20011, 333, 17, 9),
+    (40, 16, 2, 2100, 300, 2100, 3, 20, 50),
+    (30, 32, 1, 700, 300, 700, 5, 20, 40),
 ]
 
 
