@@ -7,16 +7,23 @@
 #define KV_THREADS 256
 #define KV_GROUPS (KV_THREADS / 16)
 
-// values [8 l16, 8 l16 + 8) of a row, as loaded. Rows are read once and written once: non-temporal both ways (131072 rows of 8 heads
-// into 4 bits and back 131 -> 119 us with such loads, 112 with such stores; a 32K prompt's rows 196 -> 194, 191).
+// values [8 l16, 8 l16 + 8) of a row, as loaded. Rows are written once: non-temporal (131072 rows of 8 heads into 4 bits and back 116 -> 107 us,
+// a 32K prompt's rows 159 -> 154, 2000 tokens 15.1 -> 13.5). They are read once, too, but what a call reads has just been made, and up to a
+// quarter of what the memory side keeps is taken from there (us, with ONCE and without (which as a choice at run time costs the large ones 3 %): 5105 tokens of 10 float32 heads, 26 MB, 15.5, 13.5, 32768 rows of 8
+// heads, 64 MB, 30.9, 28.2, a 32K prompt 154, 157, 8000 tokens, 98 MB, 42.5, 44.8).
+#define KV_KEPT (1 << 26)           // bytes read
 typedef uint32_t kv_u32x4 __attribute__((ext_vector_type(4)));
 template <int DT> struct KvRaw { kv_u32x4 a[DT == RA_BF16 ? 1 : 2]; };
-template <int DT>
+template <int DT, bool ONCE>
 __device__ __forceinline__ KvRaw<DT> kv_load8(const void* row, int l16) {
     constexpr int W = DT == RA_BF16 ? 1 : 2;
+    const kv_u32x4* from = reinterpret_cast<const kv_u32x4*>(row) + W * l16;
     KvRaw<DT> x;
 #pragma unroll
-    for (int i = 0; i < W; ++i) x.a[i] = __builtin_nontemporal_load(reinterpret_cast<const kv_u32x4*>(row) + W * l16 + i);
+    for (int i = 0; i < W; ++i) {
+        if constexpr (ONCE) x.a[i] = __builtin_nontemporal_load(from + i);
+        else x.a[i] = from[i];
+    }
     return x;
 }
 template <int DT>
@@ -127,7 +134,7 @@ __device__ __forceinline__ void turn(float (&v)[8], const float2 (&cs)[8], bool 
 // 206, 223, 248, 283 of then 192; that 192 had a branch and a wait for shared memory per rotated value, with a branch around
 // both sides of a rotation it was 165. Two, four, eight or 16 tokens side by side in a workgroup 197, 200, 200, 205 of 192. With 512
 // threads 211, 768 273 (a turn that is not full is a longer one).
-template <int DT, int THREADS>
+template <int DT, int THREADS, bool ONCE>
 __global__ __launch_bounds__(THREADS, 8) void append_kernel(AppendArgs a, int split) {
     __shared__ float2 s_cs[RA_D / 2];
     __shared__ float4 s_w[2][RA_D / 4];
@@ -169,7 +176,7 @@ __global__ __launch_bounds__(THREADS, 8) void append_kernel(AppendArgs a, int sp
         const int h = which == 0 ? r : which == 1 ? r - a.n_q : r - a.n_q - a.n_kv;
         const char* in = which == 0 ? in_q : which == 1 ? in_k : in_v;
         if (!in || (which && !there[0] && !there[1])) continue;
-        KvRaw<DT> row = kv_load8<DT>(in + (uint64_t)(uint32_t)h * (RA_D * esz), l16);
+        KvRaw<DT> row = kv_load8<DT, ONCE>(in + (uint64_t)(uint32_t)h * (RA_D * esz), l16);
         if (which < 2) {
             float v[8];
             kv_floats<DT>(row, v);
@@ -214,7 +221,11 @@ ra_status ra_launch_append(const AppendArgs& a, ra_dtype dt, hipStream_t st) {
     const int heads = a.n_q + 2 * a.n_kv, split = tokens <= 128 ? (heads + KV_GROUPS - 1) / KV_GROUPS : 1;
     const int64_t blocks = tokens * split;
     if (blocks > (1 << 24) - 1) RA_FAIL(RA_EUNSUP, "too many heads for one launch");
-#define KV_GO_T(DTV, THREADS) hipLaunchKernelGGL((append_kernel<DTV, THREADS>), dim3((unsigned)blocks), dim3(THREADS), 0, st, a, split)
+#define KV_GO_1(DTV, THREADS, ONCE) hipLaunchKernelGGL((append_kernel<DTV, THREADS, ONCE>), dim3((unsigned)blocks), dim3(THREADS), 0, st, a, split)
+#define KV_GO_T(DTV, THREADS)                                                                                        \
+    do {                                                                                                             \
+        if (tokens * bytes > KV_KEPT) KV_GO_1(DTV, THREADS, true); else KV_GO_1(DTV, THREADS, false);                \
+    } while (0)
     // Tokens of little data want small workgroups, which wait for less at a time, where there are enough of them to fill the part (us
     // with 64, 128 and 256 threads, bfloat16: 20000 of 6 + 2 + 2 heads 30, 35, 45; 16384 of 16 + 2 + 2 36, 39, 47; 32768 of 28 + 4 + 4
     // 123, 113, 125; 16384 of 64 + 8 + 8 135, 129, 122; float32, 16384 of 8 + 8 + 8 93, 90, 85; 2500 of 16 + 2 + 2 11.7, 10.8, 11.6;
@@ -228,6 +239,7 @@ ra_status ra_launch_append(const AppendArgs& a, ra_dtype dt, hipStream_t st) {
     } while (0)
     if (dt == RA_BF16) KV_GO(RA_BF16); else KV_GO(RA_F32);
 #undef KV_GO_T
+#undef KV_GO_1
 #undef KV_GO
     RA_HIP(hipGetLastError());
     return RA_OK;
@@ -237,7 +249,7 @@ ra_status ra_launch_append(const AppendArgs& a, ra_dtype dt, hipStream_t st) {
 // loads are all on their way before the first is worked on; a row that is not there is loaded as another one that is. Four rows where
 // there are many, else one (us into 4 bits and back: 8 heads of 131072 bf16 rows 105 with four, 108 with one, 112 with eight; 6 heads
 // of 1003 float32 rows 7.0, 5.7, 9.0).
-template <int DT, int FLY>
+template <int DT, int FLY, bool ONCE>
 __global__ __launch_bounds__(KV_THREADS) void quantize_kv4_kernel(const void* __restrict__ X, int n_kv, int64_t T,
                                                                   const int32_t* __restrict__ first, const int32_t* __restrict__ n_new,
                                                                   int64_t kv_stride, uint8_t* __restrict__ codes,
@@ -252,7 +264,7 @@ __global__ __launch_bounds__(KV_THREADS) void quantize_kv4_kernel(const void* __
 #pragma unroll
     for (int u = 0; u < FLY; ++u) {
         const int64_t t = t0 + KV_GROUPS * u;
-        raw[u] = kv_load8<DT>(rows + (t < T ? t : T - 1) * RA_D * (DT == RA_BF16 ? 2 : 4), l16);
+        raw[u] = kv_load8<DT, ONCE>(rows + (t < T ? t : T - 1) * RA_D * (DT == RA_BF16 ? 2 : 4), l16);
     }
 #pragma unroll
     for (int u = 0; u < FLY; ++u) {
@@ -280,7 +292,7 @@ __global__ __launch_bounds__(KV_THREADS) void dequantize_kv4_kernel(const uint8_
         const int64_t at = at0 + t0 + KV_GROUPS * u;
         there[u] = at >= 0 && at < kv_stride;
         const size_t row = head * kv_stride + (there[u] ? at : 0);
-        c[u] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(codes + row * Q4_ROW) + l16);
+        c[u] = reinterpret_cast<const uint32_t*>(codes + row * Q4_ROW)[l16];
         b[u] = scale[row * Q4_BLOCKS + l16 / 4];
     }
 #pragma unroll
@@ -303,16 +315,7 @@ static ra_status rows_grid(int n_seq, int n_kv, int64_t T, bool* four, dim3* gri
     *grid = dim3((unsigned)blocks, (unsigned)heads);
     return RA_OK;
 }
-#define KV_ROWS_GO(KERNEL, ...)                                                                                          \
-    do {                                                                                                                 \
-        if (dt == RA_BF16) {                                                                                             \
-            if (four) hipLaunchKernelGGL((KERNEL<RA_BF16, 4>), grid, dim3(KV_THREADS), 0, st, __VA_ARGS__);              \
-            else hipLaunchKernelGGL((KERNEL<RA_BF16, 1>), grid, dim3(KV_THREADS), 0, st, __VA_ARGS__);                   \
-        } else {                                                                                                         \
-            if (four) hipLaunchKernelGGL((KERNEL<RA_F32, 4>), grid, dim3(KV_THREADS), 0, st, __VA_ARGS__);               \
-            else hipLaunchKernelGGL((KERNEL<RA_F32, 1>), grid, dim3(KV_THREADS), 0, st, __VA_ARGS__);                    \
-        }                                                                                                                \
-    } while (0)
+#define KV_ROWS_GO(KERNEL, ...) hipLaunchKernelGGL((KERNEL), grid, dim3(KV_THREADS), 0, st, __VA_ARGS__)
 
 ra_status ra_launch_quantize_kv4(const void* X, ra_dtype dt, int n_seq, int n_kv, int64_t T, const int32_t* first,
                                  const int32_t* n_new, int64_t kv_stride, hipStream_t st, uint8_t* codes, uint8_t* scale) {
@@ -320,7 +323,15 @@ ra_status ra_launch_quantize_kv4(const void* X, ra_dtype dt, int n_seq, int n_kv
     bool four;
     const ra_status rc = rows_grid(n_seq, n_kv, T, &four, &grid);
     if (rc != RA_OK) return rc;
-    KV_ROWS_GO(quantize_kv4_kernel, X, n_kv, T, first, n_new, kv_stride, codes, scale);
+    const bool once = (int64_t)n_seq * n_kv * T * RA_D * (dt == RA_BF16 ? 2 : 4) > KV_KEPT;      // (never so few that each takes one row)
+#define KV_GO(DTV)                                                                                                              \
+    do {                                                                                                                        \
+        if (once) KV_ROWS_GO((quantize_kv4_kernel<DTV, 4, true>), X, n_kv, T, first, n_new, kv_stride, codes, scale);           \
+        else if (four) KV_ROWS_GO((quantize_kv4_kernel<DTV, 4, false>), X, n_kv, T, first, n_new, kv_stride, codes, scale);     \
+        else KV_ROWS_GO((quantize_kv4_kernel<DTV, 1, false>), X, n_kv, T, first, n_new, kv_stride, codes, scale);               \
+    } while (0)
+    if (dt == RA_BF16) KV_GO(RA_BF16); else KV_GO(RA_F32);
+#undef KV_GO
     RA_HIP(hipGetLastError());
     return RA_OK;
 }
@@ -331,7 +342,13 @@ ra_status ra_launch_dequantize_kv4(const uint8_t* codes, const uint8_t* scale, r
     bool four;
     const ra_status rc = rows_grid(n_seq, n_kv, T, &four, &grid);
     if (rc != RA_OK) return rc;
-    KV_ROWS_GO(dequantize_kv4_kernel, codes, scale, n_kv, T, first, kv_stride, X);
+#define KV_GO(DTV)                                                                                                              \
+    do {                                                                                                                        \
+        if (four) KV_ROWS_GO((dequantize_kv4_kernel<DTV, 4>), codes, scale, n_kv, T, first, kv_stride, X);                      \
+        else KV_ROWS_GO((dequantize_kv4_kernel<DTV, 1>), codes, scale, n_kv, T, first, kv_stride, X);                           \
+    } while (0)
+    if (dt == RA_BF16) KV_GO(RA_BF16); else KV_GO(RA_F32);
+#undef KV_GO
     RA_HIP(hipGetLastError());
     return RA_OK;
 }
