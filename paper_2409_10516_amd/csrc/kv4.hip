@@ -7,10 +7,11 @@
 #define KV_THREADS 256
 #define KV_GROUPS (KV_THREADS / 16)
 
-// values [8 l16, 8 l16 + 8) of a row, as loaded. Rows are written once: non-temporal (131072 rows of 8 heads into 4 bits and back 116 -> 107 us,
-// a 32K prompt's rows 159 -> 154, 2000 tokens 15.1 -> 13.5). They are read once, too, but what a call reads has just been made, and up to a
-// quarter of what the memory side keeps is taken from there (us, with ONCE and without (which as a choice at run time costs the large ones 3 %): 5105 tokens of 10 float32 heads, 26 MB, 15.5, 13.5, 32768 rows of 8
-// heads, 64 MB, 30.9, 28.2, a 32K prompt 154, 157, 8000 tokens, 98 MB, 42.5, 44.8).
+// Values [8 l16, 8 l16 + 8) of a row, as loaded. Rows are written once: non-temporal (131072 rows of 8 heads into 4 bits and back 116 -> 107
+// us, a 32K prompt's rows 159 -> 154, 2000 tokens 15.1 -> 13.5). They are read once, too, but what a call reads has just been made, and up to a
+// quarter of what the memory side keeps is taken from there (us with ONCE and without: 5105 tokens of 10 float32 heads, 26 MB, 15.5,
+// 13.5, 32768 rows of 8 heads, 64 MB, 30.9, 28.2, 8000 tokens of 48 heads, 98 MB, 42.5, 44.8, a 32K prompt 154, 157; as a choice at
+// run time it costs the large ones 3 %).
 #define KV_KEPT (1 << 26)           // bytes read
 typedef uint32_t kv_u32x4 __attribute__((ext_vector_type(4)));
 template <int DT> struct KvRaw { kv_u32x4 a[DT == RA_BF16 ? 1 : 2]; };
@@ -217,6 +218,7 @@ __global__ __launch_bounds__(THREADS, 8) void append_kernel(AppendArgs a, int sp
 ra_status ra_launch_append(const AppendArgs& a, ra_dtype dt, hipStream_t st) {
     const int64_t tokens = a.T * a.n_seq;
     if (tokens > (1 << 24) - 1) RA_FAIL(RA_EUNSUP, "more than 2^24 - 1 tokens in a call");
+    if ((int64_t)a.n_q + 2 * (int64_t)a.n_kv > (1 << 24) - 1) RA_FAIL(RA_EUNSUP, "too many heads for one launch");
     // where a workgroup per token leaves compute units idle, a workgroup for every 16 heads of one
     const int heads = a.n_q + 2 * a.n_kv, split = tokens <= 128 ? (heads + KV_GROUPS - 1) / KV_GROUPS : 1;
     const int64_t blocks = tokens * split;
