@@ -826,7 +826,7 @@ struct Q4Cut { int tiles, workgroups, unit_log2; bool whole, refused; };
 static Q4Cut q4_cut(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N) {
     Q4Cut x;
     const int heads = q4_heads(n_q / n_kv);
-    x.tiles = (n_q / n_kv + heads - 1) / heads;
+    x.tiles = (int)(((int64_t)(n_q / n_kv) + heads - 1) / heads);
     const int64_t jobs = (int64_t)n_seq * n_kv * x.tiles;
     x.whole = N <= 1024 || N <= (jobs < 2048 ? 16 * jobs : 32768) || (jobs > Q4_MOST_UNITS && N <= Q4_MOST_ROWS);
     x.unit_log2 = 7;

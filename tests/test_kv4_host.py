@@ -66,6 +66,7 @@ FULL = dict(q=_p(), dt=1, K4=_p(), K4s=_p(), V4=_p(), V4s=_p(), n_seq=1, n_q=4, 
     (dict(n_kv=0), 1, "positive"), (dict(d=256), 6, "d = 128"), (dict(K4=None), 1, "K"), (dict(V4s=None), 1, "V"),
     (dict(V4=_p(0x10004)), 1, "aligned"), (dict(N=0), 1, "positive"), (dict(N=1 << 31, stride=1 << 31), 6, "large"), (dict(stride=99), 2, "below"),
     (dict(q=_p(0x10002)), 1, "aligned"), (dict(ws=_p(0x10004)), 1, "aligned"), (dict(ws_bytes=8), 2, "workspace"),
+    (dict(n_q=(1 << 31) - 1, n_kv=1), 6, "too many heads"), (dict(n_seq=1 << 23, n_q=4, n_kv=4), 6, "too many heads"),
 ])
 def test_full_attention_refuses(change, status, needle):
     L = ra.lib()
