@@ -1,87 +1,82 @@
 // Tokens that enter a cache: norms of queries and keys per head, position rotation, the new rows (ra_append_tokens), and
-// rows into 4 bits and back (ra_quantize_kv4, ra_dequantize_kv4). All of it moves rows: 16 lanes hold one row of 128 values, 8
-// each, so a block of 32 dimensions is four lanes and the partner of a half-split rotation (a multiple of 8 dimensions away,
-// rot_dim being one of 16) is 8 values of one other lane.
+// rows into 4 bits and back (ra_quantize_kv4, ra_dequantize_kv4). All of it moves rows: a lane has 16 bytes of one, 8 values of bfloat16 in
+// 16 lanes or 4 of float32 in 32, so that an instruction reads or writes whole lines (float32 rows in 16 lanes, two instructions
+// for halves of a line's every 32 bytes: 32674 x 5 x 2 of them into 4 bits and back 99.7 us). A block of 32 dimensions is four or eight lanes, and
+// the partner of a half-split rotation (a multiple of 8 dimensions away, rot_dim being one of 16) is the same value of another lane.
 #include "q4_dev.h"
 
 #define KV_THREADS 256
-#define KV_GROUPS (KV_THREADS / 16)
+template <int DT> constexpr int KV_VALS = DT == RA_BF16 ? 8 : 4;        // of a lane
+template <int DT> constexpr int KV_LANES = RA_D / KV_VALS<DT>;          // of a row
 
-// Values [8 l16, 8 l16 + 8) of a row, as loaded. Rows are written once: non-temporal (131072 rows of 8 heads into 4 bits and back 116 -> 107
+// A lane's values of a row, as loaded. Rows are written once: non-temporal (131072 rows of 8 heads into 4 bits and back 116 -> 107
 // us, a 32K prompt's rows 159 -> 154, 2000 tokens 15.1 -> 13.5). They are read once, too, but what a call reads has just been made, and up to a
 // quarter of what the memory side keeps is taken from there (us with ONCE and without: 5105 tokens of 10 float32 heads, 26 MB, 15.5,
 // 13.5, 32768 rows of 8 heads, 64 MB, 30.9, 28.2, 8000 tokens of 48 heads, 98 MB, 42.5, 44.8, a 32K prompt 154, 157; as a choice at
 // run time it costs the large ones 3 %).
 #define KV_KEPT (1 << 26)           // bytes read
 typedef uint32_t kv_u32x4 __attribute__((ext_vector_type(4)));
-template <int DT> struct KvRaw { kv_u32x4 a[DT == RA_BF16 ? 1 : 2]; };
-template <int DT, bool ONCE>
-__device__ __forceinline__ KvRaw<DT> kv_load8(const void* row, int l16) {
-    constexpr int W = DT == RA_BF16 ? 1 : 2;
-    const kv_u32x4* from = reinterpret_cast<const kv_u32x4*>(row) + W * l16;
-    KvRaw<DT> x;
-#pragma unroll
-    for (int i = 0; i < W; ++i) {
-        if constexpr (ONCE) x.a[i] = __builtin_nontemporal_load(from + i);
-        else x.a[i] = from[i];
-    }
-    return x;
+template <bool ONCE>
+__device__ __forceinline__ kv_u32x4 kv_load(const void* row, int l) {
+    const kv_u32x4* from = reinterpret_cast<const kv_u32x4*>(row) + l;
+    if constexpr (ONCE) return __builtin_nontemporal_load(from);
+    else return *from;
+}
+__device__ __forceinline__ void kv_store(void* row, int l, kv_u32x4 x) {
+    __builtin_nontemporal_store(x, reinterpret_cast<kv_u32x4*>(row) + l);
 }
 template <int DT>
-__device__ __forceinline__ void kv_floats(const KvRaw<DT>& x, float (&v)[8]) {
+__device__ __forceinline__ void kv_floats(kv_u32x4 x, float (&v)[KV_VALS<DT>]) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        if constexpr (DT == RA_BF16) v[e] = e & 1 ? bf16_hi(x.a[0][e / 2]) : bf16_lo(x.a[0][e / 2]);
-        else v[e] = __uint_as_float(x.a[e / 4][e & 3]);
+    for (int e = 0; e < KV_VALS<DT>; ++e) {
+        if constexpr (DT == RA_BF16) v[e] = e & 1 ? bf16_hi(x[e / 2]) : bf16_lo(x[e / 2]);
+        else v[e] = __uint_as_float(x[e]);
     }
 }
 typedef __bf16 kv_bf16x8 __attribute__((ext_vector_type(8)));
 // rounded to DT
 template <int DT>
-__device__ __forceinline__ KvRaw<DT> kv_pack(const float (&v)[8]) {
-    KvRaw<DT> x;
+__device__ __forceinline__ kv_u32x4 kv_pack(const float (&v)[KV_VALS<DT>]) {
     if constexpr (DT == RA_BF16) {
         kv_bf16x8 b;
 #pragma unroll
         for (int e = 0; e < 8; ++e) b[e] = (__bf16)v[e];
-        x.a[0] = __builtin_bit_cast(kv_u32x4, b);
+        return __builtin_bit_cast(kv_u32x4, b);
     } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x.a[e / 4][e & 3] = __float_as_uint(v[e]);
+        return kv_u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
     }
-    return x;
 }
+// A row into 4 bits. Called by all of its lanes.
 template <int DT>
-__device__ __forceinline__ void kv_store8(void* row, int l16, const KvRaw<DT>& x) {
-    constexpr int W = DT == RA_BF16 ? 1 : 2;
-#pragma unroll
-    for (int i = 0; i < W; ++i) __builtin_nontemporal_store(x.a[i], reinterpret_cast<kv_u32x4*>(row) + W * l16 + i);
-}
-// A row of 16 lanes x 8 values into 4 bits. Called by whole groups of 16 lanes.
-__device__ __forceinline__ void kv_store4(uint8_t* codes, uint8_t* scale, int l16, int lane, const float (&v)[8]) {
+__device__ __forceinline__ void kv_store4(uint8_t* codes, uint8_t* scale, int l, int lane, const float (&v)[KV_VALS<DT>]) {
     uint32_t m = 0u;                                   // magnitudes compare like their bits, a NaN above all
 #pragma unroll
-    for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(v[e]) & 0x7fffffffu);
+    for (int e = 0; e < KV_VALS<DT>; ++e) m = max(m, __float_as_uint(v[e]) & 0x7fffffffu);
     m = max(m, lane_xor32<1>(m, lane));
     m = max(m, lane_xor32<2>(m, lane));
-    const uint32_t byte = q4_scale_byte(m);
-    reinterpret_cast<uint32_t*>(codes)[l16] = q4_codes(v, byte);
-    uint32_t all = byte << (8 * (l16 / 4));              // the four blocks' bytes, in one word
-    all |= lane_xor32<4>(all, lane);
+    if constexpr (DT == RA_F32) m = max(m, lane_xor32<4>(m, lane));
+    const uint32_t byte = q4_scale_byte(m), w = q4_codes(v, byte);
+    if constexpr (DT == RA_F32) reinterpret_cast<uint16_t*>(codes)[l] = (uint16_t)w;
+    else reinterpret_cast<uint32_t*>(codes)[l] = w;
+    uint32_t all = byte << (8 * (l / (32 / KV_VALS<DT>)));       // the four blocks' bytes, in one word
+    if constexpr (DT == RA_BF16) all |= lane_xor32<4>(all, lane);
     all |= lane_xor32<8>(all, lane);
-    if (l16 == 0) *reinterpret_cast<uint32_t*>(scale) = all;
+    if constexpr (DT == RA_F32) all |= lane_xor32<16>(all, lane);
+    if (l == 0) *reinterpret_cast<uint32_t*>(scale) = all;
 }
 
 __device__ __forceinline__ double xor_add(double x, uint32_t lo, uint32_t hi) {
     return x + __hiloint2double((int)hi, (int)lo);
 }
-// sum over a row of 16 lanes, the same in all of them
-__device__ __forceinline__ double sum16(double x, int lane) {
+// sum over a row's lanes, the same in all of them
+template <int LANES>
+__device__ __forceinline__ double row_sum(double x, int lane) {
     uint32_t lo, hi;
 #define KV_STEP(J)                                                                             \
     lo = (uint32_t)__double2loint(x); hi = (uint32_t)__double2hiint(x);                        \
     x = xor_add(x, lane_xor32<J>(lo, lane), lane_xor32<J>(hi, lane));
     KV_STEP(1) KV_STEP(2) KV_STEP(4) KV_STEP(8)
+    if constexpr (LANES == 32) { KV_STEP(16) }
 #undef KV_STEP
     return x;
 }
@@ -111,17 +106,17 @@ __device__ __forceinline__ float2 cos_sin64(double x) {
 
 // Rotation of a row: a value times its cosine plus its pair's other value times its sine, which is negative for a pair's first. The other
 // value is in the same lane for neighbouring pairs, else STEP lanes away (0: in lane `from`).
-template <int STEP>
-__device__ __forceinline__ void turn(float (&v)[8], const float2 (&cs)[8], bool in_rot, int lane, int from) {
-    float other[8];
+template <int STEP, int VALS>
+__device__ __forceinline__ void turn(float (&v)[VALS], const float2 (&cs)[VALS], bool in_rot, int lane, int from) {
+    float other[VALS];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < VALS; ++e) {
         if constexpr (STEP < 0) other[e] = v[e ^ 1];
         else if constexpr (STEP == 0) other[e] = __shfl(v[e], from);
         else other[e] = __uint_as_float(lane_xor32<STEP>(__float_as_uint(v[e]), lane));
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < VALS; ++e) {
         float x = v[e] * cs[e].x + other[e] * cs[e].y;
         asm("" : "+v"(x));                                         // (not to be worked out behind a branch)
         v[e] = in_rot ? x : v[e];
@@ -129,7 +124,7 @@ __device__ __forceinline__ void turn(float (&v)[8], const float2 (&cs)[8], bool 
 }
 
 // A workgroup takes a token, or with few tokens, one of `split` parts of its heads: the sines and cosines of the token's angles, one
-// per lane of its first wavefront, then the heads' rows, one per 16 lanes. What bounds it is how many rows are on their way, hence
+// per lane of its first wavefront, then the heads' rows, one per group of lanes. What bounds it is how many rows are on their way, hence
 // registers for eight wavefronts per SIMD and nothing asked for ahead, and next the vector instructions of a row.
 // A 32K prompt of 32 + 8 + 8 normed heads, 150 us (5.4 TB/s; without norm and rotation 145). Held to seven wavefronts, six, five or four
 // 206, 223, 248, 283 of then 192; that 192 had a branch and a wait for shared memory per rotated value, with a branch around
@@ -139,13 +134,14 @@ template <int DT, int THREADS, bool ONCE>
 __global__ __launch_bounds__(THREADS, 8) void append_kernel(AppendArgs a, int split) {
     __shared__ float2 s_cs[RA_D / 2];
     __shared__ float4 s_w[2][RA_D / 4];
-    const int tid = threadIdx.x, lane = tid & (RA_WAVE - 1), l16 = tid & 15, grp = tid >> 4;
+    constexpr int VALS = KV_VALS<DT>, LANES = KV_LANES<DT>, GROUPS = THREADS / LANES;
+    const int tid = threadIdx.x, lane = tid & (RA_WAVE - 1), l = tid % LANES, grp = tid / LANES;
     const size_t esz = DT == RA_BF16 ? 2 : 4;
     const int T = (int)a.T, tok = blockIdx.x / split, seq = tok / T, t = tok % T;
     if (a.n_new && t >= a.n_new[seq]) return;                       // (uniform)
     const int64_t pos = (int64_t)(a.first ? a.first[seq] : 0) + t;
     const bool there[2] = {pos >= 0 && pos < a.stride[0], pos >= 0 && pos < a.stride[1]};
-    const int n_rows = a.n_q + 2 * a.n_kv, step = THREADS / 16 * split, rot = a.rot, half = rot / 2;
+    const int n_rows = a.n_q + 2 * a.n_kv, step = GROUPS * split, rot = a.rot, half = rot / 2;
     // where the token's rows are, head 0's (none: no such input or output)
     auto at = [&](const void* p, size_t row) { return p ? reinterpret_cast<char*>(const_cast<void*>(p)) + row * esz : nullptr; };
     const char *in_q = at(a.in[0], tok * a.row[0]), *in_k = at(a.in[1], tok * a.row[1]), *in_v = at(a.in[2], tok * a.row[2]);
@@ -160,56 +156,60 @@ __global__ __launch_bounds__(THREADS, 8) void append_kernel(AppendArgs a, int sp
                 reinterpret_cast<float*>(s_w[i])[d] = DT == RA_BF16 ? bf16_lo(reinterpret_cast<const uint16_t*>(a.weight[i])[d])
                                                                     : reinterpret_cast<const float*>(a.weight[i])[d];
     __syncthreads();
-    const int near = half / 8;                                     // lanes of a half
-    const bool low = l16 < near, in_rot = l16 < 2 * near;
-    const int from = (lane & ~15) + (low ? l16 + near : in_rot ? l16 - near : l16);
-    float2 cs[8];                                                  // of the lane's dimensions, whatever the row
+    const int near = half / VALS;                                  // lanes of a half
+    const bool low = l < near, in_rot = l < 2 * near;
+    const int from = lane - l + (low ? l + near : in_rot ? l - near : l);
+    float2 cs[VALS];                                               // of the lane's dimensions, whatever the row
     if (rot) {
-        const float2* at = s_cs + (!in_rot ? 0 : a.interleaved ? 4 * l16 : 8 * (low ? l16 : l16 - near));
+        const float2* at = s_cs + (!in_rot ? 0 : a.interleaved ? VALS / 2 * l : VALS * (low ? l : l - near));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < VALS; ++e) {
             cs[e] = at[a.interleaved ? e / 2 : e];
             if (a.interleaved ? !(e & 1) : low) cs[e].y = -cs[e].y;
         }
     }
-    for (int r = grp + (int)(blockIdx.x % split) * (THREADS / 16); r < n_rows; r += step) {
+    for (int r = grp + (int)(blockIdx.x % split) * GROUPS; r < n_rows; r += step) {
         const int which = r < a.n_q ? 0 : r < a.n_q + a.n_kv ? 1 : 2;
         const int h = which == 0 ? r : which == 1 ? r - a.n_q : r - a.n_q - a.n_kv;
         const char* in = which == 0 ? in_q : which == 1 ? in_k : in_v;
         if (!in || (which && !there[0] && !there[1])) continue;
-        KvRaw<DT> row = kv_load8<DT, ONCE>(in + (uint64_t)(uint32_t)h * (RA_D * esz), l16);
+        kv_u32x4 row = kv_load<ONCE>(in + (uint64_t)(uint32_t)h * (RA_D * esz), l);
         if (which < 2) {
-            float v[8];
+            float v[VALS];
             kv_floats<DT>(row, v);
             if (a.weight[which]) {
                 double sum = 0.;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum = fma((double)v[e], (double)v[e], sum);
-                const float rinv = (float)rsqrt64(sum16(sum, lane) * (1. / RA_D) + a.eps);
-                const float4 w0 = s_w[which][2 * l16], w1 = s_w[which][2 * l16 + 1];
-                const float w[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+                for (int e = 0; e < VALS; ++e) sum = fma((double)v[e], (double)v[e], sum);
+                const float rinv = (float)rsqrt64(row_sum<LANES>(sum, lane) * (1. / RA_D) + a.eps);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = v[e] * rinv * w[e];
+                for (int f = 0; f < VALS / 4; ++f) {
+                    const float4 w = s_w[which][VALS / 4 * l + f];
+                    v[4 * f] = v[4 * f] * rinv * w.x;
+                    v[4 * f + 1] = v[4 * f + 1] * rinv * w.y;
+                    v[4 * f + 2] = v[4 * f + 2] * rinv * w.z;
+                    v[4 * f + 3] = v[4 * f + 3] * rinv * w.w;
+                }
             }
             if (rot) {
                 if (a.interleaved) turn<-1>(v, cs, in_rot, lane, from);
-                else if (near == 8) turn<8>(v, cs, in_rot, lane, from);
-                else if (near == 4) turn<4>(v, cs, in_rot, lane, from);
+                else if (near == LANES / 2) turn<LANES / 2>(v, cs, in_rot, lane, from);
+                else if (near == LANES / 4) turn<LANES / 4>(v, cs, in_rot, lane, from);
                 else turn<0>(v, cs, in_rot, lane, from);
             }
             row = kv_pack<DT>(v);
         }
         if (which == 0) {
-            kv_store8<DT>(out_q + (uint64_t)(uint32_t)h * (uint32_t)T * (RA_D * esz), l16, row);
+            kv_store(out_q + (uint64_t)(uint32_t)h * (uint32_t)T * (RA_D * esz), l, row);
         } else {
             // (capacities are below 2^30 rows)
             char* out = which == 1 ? out_k : out_v;
-            if (out && there[0]) kv_store8<DT>(out + (uint64_t)(uint32_t)h * (uint32_t)a.stride[0] * (RA_D * esz), l16, row);
+            if (out && there[0]) kv_store(out + (uint64_t)(uint32_t)h * (uint32_t)a.stride[0] * (RA_D * esz), l, row);
             if (a.codes[which - 1] && there[1]) {
-                float v[8];
+                float v[VALS];
                 kv_floats<DT>(row, v);
                 const uint64_t row4 = head4 + (uint64_t)(uint32_t)h * (uint32_t)a.stride[1];
-                kv_store4(a.codes[which - 1] + row4 * Q4_ROW, a.scale[which - 1] + row4 * Q4_BLOCKS, l16, lane, v);
+                kv_store4<DT>(a.codes[which - 1] + row4 * Q4_ROW, a.scale[which - 1] + row4 * Q4_BLOCKS, l, lane, v);
             }
         }
     }
@@ -219,8 +219,9 @@ ra_status ra_launch_append(const AppendArgs& a, ra_dtype dt, hipStream_t st) {
     const int64_t tokens = a.T * a.n_seq;
     if (tokens > (1 << 24) - 1) RA_FAIL(RA_EUNSUP, "more than 2^24 - 1 tokens in a call");
     if ((int64_t)a.n_q + 2 * (int64_t)a.n_kv > (1 << 24) - 1) RA_FAIL(RA_EUNSUP, "too many heads for one launch");
-    // where a workgroup per token leaves compute units idle, a workgroup for every 16 heads of one
-    const int heads = a.n_q + 2 * a.n_kv, split = tokens <= 128 ? (heads + KV_GROUPS - 1) / KV_GROUPS : 1;
+    // where a workgroup per token leaves compute units idle, a workgroup for as many heads of one as it takes at a time
+    const int groups = dt == RA_BF16 ? KV_THREADS / KV_LANES<RA_BF16> : KV_THREADS / KV_LANES<RA_F32>;
+    const int heads = a.n_q + 2 * a.n_kv, split = tokens <= 128 ? (heads + groups - 1) / groups : 1;
     const int64_t blocks = tokens * split;
     if (blocks > (1 << 24) - 1) RA_FAIL(RA_EUNSUP, "too many heads for one launch");
 #define KV_GO_1(DTV, THREADS, ONCE) hipLaunchKernelGGL((append_kernel<DTV, THREADS, ONCE>), dim3((unsigned)blocks), dim3(THREADS), 0, st, a, split)
@@ -235,8 +236,8 @@ ra_status ra_launch_append(const AppendArgs& a, ra_dtype dt, hipStream_t st) {
     const int64_t bytes = (int64_t)heads * RA_D * (dt == RA_BF16 ? 2 : 4);
 #define KV_GO(DTV)                                                                                    \
     do {                                                                                              \
-        if (heads <= 4 || (tokens >= 8192 && bytes <= 6144)) KV_GO_T(DTV, 64);                        \
-        else if (heads <= 8 || (tokens >= 2048 && bytes <= 10240)) KV_GO_T(DTV, 128);                 \
+        if (bytes <= 1024 || (tokens >= 8192 && bytes <= 6144)) KV_GO_T(DTV, 64);                     \
+        else if (bytes <= 2048 || (tokens >= 2048 && bytes <= 10240)) KV_GO_T(DTV, 128);                 \
         else KV_GO_T(DTV, KV_THREADS);                                                                \
     } while (0)
     if (dt == RA_BF16) KV_GO(RA_BF16); else KV_GO(RA_F32);
@@ -247,7 +248,7 @@ ra_status ra_launch_append(const AppendArgs& a, ra_dtype dt, hipStream_t st) {
     return RA_OK;
 }
 
-// grid: x = rows of a head, KV_GROUPS x FLY to a workgroup, y = head (with its sequence). A group of 16 lanes takes FLY rows, whose
+// grid: x = rows of a head, GROUPS x FLY to a workgroup, y = head (with its sequence). A group of lanes takes FLY rows, whose
 // loads are all on their way before the first is worked on; a row that is not there is loaded as another one that is. Four rows where
 // there are many, else one (us into 4 bits and back: 8 heads of 131072 bf16 rows 105 with four, 108 with one, 112 with eight; 6 heads
 // of 1003 float32 rows 7.0, 5.7, 9.0).
@@ -256,26 +257,27 @@ __global__ __launch_bounds__(KV_THREADS) void quantize_kv4_kernel(const void* __
                                                                   const int32_t* __restrict__ first, const int32_t* __restrict__ n_new,
                                                                   int64_t kv_stride, uint8_t* __restrict__ codes,
                                                                   uint8_t* __restrict__ scale) {
-    const int tid = threadIdx.x, lane = tid & (RA_WAVE - 1), l16 = tid & 15;
+    constexpr int LANES = KV_LANES<DT>, GROUPS = KV_THREADS / LANES;
+    const int tid = threadIdx.x, lane = tid & (RA_WAVE - 1), l = tid % LANES;
     const size_t head = blockIdx.y;
     const int seq = (int)(head / n_kv);
-    const int64_t t0 = (int64_t)blockIdx.x * (KV_GROUPS * FLY) + (tid >> 4), at0 = first ? first[seq] : 0;
+    const int64_t t0 = (int64_t)blockIdx.x * (GROUPS * FLY) + tid / LANES, at0 = first ? first[seq] : 0;
     const int64_t n = n_new && n_new[seq] < T ? n_new[seq] : T;
     const char* rows = reinterpret_cast<const char*>(X) + head * T * RA_D * (DT == RA_BF16 ? 2 : 4);
-    KvRaw<DT> raw[FLY];
+    kv_u32x4 raw[FLY];
 #pragma unroll
     for (int u = 0; u < FLY; ++u) {
-        const int64_t t = t0 + KV_GROUPS * u;
-        raw[u] = kv_load8<DT, ONCE>(rows + (t < T ? t : T - 1) * RA_D * (DT == RA_BF16 ? 2 : 4), l16);
+        const int64_t t = t0 + GROUPS * u;
+        raw[u] = kv_load<ONCE>(rows + (t < T ? t : T - 1) * RA_D * (DT == RA_BF16 ? 2 : 4), l);
     }
 #pragma unroll
     for (int u = 0; u < FLY; ++u) {
-        const int64_t t = t0 + KV_GROUPS * u, at = at0 + t;
+        const int64_t t = t0 + GROUPS * u, at = at0 + t;
         if (t >= n || at < 0 || at >= kv_stride) continue;
-        float v[8];
+        float v[KV_VALS<DT>];
         kv_floats<DT>(raw[u], v);
         const size_t row = head * kv_stride + at;
-        kv_store4(codes + row * Q4_ROW, scale + row * Q4_BLOCKS, l16, lane, v);
+        kv_store4<DT>(codes + row * Q4_ROW, scale + row * Q4_BLOCKS, l, lane, v);
     }
 }
 
@@ -283,35 +285,37 @@ template <int DT, int FLY>
 __global__ __launch_bounds__(KV_THREADS) void dequantize_kv4_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scale,
                                                                     int n_kv, int64_t T, const int32_t* __restrict__ first,
                                                                     int64_t kv_stride, void* __restrict__ X) {
-    const int tid = threadIdx.x, l16 = tid & 15;
+    constexpr int LANES = KV_LANES<DT>, GROUPS = KV_THREADS / LANES;
+    const int tid = threadIdx.x, l = tid % LANES;
     const size_t head = blockIdx.y;
     const int seq = (int)(head / n_kv);
-    const int64_t t0 = (int64_t)blockIdx.x * (KV_GROUPS * FLY) + (tid >> 4), at0 = first ? first[seq] : 0;
+    const int64_t t0 = (int64_t)blockIdx.x * (GROUPS * FLY) + tid / LANES, at0 = first ? first[seq] : 0;
     uint32_t c[FLY], b[FLY];
     bool there[FLY];
 #pragma unroll
     for (int u = 0; u < FLY; ++u) {
-        const int64_t at = at0 + t0 + KV_GROUPS * u;
+        const int64_t at = at0 + t0 + GROUPS * u;
         there[u] = at >= 0 && at < kv_stride;
         const size_t row = head * kv_stride + (there[u] ? at : 0);
-        c[u] = reinterpret_cast<const uint32_t*>(codes + row * Q4_ROW)[l16];
-        b[u] = scale[row * Q4_BLOCKS + l16 / 4];
+        if constexpr (DT == RA_F32) c[u] = reinterpret_cast<const uint16_t*>(codes + row * Q4_ROW)[l];
+        else c[u] = reinterpret_cast<const uint32_t*>(codes + row * Q4_ROW)[l];
+        b[u] = scale[row * Q4_BLOCKS + l / (LANES / Q4_BLOCKS)];
     }
 #pragma unroll
     for (int u = 0; u < FLY; ++u) {
-        const int64_t t = t0 + KV_GROUPS * u;
+        const int64_t t = t0 + GROUPS * u;
         if (t >= T) continue;
-        float v[8];
+        float v[KV_VALS<DT>];
         q4_values(there[u] ? c[u] : 0u, q4_unit(there[u] ? b[u] : 127u), v);
-        kv_store8<DT>(reinterpret_cast<char*>(X) + (head * T + t) * RA_D * (DT == RA_BF16 ? 2 : 4), l16, kv_pack<DT>(v));
+        kv_store(reinterpret_cast<char*>(X) + (head * T + t) * RA_D * (DT == RA_BF16 ? 2 : 4), l, kv_pack<DT>(v));
     }
 }
 
 // what both launch: rows per group of lanes, and the grid
-static ra_status rows_grid(int n_seq, int n_kv, int64_t T, bool* four, dim3* grid) {
+static ra_status rows_grid(ra_dtype dt, int n_seq, int n_kv, int64_t T, bool* four, dim3* grid) {
     const int64_t heads = (int64_t)n_seq * n_kv;
     *four = heads * T >= 1 << 16;
-    const int64_t rows = KV_GROUPS * (*four ? 4 : 1), blocks = (T + rows - 1) / rows;
+    const int64_t rows = KV_THREADS / (dt == RA_BF16 ? KV_LANES<RA_BF16> : KV_LANES<RA_F32>) * (*four ? 4 : 1), blocks = (T + rows - 1) / rows;
     if (heads > 65535) RA_FAIL(RA_EUNSUP, "more than 65535 (sequence, KV head) pairs");
     if (blocks > (1 << 24) - 1) RA_FAIL(RA_EUNSUP, "T too large");
     *grid = dim3((unsigned)blocks, (unsigned)heads);
@@ -323,7 +327,7 @@ ra_status ra_launch_quantize_kv4(const void* X, ra_dtype dt, int n_seq, int n_kv
                                  const int32_t* n_new, int64_t kv_stride, hipStream_t st, uint8_t* codes, uint8_t* scale) {
     dim3 grid;
     bool four;
-    const ra_status rc = rows_grid(n_seq, n_kv, T, &four, &grid);
+    const ra_status rc = rows_grid(dt, n_seq, n_kv, T, &four, &grid);
     if (rc != RA_OK) return rc;
     const bool once = (int64_t)n_seq * n_kv * T * RA_D * (dt == RA_BF16 ? 2 : 4) > KV_KEPT;      // (never so few that each takes one row)
 #define KV_GO(DTV)                                                                                                              \
@@ -342,7 +346,7 @@ ra_status ra_launch_dequantize_kv4(const uint8_t* codes, const uint8_t* scale, r
                                    const int32_t* first, int64_t kv_stride, hipStream_t st, void* X) {
     dim3 grid;
     bool four;
-    const ra_status rc = rows_grid(n_seq, n_kv, T, &four, &grid);
+    const ra_status rc = rows_grid(dt, n_seq, n_kv, T, &four, &grid);
     if (rc != RA_OK) return rc;
 #define KV_GO(DTV)                                                                                                              \
     do {                                                                                                                        \

@@ -14,7 +14,11 @@
 typedef float q4_f32x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ float q4_unit(uint32_t byte) { return __uint_as_float(byte << 23); }
 
-// the values of 8 codes, first dimension in the lowest bits
+// the values of 8 codes, or of 4, first dimension in the lowest bits
+__device__ __forceinline__ void q4_values(uint32_t codes, float unit, float (&v)[4]) {
+    const q4_f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, unit, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, unit, 1);
+    v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
+}
 __device__ __forceinline__ void q4_values(uint32_t codes, float unit, float (&v)[8]) {
     const q4_f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, unit, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, unit, 1);
     const q4_f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, unit, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, unit, 3);
@@ -28,7 +32,13 @@ __device__ __forceinline__ uint32_t q4_scale_byte(uint32_t bits) {
     const uint32_t e = (bits >> 23) + ((bits & 0x7fffffu) > 0x400000u ? 1u : 0u);
     return e > Q4_LEAST + 2u ? e - 2u : Q4_LEAST;
 }
-// 8 values of a block with that scale byte -> codes
+// 4 or 8 values of a block with that scale byte -> codes
+__device__ __forceinline__ uint32_t q4_codes(const float (&v)[4], uint32_t byte) {
+    if (byte == 255u) return 0u;
+    const float unit = q4_unit(byte);
+    const uint32_t w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, v[0], v[1], unit, 0);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2], v[3], unit, 1);
+}
 __device__ __forceinline__ uint32_t q4_codes(const float (&v)[8], uint32_t byte) {
     if (byte == 255u) return 0u;
     const float unit = q4_unit(byte);
