@@ -231,7 +231,7 @@ ra_status ra_launch_append(const AppendArgs& a, ra_dtype dt, hipStream_t st) {
     } while (0)
     // Tokens of little data want small workgroups, which wait for less at a time, where there are enough of them to fill the part (us
     // with 64, 128 and 256 threads, bfloat16: 20000 of 6 + 2 + 2 heads 30, 35, 45; 16384 of 16 + 2 + 2 36, 39, 47; 32768 of 28 + 4 + 4
-    // 123, 113, 125; 16384 of 64 + 8 + 8 135, 129, 122; float32, 16384 of 8 + 8 + 8 93, 90, 85; 2500 of 16 + 2 + 2 11.7, 10.8, 11.6;
+    // 123, 113, 125; 16384 of 64 + 8 + 8 135, 129, 122; float32, 16384 of 6 + 2 + 2 38, 41, 47, of 16 + 2 + 2 67, 69, 71; 2500 of 16 + 2 + 2 11.7, 10.8, 11.6;
     // 1000 of 32 + 8 + 8 17.5, 11.5, 9.4, of 4 + 1 + 1 6.1, 5.0, 5.4).
     const int64_t bytes = (int64_t)heads * RA_D * (dt == RA_BF16 ? 2 : 4);
 #define KV_GO(DTV)                                                                                    \
@@ -250,8 +250,8 @@ ra_status ra_launch_append(const AppendArgs& a, ra_dtype dt, hipStream_t st) {
 
 // grid: x = rows of a head, GROUPS x FLY to a workgroup, y = head (with its sequence). A group of lanes takes FLY rows, whose
 // loads are all on their way before the first is worked on; a row that is not there is loaded as another one that is. Four rows where
-// there are many, else one (us into 4 bits and back: 8 heads of 131072 bf16 rows 105 with four, 108 with one, 112 with eight; 6 heads
-// of 1003 float32 rows 7.0, 5.7, 9.0).
+// there are many, else one (us into 4 bits and back, four and one: 8 heads of 131072 bfloat16 rows 103, 109, of 4096 7.1, 6.8; 6 heads
+// of 1003 float32 rows 5.7, 5.3).
 template <int DT, int FLY, bool ONCE>
 __global__ __launch_bounds__(KV_THREADS) void quantize_kv4_kernel(const void* __restrict__ X, int n_kv, int64_t T,
                                                                   const int32_t* __restrict__ first, const int32_t* __restrict__ n_new,
