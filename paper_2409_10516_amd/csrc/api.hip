@@ -827,7 +827,7 @@ extern "C" ra_status ra_append_tokens(const void* q_in, const void* k_in, const 
     if (V4) RA_TRY(check_q4(V4, V4s, "V"));
     if (rot_dim < 0 || rot_dim > RA_D) RA_FAIL(RA_EINVAL, "rot_dim %d outside [0, %d]", rot_dim, RA_D);
     if (rot_dim % 16) RA_FAIL(RA_EUNSUP, "rot_dim %d is not a multiple of 16", rot_dim);
-    if (rot_dim && (q_in || k_in) && !inv_freq) RA_FAIL(RA_EINVAL, "NULL argument: inv_freq");
+    if (rot_dim && !inv_freq) RA_FAIL(RA_EINVAL, "NULL argument: inv_freq");
     if ((q_weight || k_weight) && !(eps >= 0.)) RA_FAIL(RA_EINVAL, "eps must be non-negative");
     const size_t esz = dt == RA_BF16 ? 2 : 4;
     AppendArgs a{{q_in, k_in, v_in}, {q_weight, k_weight}, {q_row, k_row, v_row}, {q_out, K, V}, {K4, V4}, {K4s, V4s},

@@ -26,6 +26,7 @@ GOOD = dict(q_in=_p(), k_in=_p(), v_in=_p(), dt=1, n_seq=2, n_q=4, n_kv=2, T=3, 
     (dict(k_row=0), 2, "apart"), (dict(q_row=513), 6, "16 bytes"), (dict(q_in=_p(0x10008)), 1, "aligned"), (dict(V=_p(0x10004)), 1, "aligned"),
     (dict(qw=_p(), eps=-1.0), 1, "eps"), (dict(kw=_p(), eps=float("nan")), 1, "eps"), (dict(qw=_p(0x10001)), 1, "aligned"),
     (dict(T=1 << 23, n_seq=2, q_row=512), 6, "tokens"), (dict(n_q=(1 << 31) - 2, q_row=1 << 38), 6, "heads"),
+    (dict(q_in=None, q_out=None, k_in=None, K=None, inv_freq=None), 1, "inv_freq"),    # (values alone are not rotated, but a length is given)
     (dict(n_q=1 << 24, q_row=1 << 31), 6, "heads"), (dict(n_q=1 << 23, n_seq=120, T=1, q_row=1 << 30), 6, "heads"),
 ])
 def test_append_refuses(change, status, needle):
