@@ -328,8 +328,7 @@ ra_status ra_dequantize_kv4(const uint8_t* codes, const uint8_t* scale, ra_dtype
 
 /* ra_full_attention over a cache in 4 bits: q [n_seq][n_q_heads][128] of type dt; rows [0, n) of sequence s, n =
  * min(n_tokens[s], N) (device int32; NULL: N for every sequence). A sequence without rows gets out = 0 and lse = -inf. Rows
- * from n on are not looked at. float32 accumulation; the weights of the softmax meet the values with 16 bits (dt = bfloat16)
- * or 24 (float32) of mantissa, and their sum is taken of what remains.
+ * from n on are not looked at. float32 accumulation; the weights of the softmax meet the values with all their 24 bits.
  * RA_EUNSUP where a workgroup's part of one head would pass 2^24 rows (hundreds of query heads per KV head over tens of millions of
  * tokens), and past 2^21 tiles of up to 16 query heads.
  * workspace: device memory of at least ra_full_attention_q4_workspace_bytes(...) bytes, 16-byte aligned, which nothing else may use
@@ -343,7 +342,7 @@ ra_status ra_full_attention_q4(const void* q, ra_dtype dt, const uint8_t* K4, co
 /* ra_attend over a cache in 4 bits (what follows ra_search or ra_search_q8 where no other cache is kept): Eq. 2 over Omega = ids
  * and over W, their combination by Eq. 4-5 into out/lse, and the four partial outputs, each of which may be NULL. N >= the
  * index's N tokens are in the cache, N <= kv_stride; as in ra_decode_step_grown W = [0, sink) u [min(N - window, N_index), N).
- * ids must not contain members of W; -1 and ids >= N are skipped. Weights have 24 bits for both types. Errors as for ra_attend.
+ * ids must not contain members of W; -1 and ids >= N are skipped. Weights have 24 bits. Errors as for ra_attend.
  * Calls on one handle share its workspace: calls that overlap in time on one handle race. The workspace grows with the sizes of the
  * calls, which cannot be done under capture: make a call of these sizes or larger before. A captured call stays good for
  * as long as the handle lives, whatever later calls need. */

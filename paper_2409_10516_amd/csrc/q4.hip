@@ -22,10 +22,12 @@
 //   sums    O[dimension][column] += V^T P. The lane's weights of the two halves are 8 consecutive slots of the contraction, so
 //           they go in as they come out; V^T wants for them, per dimension, the same 8 rows. Lane (kg, r) reads codes 8 r .. 8 r + 7 of
 //           these rows, four bytes each (16 lanes read a row): instruction m takes the m-th of each, dimension 8 r + m.
-// Codes become bfloat16 exactly. A float32 weight goes in as TERMS terms of bfloat16, the first as rounded, the next what the rounding
-// left, an instruction for each: 2 (16 bits) for bfloat16 over all tokens, else 3 (24 bits). Sparse sets are a few rows with all the
-// weight: with 16 bits their outputs were up to 1.2e-6 off (2-norm), with 24 bits 0.2e-6, for 2 % of the time; over all tokens 16 bits are
-// 0.7e-6 off, and 24 would be 2 to 7 % of the time. Float32 queries are three terms too. The sum of the weights is that of the terms (an
+// Codes become bfloat16 exactly. A float32 weight goes in as three terms of bfloat16, the first as rounded, the next what the rounding
+// left, an instruction for each: all of its 24 bits. Two (16 bits) are not enough: with a flat softmax (logits of deviation 1, bfloat16 queries) outputs
+// over 200, 2000 and 131072 tokens were 1.6, 1.8 and 2.2e-6 off (2-norm), with three 0.15, 0.18 and 0.50e-6; with logits of deviation 5, 0.42, 0.18
+// and 0.24e-6 and now 0.11, 0.18 and 0.21e-6; a sparse set, a few rows with all the weight, up to 1.2e-6 and now 0.2e-6. The third costs 2 to 4 % over all
+// tokens (131072 of 8 heads, 32 query heads, 31.8 -> 32.9 us, 16 sequences of up to 32768 61.6 -> 63.3), where 16 query heads share a KV head 7 % (a million tokens
+// 33.7 -> 36.0), and 2 % for a sparse set. Float32 queries are three terms too. The sum of the weights is that of the terms (an
 // instruction with a row of ones), so that what their rounding does to a weight that has nearly everything cancels.
 // Columns are heads, HEADS of them; where that is 8 or 4, two or four groups of columns have the same heads, and a lane makes the weights of
 // half or a quarter of its rows only (the others are zero): exponentials and splits are what vector instructions are short of,
@@ -43,9 +45,9 @@ struct Q4Chunk {
     uint32_t ks[2], v[8], vs[8];
 };
 
-template <int DT, int HEADS, int TERMS>
+template <int DT, int HEADS>
 struct Q4Wave {
-    static constexpr int QTERMS = DT == RA_BF16 ? 1 : 3;
+    static constexpr int TERMS = 3, QTERMS = DT == RA_BF16 ? 1 : 3;        // of weights and of queries
     static constexpr int SHARES = 16 / HEADS, MINE = 8 / SHARES;        // groups of columns; rows of a lane's 8 that are its own
     q4_bf16x8 q[QTERMS][4];
     q4_f32x4 acc[8], sum;       // weighted sums, and the sum of the weights as they went in, the same in all rows
@@ -253,8 +255,8 @@ struct Q4Lds { float a[Q4_WAVES][16][Q4_PAD], m[Q4_WAVES][16], l[Q4_WAVES][16]; 
 
 // The states of the wavefronts' columns -> one per head: f(head of the tile, dimension, sum, maximum, sum of weights), called by
 // one thread for each; a head without rows has the maximum -infinity.
-template <int DT, int HEADS, int TERMS, class Fn>
-__device__ __forceinline__ void q4_close(Q4Wave<DT, HEADS, TERMS>& s, Q4Lds& lds, int n, int tid, Fn f) {
+template <int DT, int HEADS, class Fn>
+__device__ __forceinline__ void q4_close(Q4Wave<DT, HEADS>& s, Q4Lds& lds, int n, int tid, Fn f) {
     constexpr int SHARES = 16 / HEADS;
     const int wv = tid / RA_WAVE, lane = tid & 63, kg = lane >> 4, col = lane & 15;
     const float l = s.sum[0];
@@ -434,7 +436,7 @@ __global__ __launch_bounds__(Q4_THREADS, DT == RA_BF16 ? 3 : 2) void q4_full_ker
         const int step = Q4_UNIT, rows = (int)(to - from);
         int row = __builtin_amdgcn_readfirstlane(wv) * Q4_CHUNK;
         const int last = row + (rows - Q4_CHUNK - row) / step * step;
-        Q4Wave<DT, HEADS, DT == RA_BF16 ? 2 : 3> s;
+        Q4Wave<DT, HEADS> s;
         Q4Chunk a, b;
         s.start(reinterpret_cast<const char*>(q) + head0 * RA_D * (DT == RA_BF16 ? 2 : 4), heads, lane);
         if (row + Q4_CHUNK <= rows) {
@@ -718,7 +720,7 @@ __global__ __launch_bounds__(Q4_THREADS, 3) void q4_attend_kernel(const void* __
                     c.vs + kv_head * c.kv_stride * Q4_BLOCKS, c.kv_stride};
     const Q4Rows src = om ? Q4Rows{ids + head0 * topk, N, 0, 0, topk} : Q4Rows{nullptr, N, s, w, (int)(s + N - w)};
     const int span = om ? spanG : spanS, from = part * span, to = from + span < src.count ? from + span : src.count;
-    Q4Wave<DT, HEADS, 3> st;
+    Q4Wave<DT, HEADS> st;
     st.start(reinterpret_cast<const char*>(q) + head0 * RA_D * (DT == RA_BF16 ? 2 : 4), heads, lane);
     // Whole chunks of W's rows behind the sink lie side by side, [lo, hi) in steps, and are read as over all tokens, the next one always on
     // its way; then all others (us, one sequence of 32 + 8 heads with 8644, 30644 and 100644 static rows 15.0, 19.9, 36 without, 11.4, 14.6, 28).
@@ -819,8 +821,8 @@ static int q4_heads(int group) { return group <= 4 ? 4 : group <= 8 ? 8 : 16; }
 // of 8000 and 504 of 200 17 and 46; 1024 of 16000 288 and 275, of 0 to 16000 189 and 160; 2048 of 20000 711 and 655. A job of its own costs what
 // the longest takes alone, 5 ns a row, hence the limit however many there are.
 // Otherwise three workgroups of bfloat16 fit a compute unit, two of float32; where few jobs share them, two leave fewer records to
-// combine (us, two and three: 8 jobs of 131072 rows 37.1, 38.0, one of a million 39.4, 40.5, 64 of 20011 33.9, 34.3, 128 of up to
-// 32768 64.2, 62.6).
+// combine (us, two and three: 8 jobs of 131072 rows 32.9, 33.9, one of a million 36.0, 40.3, 64 of 20011 38.1, 38.5; 128 of up to
+// 32768, with 16 bits of the weights, 64.2, 62.6).
 #define Q4_MOST_ROWS (1 << 24)      // of one job in a stretch: places in its codes fit 31 bits
 struct Q4Cut { int tiles, workgroups, unit_log2; bool whole, refused; };
 static Q4Cut q4_cut(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N) {
