@@ -181,7 +181,14 @@ __global__ __launch_bounds__(THREADS, 8) void append_kernel(AppendArgs a, int sp
                 double sum = 0.;
 #pragma unroll
                 for (int e = 0; e < VALS; ++e) sum = fma((double)v[e], (double)v[e], sum);
-                const float rinv = (float)rsqrt64(row_sum<LANES>(sum, lane) * (1. / RA_D) + a.eps);
+                double r64 = rsqrt64(row_sum<LANES>(sum, lane) * (1. / RA_D) + a.eps);
+                if (r64 > 0x1p100 || r64 < 0x1p-100) {             // (near or past float32's ends: the values take a part of it, exactly)
+                    const bool tiny = r64 > 1.;
+#pragma unroll
+                    for (int e = 0; e < VALS; ++e) v[e] *= tiny ? 0x1p64f : 0x1p-64f;
+                    r64 *= tiny ? 0x1p-64 : 0x1p64;
+                }
+                const float rinv = (float)r64;
 #pragma unroll
                 for (int f = 0; f < VALS / 4; ++f) {
                     const float4 w = s_w[which][VALS / 4 * l + f];
