@@ -342,7 +342,8 @@ ra_status ra_full_attention_q4(const void* q, ra_dtype dt, const uint8_t* K4, co
 /* ra_attend over a cache in 4 bits (what follows ra_search or ra_search_q8 where no other cache is kept): Eq. 2 over Omega = ids
  * and over W, their combination by Eq. 4-5 into out/lse, and the four partial outputs, each of which may be NULL. N >= the
  * index's N tokens are in the cache, N <= kv_stride; as in ra_decode_step_grown W = [0, sink) u [min(N - window, N_index), N).
- * ids must not contain members of W; -1 and ids >= N are skipped. Weights have 24 bits. Errors as for ra_attend.
+ * ids must not contain members of W; -1 and ids >= N are skipped. Weights have 24 bits. Errors as for ra_attend; a handle
+ * that does not live on the current device is refused (RA_EINVAL).
  * Calls on one handle share its workspace: calls that overlap in time on one handle race. The workspace grows with the sizes of the
  * calls, which cannot be done under capture: make a call of these sizes or larger before. A captured call stays good for
  * as long as the handle lives, whatever later calls need. */
@@ -362,7 +363,8 @@ ra_status ra_attend_q4(const void* q, const ra_index* idx, ra_dtype dt, const ui
  *   device),
  * 10 messages the handle's first search has sent to its workers so far, modulo 2^32: one for every step that was shared, one when
  *   the walk ended (0 where 9 can only be 0; synchronises the device),
- * 11 launches of ra_decode_step so far whose walks were to share their steps (one for a launch that is being recorded). */
+ * 11 launches of ra_decode_step so far whose walks were to share their steps (one for a launch that is being recorded),
+ * 12 the device that the handle lives on. */
 int64_t ra_index_info(const ra_index* idx, int what);
 
 /* Settings of the handle's decode path (host side; synchronises the device).

@@ -303,6 +303,11 @@ class Index:
         """(n_seq, n_q_heads, n_kv_heads), which a handle keeps for life."""
         return self.n_seq, self.n_q_heads, self.n_kv_heads
 
+    @functools.cached_property
+    def device(self):
+        """The index of the GPU it lives on."""
+        return self.info(12)
+
     def configure(self, what: int, value: int) -> None:
         """ra_index_configure: RA_CFG_HELPERS / RA_CFG_HELPER_SPIN / RA_CFG_SEEDS / RA_CFG_SEED_SHARES."""
         _check(_room(lib().ra_index_configure, self.handle, what, value))
@@ -726,6 +731,8 @@ def ra_attend_q4(q, idx: Index, k4, v4, sink: int, window: int, ids: torch.Tenso
     n_kv, shape = k4[0].shape[1], ids.shape
     if (n_seq, n_q, n_kv) != idx.heads or d != 128:
         raise ValueError("q must be [n_seq][n_q][128], and its heads and the cache's those of the index")
+    if idx.device != here:
+        raise ValueError(f"the index must live on the current GPU ({here}), not on {idx.device}")
     if ids.dtype is not torch.int32 or len(shape) != 3 or shape[0] != n_seq or shape[1] != n_q or not ids.is_contiguous() \
             or ids.get_device() != here:
         raise ValueError("ids must be contiguous int32 [n_seq][n_q][topk] on the current GPU")

@@ -318,6 +318,7 @@ extern "C" int64_t ra_index_info(const ra_index* ix, int what) {
             return sent;
         }
         case 11: return ix->walk_launches;
+        case 12: return ix->device;
         default: return -1;
     }
 }
@@ -907,6 +908,9 @@ extern "C" ra_status ra_attend_q4(const void* q, const ra_index* idx, ra_dtype d
     if (N > 0x7fffffff / 2 || kv_stride > 0x7fffffff / 2) RA_FAIL(RA_EUNSUP, "N or kv_stride too large");
     if (kv_stride < N) RA_FAIL(RA_ESHAPE, "kv_stride %lld is below N = %lld", (long long)kv_stride, (long long)N);
     RA_TRY(check_aligned(q, 16, "q"));
+    int here = 0;
+    RA_HIP(hipGetDevice(&here));
+    if (here != idx->device) RA_FAIL(RA_EINVAL, "the index is on device %d, the current one is %d", idx->device, here);
     ra_index* ix = const_cast<ra_index*>(idx);
     const size_t need = ra_attend_q4_partial_floats(dt, ix->n_seq, ix->n_q, ix->n_kv, N, ix->N, sink, window, topk) * sizeof(float);
     if (need > ix->q4_ws_bytes) {

@@ -66,3 +66,13 @@ def test_streams_of_another_device_are_refused(name):
     call, args = _good()[name]
     with pytest.raises(ValueError, match="current GPU"):
         call(**args, stream=_Elsewhere())
+
+
+def test_a_handle_of_another_device_is_refused():
+    call, args = _good()["attend"]
+    idx = args["idx"]
+    assert idx.device == torch.cuda.current_device() and idx.info(12) == idx.device
+    call(**args)
+    idx.__dict__["device"] = 7                      # (kept for a handle's life once it has been asked for)
+    with pytest.raises(ValueError, match="current GPU"):
+        call(**args)
