@@ -309,28 +309,32 @@ ra_status ra_decode_step_q8(const void* q, const ra_index* idx, const void* K, c
  *   K, V              caches [n_seq][n_kv_heads][kv_stride][128] of type dt, each may be NULL
  *   K4, K4s, V4, V4s  caches in 4 bits of capacity kv4_stride, codes and scale of each NULL or given: the rows of K and V (as
  *                     rounded to dt) in 4 bits. (An index is built over a K of exactly N rows; the cache beside it has room to grow.)
- * Outputs must not overlap inputs. Inputs, q_out, K and V 16-byte aligned, rows apart by a multiple of 16 bytes. */
+ * Outputs must not overlap inputs. Inputs, q_out, K and V 16-byte aligned, rows apart by a multiple of 16 bytes; q_row, k_row and v_row hold
+ * from one sequence's last token to the next one's first, too. RA_EUNSUP past 2^24 - 1 tokens (n_seq T), past 2^24 - 1 heads
+ * n_q_heads + 2 n_kv_heads of a token, and with up to 128 tokens past 2^24 - 1 workgroups, one for 16 heads of a token (float32: 8). Angles are
+ * reduced from magnitudes of up to 2^50. */
 ra_status ra_append_tokens(const void* q_in, const void* k_in, const void* v_in, ra_dtype dt, int n_seq, int n_q_heads,
                            int n_kv_heads, int64_t T, int d, int64_t q_row, int64_t k_row, int64_t v_row,
                            const void* q_weight, const void* k_weight, double eps, const float* inv_freq, int rot_dim,
                            int interleaved, const int32_t* first, const int32_t* n_new, int64_t kv_stride,
                            int64_t kv4_stride, void* stream, void* q_out, void* K, void* V, uint8_t* K4, uint8_t* K4s, uint8_t* V4, uint8_t* V4s);
 
-/* Rows into 4 bits: X [n_seq][n_kv_heads][T][128] (dt, 16-byte aligned) -> rows first[s] + t, t < n_new[s], of codes and scale. */
+/* Rows into 4 bits: X [n_seq][n_kv_heads][T][128] (dt, 16-byte aligned) -> rows first[s] + t, t < n_new[s], of codes and scale.
+ * RA_EUNSUP past 65535 heads n_seq x n_kv_heads. */
 ra_status ra_quantize_kv4(const void* X, ra_dtype dt, int n_seq, int n_kv_heads, int64_t T, int d, const int32_t* first,
                           const int32_t* n_new, int64_t kv_stride, void* stream, uint8_t* codes, uint8_t* scale);
 
 /* And back: rows first[s] + t, t < T -> X [n_seq][n_kv_heads][T][128] (dt, 16-byte aligned), the values they stand for, exactly
  * (bfloat16 and float32 hold all of them). Rows outside [0, kv_stride) come as zeroes. What an index is built
- * from again where the cache is kept in 4 bits only. */
+ * from again where the cache is kept in 4 bits only. RA_EUNSUP past 65535 heads n_seq x n_kv_heads. */
 ra_status ra_dequantize_kv4(const uint8_t* codes, const uint8_t* scale, ra_dtype dt, int n_seq, int n_kv_heads, int64_t T, int d,
                             const int32_t* first, int64_t kv_stride, void* stream, void* X);
 
 /* ra_full_attention over a cache in 4 bits: q [n_seq][n_q_heads][128] of type dt; rows [0, n) of sequence s, n =
  * min(n_tokens[s], N) (device int32; NULL: N for every sequence). A sequence without rows gets out = 0 and lse = -inf. Rows
  * from n on are not looked at. float32 accumulation; the weights of the softmax meet the values with all their 24 bits.
- * RA_EUNSUP where a workgroup's part of one head would pass 2^24 rows (hundreds of query heads per KV head over tens of millions of
- * tokens), and past 2^21 tiles of up to 16 query heads.
+ * RA_EUNSUP from 2^24 tiles of up to 16 query heads of a KV head on; over N > 2^24 tokens from 2^21 tiles on, and where a workgroup's
+ * part of one head would pass 2^24 rows (hundreds of query heads per KV head over tens of millions of tokens).
  * workspace: device memory of at least ra_full_attention_q4_workspace_bytes(...) bytes, 16-byte aligned, which nothing else may use
  * until the call has run; it needs no initialisation. */
 size_t ra_full_attention_q4_workspace_bytes(ra_dtype dt, int n_seq, int n_q_heads, int n_kv_heads, int64_t N);

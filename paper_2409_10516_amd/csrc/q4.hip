@@ -824,22 +824,27 @@ static int q4_heads(int group) { return group <= 4 ? 4 : group <= 8 ? 8 : 16; }
 // combine (us, two and three: 8 jobs of 131072 rows 32.9, 33.9, one of a million 36.0, 40.3, 64 of 20011 38.1, 38.5; 128 of up to
 // 32768, with 16 bits of the weights, 64.2, 62.6).
 #define Q4_MOST_ROWS (1 << 24)      // of one job in a stretch: places in its codes fit 31 bits
-struct Q4Cut { int tiles, workgroups, unit_log2; bool whole, refused; };
+struct Q4Cut { int tiles, workgroups, unit_log2; bool whole; const char* refused; };       // refused: why, or null
 static Q4Cut q4_cut(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N) {
     Q4Cut x;
     const int heads = q4_heads(n_q / n_kv);
     x.tiles = (int)(((int64_t)(n_q / n_kv) + heads - 1) / heads);
     const int64_t jobs = (int64_t)n_seq * n_kv * x.tiles;
-    x.whole = N <= 1024 || N <= (jobs < 2048 ? 16 * jobs : 32768) || (jobs > Q4_MOST_UNITS && N <= Q4_MOST_ROWS);
+    // (from Q4_MOST_UNITS jobs on there is no list: its units, and the threads of the second kernel, 128 for each of up to 16 heads, fit 32 bits)
+    x.whole = N <= 1024 || N <= (jobs < 2048 ? 16 * jobs : 32768) || (jobs >= Q4_MOST_UNITS && N <= Q4_MOST_ROWS);
     x.unit_log2 = 7;
     static_assert(Q4_UNIT == 1 << 7, "rows of a unit");
+    x.refused = x.whole && jobs >= 1 << 24 ? "too many heads for one launch: 2^24 tiles of up to 16 query heads"
+                : !x.whole && jobs >= Q4_MOST_UNITS ? "too many heads for one launch: 2^21 tiles of up to 16 query heads over more than 2^24 tokens" : nullptr;
+    x.workgroups = (int)jobs;
+    if (x.whole || x.refused) return x;
     auto units = [&] { return jobs * ((N + ((int64_t)1 << x.unit_log2) - 1) >> x.unit_log2); };
-    while (!x.whole && jobs <= Q4_MOST_UNITS && units() > Q4_MOST_UNITS) ++x.unit_log2;
-    x.refused = (x.whole ? jobs : 0) >= 1 << 24 || (!x.whole && jobs > Q4_MOST_UNITS);
+    while (units() > Q4_MOST_UNITS) ++x.unit_log2;
     const int most = jobs <= 64 || dt == RA_F32 ? Q4_MOST_WORKGROUPS / 3 * 2 : Q4_MOST_WORKGROUPS;
-    x.workgroups = (int)(x.whole ? (x.refused ? 0 : jobs) : units() < most ? units() : most);
+    x.workgroups = (int)(units() < most ? units() : most);
     // (a stretch is longest with all sequences at their longest; only very many query heads of one KV head get here)
-    if (!x.whole && !x.refused && N > Q4_MOST_ROWS) x.refused = ((units() / x.workgroups + 1) << x.unit_log2) > Q4_MOST_ROWS;
+    if (N > Q4_MOST_ROWS && ((units() / x.workgroups + 1) << x.unit_log2) > Q4_MOST_ROWS)
+        x.refused = "too many heads for one launch: a workgroup's part of one would pass 2^24 rows";
     return x;
 }
 
@@ -852,7 +857,7 @@ size_t ra_full_q4_partial_floats(ra_dtype dt, int n_seq, int n_q, int n_kv, int6
 ra_status ra_launch_full_q4(const void* q, ra_dtype dt, const Q4Cache& c, int n_seq, int n_q, int n_kv, int64_t N,
                             const int32_t* n_tokens, float* partials, hipStream_t st, float* out, float* lse) {
     const Q4Cut x = q4_cut(dt, n_seq, n_q, n_kv, N);
-    if (x.refused) RA_FAIL(RA_EUNSUP, "too many heads for one launch");
+    if (x.refused) RA_FAIL(RA_EUNSUP, "%s", x.refused);
 #define Q4_GO(DTV, HV)                                                                                                         \
     hipLaunchKernelGGL((q4_full_kernel<DTV, HV>), dim3(x.workgroups), dim3(Q4_THREADS), 0, st, q, c, n_seq, n_q, n_kv, (int)N, n_tokens, \
                        x.tiles, x.unit_log2, (int)x.whole, partials, out, lse)

@@ -76,3 +76,17 @@ def test_a_handle_of_another_device_is_refused():
     idx.__dict__["device"] = 7                      # (kept for a handle's life once it has been asked for)
     with pytest.raises(ValueError, match="current GPU"):
         call(**args)
+
+
+@pytest.mark.parametrize("n_kv", [32767, 65535])
+def test_conversions_take_as_many_heads_as_they_say(n_kv):
+    """n_seq x n_kv_heads up to 65535; one more is refused."""
+    X = torch.randn((1, n_kv, 2, 128), generator=torch.Generator(device=DEV).manual_seed(n_kv), device=DEV)
+    x4 = ra.ra_quantize_kv4(X)
+    back = ra.ra_dequantize_kv4(x4, torch.float32)
+    for h in (0, 1, n_kv // 2, n_kv - 1):
+        one = ra.ra_quantize_kv4(X[:, h:h + 1].contiguous())
+        assert all(torch.equal(a[:, h:h + 1], b) for a, b in zip(x4, one))
+        assert torch.equal(ra.ra_dequantize_kv4(one, torch.float32), back[:, h:h + 1])
+    with pytest.raises(ra.RaError, match="65535"):
+        ra.ra_quantize_kv4(torch.zeros((2, 32768, 1, 128), device=DEV))
