@@ -917,7 +917,16 @@ size_t ra_attend_q4_partial_floats(ra_dtype, int n_seq, int n_q, int n_kv, int64
     return (size_t)n_seq * n_q * (p.nS + p.nG) * Q4_REC;
 }
 
-#define Q4_TICKET_RECORDS 1024
+// Whether a head's last workgroup combines its records, or a second launch, which costs 1 us, does. That workgroup reads past the L2, eight
+// records at a time and two heads side by side, for all heads of a tile that it was the last of; and storing and drawing tickets costs each
+// workgroup something. So: up to 4 heads to a tile, three trips of eight records, fewer than 2048 records in all (us, second launch and
+// tickets. 32 + 8 heads, 7 records a head, of 1, 4 and 8 sequences 8.2, 7.3, 10.5, 9.8, 12.3, 11.4; 13 records, of 1 and 4 sequences 8.9, 7.9, 11.7, 10.4; 3 or 4
+// records, of 12, 16, 24 and 32 sequences 13.1, 12.5, 14.2, 13.8, 18.9, 19.6, 22.2, 24.0; 4 heads of one KV head, 13, 21, 29, 41, 64 and 127 records 8.5,
+// 7.7, 8.3, 8.2, 8.3, 8.8, 8.4, 9.3, 8.4, 11.0, 9.3, 16.4; 32 + 8 heads, 21 and 29 records 8.8, 9.2, 9.0, 12.9; 8 heads of one KV head, 7
+// records, of 1 and 16 sequences 7.9, 7.4 to 8.4, 9.1, 9.7 to 10.6; 16 of one, 7 and 64 records 8.7, 18.5, 9.4, 50.9).
+#define Q4_TICKET_HEADS 4
+#define Q4_TICKET_TRIPS 3
+#define Q4_TICKET_RECORDS 2048
 
 ra_status ra_launch_attend_q4(const void* q, ra_dtype dt, const Q4Cache& c, int n_seq, int n_q, int n_kv, int64_t N, int64_t Ng,
                               int sink, int window, int topk, const int32_t* ids, float* partials, uint32_t* tickets,
@@ -927,7 +936,8 @@ ra_status ra_launch_attend_q4(const void* q, ra_dtype dt, const Q4Cache& c, int 
     const Q4Parts p = q4_parts(n_seq, n_q, n_kv, s + N - w, topk);
     const int64_t blocks = (int64_t)n_seq * n_kv * (p.tiles * p.nS + n_q / n_kv * p.nG);
     if (blocks > (1 << 24) - 1) RA_FAIL(RA_EUNSUP, "too many heads for one launch");
-    if ((int64_t)n_seq * n_q * (p.nS + p.nG) > Q4_TICKET_RECORDS) tickets = nullptr;
+    const int trips = (p.nS + 7) / 8 + (p.nG + 7) / 8;
+    if (n_q / n_kv > Q4_TICKET_HEADS || trips > Q4_TICKET_TRIPS || (int64_t)n_seq * n_q * (p.nS + p.nG) >= Q4_TICKET_RECORDS) tickets = nullptr;
     const Q4Out o{tickets, out, lse, o_omega, lse_omega, o_w, lse_w};
 #define Q4_GO(DTV, TK)                                                                                                          \
     hipLaunchKernelGGL((q4_attend_kernel<DTV, Q4_ATTEND_HEADS, TK>), dim3((unsigned)blocks), dim3(Q4_THREADS), 0, st, q, c, n_q, n_kv, N, s, w, \
@@ -939,7 +949,7 @@ ra_status ra_launch_attend_q4(const void* q, ra_dtype dt, const Q4Cache& c, int 
     if (tickets) return RA_OK;
     // (eight records are on their way at a time. 16 heads of one KV head, 100640 static rows in 394 records: 44 us with one thread per
     // dimension, 19 with eight; 24 records 26.7 and 27.3)
-    if ((p.nS + 7) / 8 + (p.nG + 7) / 8 <= 3) hipLaunchKernelGGL(q4_merge_kernel<1>, dim3(n_seq * n_q), dim3(RA_D), 0, st, partials, p.nS, p.nG, o);
+    if (trips <= 3) hipLaunchKernelGGL(q4_merge_kernel<1>, dim3(n_seq * n_q), dim3(RA_D), 0, st, partials, p.nS, p.nG, o);
     else hipLaunchKernelGGL(q4_merge_kernel<8>, dim3(n_seq * n_q), dim3(RA_D * 8), 0, st, partials, p.nS, p.nG, o);
     RA_HIP(hipGetLastError());
     return RA_OK;

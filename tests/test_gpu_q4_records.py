@@ -79,9 +79,10 @@ def test_a_nan_row_in_a_late_record(case, dtype):
 
 SPARSE = [
     # n_seq, n_q, n_kv, N, index covers, sink, window, topk
-    (1, 4, 1, 20011, 500, 4, 17, 9),            # in the same launch
-    (1, 16, 1, 40001, 3001, 4, 640, 100),       # by a second one, many records: eight threads a dimension
+    (1, 4, 1, 20011, 500, 4, 17, 9),            # by a second launch, many records: eight threads a dimension
+    (1, 16, 1, 40001, 3001, 4, 640, 100),       # the same, of 16 heads together
     (40, 16, 2, 2100, 300, 3, 20, 50),          # by a second one, two records
+    (20, 4, 2, 5000, 300, 4, 17, 9),            # in the same launch, 13 records of a few heads each
 ]
 
 
