@@ -576,8 +576,9 @@ def ra_append_tokens(q, k, v, first, *, n_new=None, q_weight=None, k_weight=None
                      interleaved: bool = False, q_out=None, K=None, V=None, k4=None, v4=None, stream=None):
     """The tokens that enter a cache: norm of every query and key head (weight [128], None: no norm), rotation of the first
     2 * len(inv_freq) dimensions at positions first[s] + t, new rows of the caches. q, k, v: [n_seq][T][heads][128] (any may be
-    None), the heads of a token side by side, tokens any multiple of 16 bytes apart, so that they may be parts of one buffer. first,
-    n_new: int32 [n_seq] on the GPU (None: 0, and T). K, V: caches [n_seq][n_kv][capacity][128]; k4, v4: caches in 4 bits, of a
+    None), the heads of a token side by side, tokens any multiple of 16 bytes apart, so that they may be parts of one buffer; one
+    distance for all tokens, from a sequence's last to the next one's first, too (a slice of several tokens of each of several sequences is
+    copied first). first, n_new: int32 [n_seq] on the GPU (None: 0, and T). K, V: caches [n_seq][n_kv][capacity][128]; k4, v4: caches in 4 bits, of a
     capacity of their own, (codes, scale) as from ra_quantize_kv4. -> q_out [n_seq][n_q][T][128] (None without q); where tokens are fewer
     than T and no q_out is given, the rows behind the last one are zero."""
     some = q if q is not None else k if k is not None else v

@@ -432,7 +432,9 @@ __global__ __launch_bounds__(Q4_THREADS, DT == RA_BF16 ? 3 : 2) void q4_full_ker
         const Q4Cache h{c.k + kv_head * c.kv_stride * Q4_ROW, c.ks + kv_head * c.kv_stride * Q4_BLOCKS,
                         c.v + kv_head * c.kv_stride * Q4_ROW, c.vs + kv_head * c.kv_stride * Q4_BLOCKS, c.kv_stride};
         // whole chunks, then the last, if it is not. Loads are not branched around (the counts of what is on its way would have to
-        // hold for both ways, and every chunk would wait for the next one's loads): past the end it is the last chunk again.
+        // hold for both ways, and every chunk would wait for the next one's loads): past the end it is the last chunk again. That is so for
+        // bfloat16. With float32 queries the compiler puts the next chunk's loads behind the first products of the current one and a wait for all of
+        // that one's, values included, and a head's queries, split into terms, are waited for in two groups before its first rows are asked for.
         const int step = Q4_UNIT, rows = (int)(to - from);
         int row = __builtin_amdgcn_readfirstlane(wv) * Q4_CHUNK;
         const int last = row + (rows - Q4_CHUNK - row) / step * step;
@@ -602,8 +604,8 @@ __device__ __forceinline__ int q4_row(const Q4Rows& src, int r) {
     }
     return r >= src.count ? -1 : r < src.s ? r : (int)(src.w - src.s) + r;
 }
-// rows [at, at + 32) of a job; returns which of the lane's rows there are. Loads are never branched around: a row that is
-// not there is row 0.
+// rows [at, at + 32) of a job; returns which of the lane's rows there are. Loads of rows are not branched around: a row that is
+// not there is row 0. (Its ids are: as compiled, a lane's ten are read and waited for one after another, nearly all from the nearest cache.)
 __device__ __forceinline__ uint32_t q4_gather(Q4Chunk& c, const Q4Cache& h, const Q4Rows& src, int at, int lane) {
     const int kg = lane >> 4, r = lane & 15;
     int kr[2], vr[8];
@@ -723,7 +725,8 @@ __global__ __launch_bounds__(Q4_THREADS, 3) void q4_attend_kernel(const void* __
     Q4Wave<DT, HEADS> st;
     st.start(reinterpret_cast<const char*>(q) + head0 * RA_D * (DT == RA_BF16 ? 2 : 4), heads, lane);
     // Whole chunks of W's rows behind the sink lie side by side, [lo, hi) in steps, and are read as over all tokens, the next one always on
-    // its way; then all others (us, one sequence of 32 + 8 heads with 8644, 30644 and 100644 static rows 15.0, 19.9, 36 without, 11.4, 14.6, 28).
+    // its way (with float32 queries asked for as late as in q4_full_kernel); then all others (us, one sequence of 32 + 8 heads with 8644,
+    // 30644 and 100644 static rows 15.0, 19.9, 36 without, 11.4, 14.6, 28). Where everything is static there is no such part: all rows are others.
     const int step = Q4_WAVES * Q4_CHUNK, mine = from + wv * Q4_CHUNK;
     int lo = mine, hi = mine;
     if (!om) {
@@ -816,10 +819,11 @@ static int q4_heads(int group) { return group <= 4 ? 4 : group <= 8 ? 8 : 16; }
     } while (0)
 
 // How a call is cut: tiles of query heads per KV head, workgroups, and whether each has a job of its own. That is so where a head's rows are
-// few or the jobs many: shared out, 512 rows of 8 jobs take 8.7 us and by themselves 6.9, 1000 rows 8.9 and 9.5 (and a launch less on the host's
-// side), 2000 rows 8.9 and 14.0; 128 jobs of 2000 rows 16.8 and 15.4, of 4000 21.7 and 24.3; 512 of 8000 79 and 75, of 0 to 8000 70 and 54, one
-// of 8000 and 504 of 200 17 and 46; 1024 of 16000 288 and 275, of 0 to 16000 189 and 160; 2048 of 20000 711 and 655. A job of its own costs what
-// the longest takes alone, 5 ns a row, hence the limit however many there are.
+// few or the jobs many. Shared out and by themselves, us: 512 rows of 8 jobs 8.8, 7.0, 1000 rows 9.0, 9.8 (and a launch less on the host's
+// side), 2000 rows 8.9, 15.2; 128 jobs of 2000 rows 17.3, 16.5, of 4000 22.1, 26.7, of 8000 32.1, 47.8; 512 of 8000 107, 99.5, of 0 to 8000 70, 67; 1024
+// of 16000 388, 375, of 0 to 16000 235, 244; 2048 of 20000 927, 886. The price is what a job costs that is longer than the others: it takes 5 ns a
+// row alone, hence the limit however many there are. 8 jobs of 8000 rows (one sequence) beside 504 of 200 take 18.8 shared out and 47 by themselves: the
+// lengths are known on the device only, and this goes by the capacity.
 // Otherwise three workgroups of bfloat16 fit a compute unit, two of float32; where few jobs share them, two leave fewer records to
 // combine (us, two and three: 8 jobs of 131072 rows 32.9, 33.9, one of a million 36.0, 40.3, 64 of 20011 38.1, 38.5; 128 of up to
 // 32768, with 16 bits of the weights, 64.2, 62.6).
