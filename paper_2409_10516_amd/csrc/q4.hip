@@ -825,8 +825,8 @@ static int q4_heads(int group) { return group <= 4 ? 4 : group <= 8 ? 8 : 16; }
 // row alone, hence the limit however many there are. 8 jobs of 8000 rows (one sequence) beside 504 of 200 take 18.8 shared out and 47 by themselves: the
 // lengths are known on the device only, and this goes by the capacity.
 // Otherwise three workgroups of bfloat16 fit a compute unit, two of float32; where few jobs share them, two leave fewer records to
-// combine (us, two and three: 8 jobs of 131072 rows 32.9, 33.9, one of a million 36.0, 40.3, 64 of 20011 38.1, 38.5; 128 of up to
-// 32768, with 16 bits of the weights, 64.2, 62.6).
+// combine (us, two and three: 8 jobs of 131072 rows 32.9, 33.9, one of a million 36.0, 40.3, 64 of 20011 38.1, 38.5, 128 of up to
+// 32768 64.5, 62.8).
 #define Q4_MOST_ROWS (1 << 24)      // of one job in a stretch: places in its codes fit 31 bits
 struct Q4Cut { int tiles, workgroups, unit_log2; bool whole; const char* refused; };       // refused: why, or null
 static Q4Cut q4_cut(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N) {
