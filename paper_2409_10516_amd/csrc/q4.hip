@@ -5,13 +5,12 @@
 // z log2(e), the sum of weights), and a head's records are combined by a second kernel or by whoever stores the last. Weights are powers of two,
 // p = 2^(c <q, k> - m) with c = log2(e) / sqrt(d): one multiply-add and one instruction each.
 #include "q4_dev.h"
+#include "records.h"
 #include "ticket.h"
 
 #define Q4_THREADS 256
-#define Q4_REC (RA_D + 4)           // floats of a record: sums, maximum, sum of weights, 2 pad
 #define Q4_PART 128                 // rows of a part of the sparse set
 #define Q4_C ((float)(1.4426950408889634 / 11.313708498984761))
-#define Q4_LN2 0.6931471805599453f
 
 // ---- chunks of 32 rows on the matrix cores ---------------------------------------------------
 // A wavefront takes 32 rows at a time for a tile of query heads of one KV head, two products of v_mfma_f32_16x16x32_bf16
@@ -301,94 +300,6 @@ __device__ __forceinline__ void q4_close(Q4Wave<DT, HEADS>& s, Q4Lds& lds, int n
 // A launch of as many workgroups as jobs (`whole`) gives each its job, and the workgroup writes the result.
 #define Q4_UNIT (Q4_WAVES * Q4_CHUNK)
 #define Q4_MOST_UNITS (1u << 21)    // times the workgroups, below 2^32
-#define Q4_LEAST_UNITS 2u           // units that are worth a workgroup
-#define Q4_MOST_WORKGROUPS 768      // three per compute unit
-// over the 64 lanes: the sum, in all of them, and the sums up to each
-__device__ __forceinline__ uint32_t q4_sum64(uint32_t x, int lane) {
-    x += lane_xor32<1>(x, lane); x += lane_xor32<2>(x, lane); x += lane_xor32<4>(x, lane);
-    x += lane_xor32<8>(x, lane); x += lane_xor32<16>(x, lane); x += lane_xor32<32>(x, lane);
-    return (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
-}
-__device__ __forceinline__ uint32_t q4_scan64(uint32_t x) {
-#define Q4_STEP(CTRL, ROWS) x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xF, ROWS == 0xF)
-    Q4_STEP(0x111, 0xF); Q4_STEP(0x112, 0xF); Q4_STEP(0x114, 0xF); Q4_STEP(0x118, 0xF);     // within rows of 16
-    Q4_STEP(0x142, 0xA); Q4_STEP(0x143, 0xC);           // the row before's last to every second row, then the half before's
-#undef Q4_STEP
-    return x;
-}
-struct Q4List {
-    uint32_t units, first;          // of the whole list; before a sequence's jobs
-    int n;                          // rows of the sequence
-    uint32_t workgroups;            // that have a stretch
-    int rows;                       // rows of sequence `lane`
-
-    __device__ __forceinline__ uint32_t from(uint32_t wg) const { return units * wg / workgroups; }
-    __device__ __forceinline__ uint32_t owner(uint32_t unit) const { return ((unit + 1) * workgroups - 1) / units; }
-};
-__device__ __forceinline__ int q4_rows_of(const int32_t* n_tokens, int seq, int N) {
-    const int n = n_tokens ? n_tokens[seq] : N;
-    return n < 0 ? 0 : n < N ? n : N;
-}
-__device__ __forceinline__ uint32_t q4_units(int rows, int unit_log2) { return ((uint32_t)rows + (1u << unit_log2) - 1u) >> unit_log2; }
-// the list, and where sequence `seq`'s part of it begins; called by whole wavefronts, the same in all lanes
-__device__ __forceinline__ Q4List q4_list(const int32_t* n_tokens, int n_seq, int seq, int N, int unit_log2, uint32_t jobs, uint32_t grid) {
-    Q4List x;
-    x.rows = N;
-    if (!n_tokens) {
-        x.units = q4_units(N, unit_log2) * n_seq * jobs;
-        x.first = q4_units(N, unit_log2) * seq * jobs;
-        x.n = N;
-    } else if (n_seq == 1) {        // (a scalar load, and nothing to add up)
-        x.n = x.rows = q4_rows_of(n_tokens, 0, N);
-        x.units = q4_units(x.n, unit_log2) * jobs;
-        x.first = 0;
-    } else {
-        uint32_t all = 0, before = 0, mine = 0;
-        const int lane = threadIdx.x & 63;
-        for (int s0 = 0; s0 < n_seq; s0 += RA_WAVE) {
-            const int s = s0 + lane, rows = s < n_seq ? q4_rows_of(n_tokens, s, N) : 0;
-            const uint32_t u = q4_units(rows, unit_log2);
-            if (s0 == 0) x.rows = rows;
-            all += u;
-            before += s < seq ? u : 0u;
-            mine += s == seq ? (uint32_t)rows : 0u;
-        }
-        x.units = q4_sum64(all, lane) * jobs;
-        x.first = q4_sum64(before, lane) * jobs;
-        x.n = (int)q4_sum64(mine, lane);
-    }
-    const uint32_t most = (x.units + Q4_LEAST_UNITS - 1u) / Q4_LEAST_UNITS;
-    x.workgroups = most < grid ? most : grid;
-    return x;
-}
-// the sequence that has unit `unit` (one of the list's), and where its part begins
-__device__ __forceinline__ int q4_seq_of(const Q4List& x, const int32_t* n_tokens, int n_seq, int N, int unit_log2, uint32_t jobs,
-                                         uint32_t unit, uint32_t* first) {
-    if (n_seq == 1) {
-        *first = 0;
-        return 0;
-    }
-    if (!n_tokens) {
-        const uint32_t per = q4_units(N, unit_log2) * jobs, seq = unit / per;
-        *first = seq * per;
-        return (int)seq;
-    }
-    const int lane = threadIdx.x & 63;
-    uint32_t at = 0;
-    for (int s0 = 0;; s0 += RA_WAVE) {
-        const int s = s0 + lane;
-        const uint32_t u = q4_units(s0 == 0 ? x.rows : s < n_seq ? q4_rows_of(n_tokens, s, N) : 0, unit_log2);
-        const uint32_t upto = q4_scan64(u);
-        const unsigned long long past = __ballot(at + upto * jobs > unit);
-        if (past != 0ull || s0 + RA_WAVE >= n_seq) {
-            const int l = past != 0ull ? __ffsll(past) - 1 : 63;
-            *first = at + (uint32_t)__builtin_amdgcn_readlane((int)(upto - u), l) * jobs;
-            return s0 + l;
-        }
-        at += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63) * jobs;
-    }
-}
-
 template <int DT, int HEADS>
 __global__ __launch_bounds__(Q4_THREADS, DT == RA_BF16 ? 3 : 2) void q4_full_kernel(const void* __restrict__ q, Q4Cache c, int n_seq, int n_q,
                                                                                   int n_kv, int N, const int32_t* __restrict__ n_tokens,
@@ -398,21 +309,21 @@ __global__ __launch_bounds__(Q4_THREADS, DT == RA_BF16 ? 3 : 2) void q4_full_ker
     const int jobs = n_kv * tiles, group = n_q / n_kv, wg = blockIdx.x;
     uint32_t at = 0, end = 1, first = 0;
     int seq = wg / jobs;
-    Q4List x;
+    RowList x;
     if (!whole) {
-        x = q4_list(n_tokens, n_seq, 0, N, unit_log2, jobs, gridDim.x);
+        x = row_list(n_tokens, n_seq, 0, N, unit_log2, jobs, gridDim.x);
         if ((uint32_t)wg >= x.workgroups) return;
         at = x.from(wg);
         end = x.from(wg + 1);
-        seq = q4_seq_of(x, n_tokens, n_seq, N, unit_log2, jobs, at, &first);
+        seq = row_seq_of(x, n_tokens, n_seq, N, unit_log2, jobs, at, &first);
     }
     while (at < end) {
         // (what depends on the thread alone is worked out anew for each job: kept over the loop it takes 80 registers)
         int tid = threadIdx.x;
         asm volatile("" : "+v"(tid));
         const int lane = tid & 63, wv = tid / RA_WAVE;
-        const int n = whole || seq >= RA_WAVE ? q4_rows_of(n_tokens, seq, N) : __builtin_amdgcn_readlane(x.rows, seq);
-        const uint32_t units = q4_units(n, unit_log2);
+        const int n = whole || seq >= RA_WAVE ? seq_rows(n_tokens, seq, N) : __builtin_amdgcn_readlane(x.rows, seq);
+        const uint32_t units = row_units(n, unit_log2);
         int job = wg % jobs;
         uint32_t unit0 = 0, unit1 = units;
         if (!whole) {
@@ -467,7 +378,7 @@ __global__ __launch_bounds__(Q4_THREADS, DT == RA_BF16 ? 3 : 2) void q4_full_ker
                 if (d == 0) reinterpret_cast<float2*>(partials + HEADS * places * RA_D)[hd * places + place] = make_float2(mx, l);
             } else {
                 out[(head0 + hd) * RA_D + d] = mx > -INFINITY ? sum / l : 0.f;
-                if (d == 0) lse[head0 + hd] = mx > -INFINITY ? mx * Q4_LN2 + logf(l) : -INFINITY;
+                if (d == 0) lse[head0 + hd] = mx > -INFINITY ? mx * REC_LN2 + logf(l) : -INFINITY;
             }
         });
         if (whole) return;
@@ -482,8 +393,8 @@ __device__ __forceinline__ Q4Records q4_records(const float* partials, size_t he
                                                 const int32_t* n_tokens, int tiles, int unit_log2, int heads, int grid) {
     const int seq = (int)(head / n_q), group = n_q / n_kv, h = (int)(head % n_q), jobs = n_kv * tiles;
     const int job = h / group * tiles + h % group / heads;
-    const Q4List x = q4_list(n_tokens, n_seq, seq, N, unit_log2, jobs, grid);
-    const uint32_t units = q4_units(x.n, unit_log2);
+    const RowList x = row_list(n_tokens, n_seq, seq, N, unit_log2, jobs, grid);
+    const uint32_t units = row_units(x.n, unit_log2);
     int have = 0, wg0 = 0;
     if (units) {
         const uint32_t unit0 = x.first + job * units;
@@ -506,7 +417,7 @@ __global__ __launch_bounds__(THREADS) void q4_full_merge_kernel(const float* __r
                                                                          int unit_log2, int heads, int grid, float* __restrict__ out,
                                                                          float* __restrict__ lse) {
     constexpr int WAVES = THREADS / RA_WAVE, SL = THREADS / DIMS, FLY = DIMS == RA_D ? 16 : 32;
-    constexpr int MOST = DIMS == RA_D ? Q4_MOST_WORKGROUPS : Q4_MOST_WORKGROUPS / 3 * 2;       // records of a head
+    constexpr int MOST = DIMS == RA_D ? ROW_MOST_WORKGROUPS : ROW_MOST_WORKGROUPS / 3 * 2;       // records of a head
     constexpr int MINE = (MOST + THREADS - 1) / THREADS;                     // that a thread makes the weight of
     __shared__ float s_w[MINE * THREADS], s_m[WAVES], s_l[WAVES], s_a[SL][DIMS];
     const int tid = threadIdx.x, t = tid % DIMS, slice = tid / DIMS, lane = tid & 63;
@@ -582,15 +493,10 @@ __global__ __launch_bounds__(THREADS) void q4_full_merge_kernel(const float* __r
         for (int i = 1; i < SL; ++i) a += s_a[i][t];
     }
     out[head * RA_D + dim] = mx > -INFINITY ? a / ll : 0.f;
-    if (dim == 0) lse[head] = mx > -INFINITY ? mx * Q4_LN2 + logf(ll) : -INFINITY;
+    if (dim == 0) lse[head] = mx > -INFINITY ? mx * REC_LN2 + logf(ll) : -INFINITY;
 }
 
 // ---- the retrieved set and the static set -------------------------------------------------------
-struct Q4Out {
-    uint32_t* tickets;                  // one word per query head (ticket.h), or null
-    float *out, *lse, *o_om, *lse_om, *o_w, *lse_w;
-};
-
 // the rows of a job: ids of a head, or [0, s) and then from `w` on
 struct Q4Rows {
     const int32_t* ids;
@@ -630,82 +536,13 @@ __device__ __forceinline__ uint32_t q4_gather(Q4Chunk& c, const Q4Cache& h, cons
     return there;
 }
 
-template <bool COHERENT>
-__device__ __forceinline__ void q4_store(float* p, float v) {
-    if (COHERENT) __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    else *p = v;
-}
-template <bool COHERENT>
-__device__ __forceinline__ float q4_load(const float* p) {
-    return COHERENT ? __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : *p;
-}
-
-// Dimension d of a head's records [first, last), every `by`th: their maximum, sum of weights and weighted sum.
-struct Q4Sum { float m, l, a; };
-template <bool COHERENT>
-__device__ __forceinline__ Q4Sum q4_add_up(const float* rec, int first, int last, int by, int d) {
-    constexpr int FLY = 8;
-    Q4Sum x{-INFINITY, 0.f, 0.f};
-    for (int i0 = first; i0 < last; i0 += FLY * by) {
-        float m[FLY], l[FLY], a[FLY], mx = x.m;
-#pragma unroll
-        for (int u = 0; u < FLY; ++u) {
-            const float* y = rec + (size_t)(i0 + u * by < last ? i0 + u * by : i0) * Q4_REC;
-            m[u] = q4_load<COHERENT>(y + RA_D);
-            l[u] = q4_load<COHERENT>(y + RA_D + 1);
-            a[u] = q4_load<COHERENT>(y + d);
-        }
-#pragma unroll
-        for (int u = 0; u < FLY; ++u) mx = fmaxf(mx, m[u]);
-        if (mx == -INFINITY) continue;
-        const float corr = __builtin_amdgcn_exp2f(x.m - mx);
-        x.a *= corr;
-        x.l *= corr;
-#pragma unroll
-        for (int u = 0; u < FLY; ++u) {
-            const float w = i0 + u * by < last ? __builtin_amdgcn_exp2f(m[u] - mx) : 0.f;
-            x.a = fmaf(a[u], w, x.a);
-            x.l = fmaf(l[u], w, x.l);
-        }
-        x.m = mx;
-    }
-    return x;
-}
-// Eq. 4 for the static set and for Omega, Eq. 5 for both
-__device__ __forceinline__ void q4_write(const Q4Sum (&set)[2], size_t head, int d, const Q4Out& o) {
-    float* o_set[2] = {o.o_w, o.o_om};
-    float* l_set[2] = {o.lse_w, o.lse_om};
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const bool empty = set[i].m == -INFINITY;
-        if (o_set[i]) o_set[i][head * RA_D + d] = empty ? 0.f : set[i].a / set[i].l;
-        if (l_set[i] && d == 0) l_set[i][head] = empty ? -INFINITY : set[i].m * Q4_LN2 + logf(set[i].l);
-    }
-    const float mx = fmaxf(set[0].m, set[1].m);
-    float out = 0.f, lse = -INFINITY;
-    if (mx > -INFINITY) {
-        const float e0 = __builtin_amdgcn_exp2f(set[0].m - mx), e1 = __builtin_amdgcn_exp2f(set[1].m - mx);
-        const float l = set[0].l * e0 + set[1].l * e1;
-        out = (set[0].a * e0 + set[1].a * e1) / l;
-        lse = mx * Q4_LN2 + logf(l);
-    }
-    o.out[head * RA_D + d] = out;
-    if (d == 0) o.lse[head] = lse;
-}
-// dimension d of a head from its records, nS of the static set and nG of Omega
-template <bool COHERENT>
-__device__ __forceinline__ void q4_finish(const float* rec, int nS, int nG, size_t head, int d, const Q4Out& o) {
-    const Q4Sum set[2] = {q4_add_up<COHERENT>(rec, 0, nS, 1, d), q4_add_up<COHERENT>(rec, nS, nS + nG, 1, d)};
-    q4_write(set, head, d, o);
-}
-
 // grid: per (sequence, KV head) the parts of each of its query heads' Omega (their loads wait for ids, so they start first), then
 // the parts of the static set per tile of heads. `spanS`, `spanG`: rows of a part. TICKETS: the workgroup that stores a head's last
 // record combines them all (ticket.h), which saves a launch.
 template <int DT, int HEADS, bool TICKETS>
 __global__ __launch_bounds__(Q4_THREADS, 3) void q4_attend_kernel(const void* __restrict__ q, Q4Cache c, int n_q, int n_kv, int64_t N,
                                                                int64_t s, int64_t w, int topk, const int32_t* __restrict__ ids, int nS,
-                                                               int nG, int spanS, int spanG, int tiles, float* partials, Q4Out o) {
+                                                               int nG, int spanS, int spanG, int tiles, float* partials, SetOut o) {
     __shared__ Q4Lds lds;
     __shared__ uint32_t s_last[HEADS];
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid / RA_WAVE);
@@ -758,9 +595,9 @@ __global__ __launch_bounds__(Q4_THREADS, 3) void q4_attend_kernel(const void* __
         st.template add<false>(ch, there, lane);
     }
     q4_close(st, lds, heads, tid, [&](int hd, int d, float sum, float mx, float l) {
-        float* rec = partials + ((head0 + hd) * P + slot) * Q4_REC;
-        q4_store<TICKETS>(rec + d, sum);
-        if (d == 0) { q4_store<TICKETS>(rec + RA_D, mx); q4_store<TICKETS>(rec + RA_D + 1, l); }
+        float* rec = partials + ((head0 + hd) * P + slot) * REC_FLOATS;
+        rec_put<TICKETS>(rec + d, sum);
+        if (d == 0) { rec_put<TICKETS>(rec + RA_D, mx); rec_put<TICKETS>(rec + RA_D + 1, l); }
     });
     if constexpr (TICKETS) {
         __builtin_amdgcn_s_waitcnt(0x0F70);     // vmcnt(0): this wavefront's record stores have completed
@@ -771,28 +608,28 @@ __global__ __launch_bounds__(Q4_THREADS, 3) void q4_attend_kernel(const void* __
         }
         __syncthreads();
         for (int y = tid; y < heads * RA_D; y += Q4_THREADS)
-            if (s_last[y / RA_D]) q4_finish<true>(partials + (head0 + y / RA_D) * P * Q4_REC, nS, nG, head0 + y / RA_D, y % RA_D, o);
+            if (s_last[y / RA_D]) rec_finish<true>(partials + (head0 + y / RA_D) * P * REC_FLOATS, nS, nG, head0 + y / RA_D, y % RA_D, o);
     }
 }
 
 // grid: x = head (with its sequence); SLICES threads per dimension take the records in turn
 template <int SLICES>
-__global__ __launch_bounds__(RA_D * SLICES) void q4_merge_kernel(const float* __restrict__ partials, int nS, int nG, Q4Out o) {
+__global__ __launch_bounds__(RA_D * SLICES) void q4_merge_kernel(const float* __restrict__ partials, int nS, int nG, SetOut o) {
     const size_t head = blockIdx.x;
-    const float* rec = partials + head * (nS + nG) * Q4_REC;
+    const float* rec = partials + head * (nS + nG) * REC_FLOATS;
     const int d = threadIdx.x % RA_D, slice = threadIdx.x / RA_D;
     if constexpr (SLICES == 1) {
-        q4_finish<false>(rec, nS, nG, head, d, o);
+        rec_finish<false>(rec, nS, nG, head, d, o);
     } else {
-        __shared__ Q4Sum s_part[SLICES][2][RA_D];
-        s_part[slice][0][d] = q4_add_up<false>(rec, slice, nS, SLICES, d);
-        s_part[slice][1][d] = q4_add_up<false>(rec, nS + slice, nS + nG, SLICES, d);
+        __shared__ RecSum s_part[SLICES][2][RA_D];
+        s_part[slice][0][d] = rec_add_up<false>(rec, slice, nS, SLICES, d);
+        s_part[slice][1][d] = rec_add_up<false>(rec, nS + slice, nS + nG, SLICES, d);
         __syncthreads();
         if (slice) return;
-        Q4Sum set[2];
+        RecSum set[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            Q4Sum x{-INFINITY, 0.f, 0.f};
+            RecSum x{-INFINITY, 0.f, 0.f};
 #pragma unroll
             for (int y = 0; y < SLICES; ++y) x.m = fmaxf(x.m, s_part[y][i][d].m);
             const float base = x.m > -INFINITY ? x.m : 0.f;
@@ -804,7 +641,7 @@ __global__ __launch_bounds__(RA_D * SLICES) void q4_merge_kernel(const float* __
             }
             set[i] = x;
         }
-        q4_write(set, head, d, o);
+        rec_write(set, head, d, o);
     }
 }
 
@@ -844,7 +681,7 @@ static Q4Cut q4_cut(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N) {
     if (x.whole || x.refused) return x;
     auto units = [&] { return jobs * ((N + ((int64_t)1 << x.unit_log2) - 1) >> x.unit_log2); };
     while (units() > Q4_MOST_UNITS) ++x.unit_log2;
-    const int most = jobs <= 64 || dt == RA_F32 ? Q4_MOST_WORKGROUPS / 3 * 2 : Q4_MOST_WORKGROUPS;
+    const int most = jobs <= 64 || dt == RA_F32 ? ROW_MOST_WORKGROUPS / 3 * 2 : ROW_MOST_WORKGROUPS;
     x.workgroups = (int)(units() < most ? units() : most);
     // (a stretch is longest with all sequences at their longest; only very many query heads of one KV head get here)
     if (N > Q4_MOST_ROWS && ((units() / x.workgroups + 1) << x.unit_log2) > Q4_MOST_ROWS)
@@ -858,6 +695,20 @@ size_t ra_full_q4_partial_floats(ra_dtype dt, int n_seq, int n_q, int n_kv, int6
 }
 
 #define Q4_FEW_RECORDS 32
+ra_status ra_launch_full_merge(const float* partials, int n_seq, int n_q, int n_kv, int64_t N, const int32_t* n_tokens, int tiles, int unit_log2,
+                               int heads, int workgroups, hipStream_t st, float* out, float* lse) {
+#define Q4_MERGE(THREADS, DIMS)                                                                                                                  \
+    hipLaunchKernelGGL((q4_full_merge_kernel<THREADS, DIMS>), dim3(n_seq * n_q * (RA_D / DIMS)), dim3(THREADS), 0, st, partials, n_seq, n_q, n_kv, \
+                       (int)N, n_tokens, tiles, unit_log2, heads, workgroups, out, lse)
+    // records per head, were all sequences as long as the longest
+    if (workgroups / (n_seq * n_kv * tiles) > Q4_FEW_RECORDS) Q4_MERGE(512, 32);
+    else if ((int64_t)n_seq * n_q <= 1024) Q4_MERGE(512, RA_D);
+    else Q4_MERGE(128, RA_D);
+#undef Q4_MERGE
+    RA_HIP(hipGetLastError());
+    return RA_OK;
+}
+
 ra_status ra_launch_full_q4(const void* q, ra_dtype dt, const Q4Cache& c, int n_seq, int n_q, int n_kv, int64_t N,
                             const int32_t* n_tokens, float* partials, hipStream_t st, float* out, float* lse) {
     const Q4Cut x = q4_cut(dt, n_seq, n_q, n_kv, N);
@@ -869,16 +720,7 @@ ra_status ra_launch_full_q4(const void* q, ra_dtype dt, const Q4Cache& c, int n_
 #undef Q4_GO
     RA_HIP(hipGetLastError());
     if (x.whole) return RA_OK;
-#define Q4_MERGE(THREADS, DIMS)                                                                                                                  \
-    hipLaunchKernelGGL((q4_full_merge_kernel<THREADS, DIMS>), dim3(n_seq * n_q * (RA_D / DIMS)), dim3(THREADS), 0, st, partials, n_seq, n_q, n_kv, \
-                       (int)N, n_tokens, x.tiles, x.unit_log2, q4_heads(n_q / n_kv), x.workgroups, out, lse)
-    // records per head, were all sequences as long as the longest
-    if (x.workgroups / (n_seq * n_kv * x.tiles) > Q4_FEW_RECORDS) Q4_MERGE(512, 32);
-    else if ((int64_t)n_seq * n_q <= 1024) Q4_MERGE(512, RA_D);
-    else Q4_MERGE(128, RA_D);
-#undef Q4_MERGE
-    RA_HIP(hipGetLastError());
-    return RA_OK;
+    return ra_launch_full_merge(partials, n_seq, n_q, n_kv, N, n_tokens, x.tiles, x.unit_log2, q4_heads(n_q / n_kv), x.workgroups, st, out, lse);
 }
 
 // W = [0, s) u [w, N) of Sec. 3.3, with what came after the index was built; ranges that meet make everything static
@@ -918,7 +760,7 @@ size_t ra_attend_q4_partial_floats(ra_dtype, int n_seq, int n_q, int n_kv, int64
     int64_t s, w;
     q4_static(N, Ng, sink, window, &s, &w);
     const Q4Parts p = q4_parts(n_seq, n_q, n_kv, s + N - w, topk);
-    return (size_t)n_seq * n_q * (p.nS + p.nG) * Q4_REC;
+    return (size_t)n_seq * n_q * (p.nS + p.nG) * REC_FLOATS;
 }
 
 // Whether a head's last workgroup combines its records, or a second launch, which costs 1 us, does. That workgroup reads past the L2, eight
@@ -942,7 +784,7 @@ ra_status ra_launch_attend_q4(const void* q, ra_dtype dt, const Q4Cache& c, int 
     if (blocks > (1 << 24) - 1) RA_FAIL(RA_EUNSUP, "too many heads for one launch");
     const int trips = (p.nS + 7) / 8 + (p.nG + 7) / 8;
     if (n_q / n_kv > Q4_TICKET_HEADS || trips > Q4_TICKET_TRIPS || (int64_t)n_seq * n_q * (p.nS + p.nG) >= Q4_TICKET_RECORDS) tickets = nullptr;
-    const Q4Out o{tickets, out, lse, o_omega, lse_omega, o_w, lse_w};
+    const SetOut o{tickets, out, lse, o_omega, lse_omega, o_w, lse_w};
 #define Q4_GO(DTV, TK)                                                                                                          \
     hipLaunchKernelGGL((q4_attend_kernel<DTV, Q4_ATTEND_HEADS, TK>), dim3((unsigned)blocks), dim3(Q4_THREADS), 0, st, q, c, n_q, n_kv, N, s, w, \
                        topk, ids, p.nS, p.nG, p.spanS, p.spanG, p.tiles, partials, o)
