@@ -356,6 +356,59 @@ ra_status ra_attend_q4(const void* q, const ra_index* idx, ra_dtype dt, const ui
                        const int32_t* ids, void* stream, float* out, float* lse, float* o_omega, float* lse_omega,
                        float* o_w, float* lse_w);
 
+/* ---- a cache in pages ----------------------------------------------------------------
+ *
+ * Sequences of unequal and growing length share a pool of pages: K, V [n_pages][n_kv_heads][page][128], `page` rows (a power of two) of
+ * every KV head of a token together. Row r of sequence s is slot r % page of page table[s][r / page]. An entry of the table outside
+ * [0, n_pages) is no page: its rows are neither read nor written, they are not attended, and come as zeroes where rows are gathered. So
+ * entries behind a sequence's last page may hold anything, a page that has been given back is marked by -1, and sequences may share
+ * the pages of a common beginning. (Two new tokens of one call must not have the same slot.) The table is device memory: it can
+ * change between the replays of a captured graph, as first, n_new, n_tokens and n_indexed can.
+ * RA_EUNSUP past RA_MAX_PAGE rows of a page, 2^31 - 1 rows of a pool (n_pages n_kv_heads page) or 2^30 - 1 of a sequence (table_pages page). */
+#define RA_MAX_PAGE 65536
+typedef struct {                    /* host memory, read before the call returns */
+    const void *K, *V;              /* device, 16-byte aligned; either may be NULL where a call does not use it */
+    const int32_t* table;           /* device [n_seq][table_pages], rows table_stride entries apart */
+    int64_t table_stride;
+    int32_t dt;                     /* ra_dtype of K and V, and of what is appended or attends */
+    int32_t n_seq, n_kv_heads, n_pages, page, table_pages;
+} ra_paged_cache;
+
+/* ra_append_tokens into a cache in pages: token t of sequence s is row first[s] + t of the sequence. Same norm and rotation, whose
+ * cosines and sines are multiplied by rot_scale (the factor that positions scaled for long contexts come with; 1: none; scaled
+ * frequencies are the caller's, in inv_freq). k_in and v_in may be NULL: nothing of K or V is written. Limits as for ra_append_tokens. */
+ra_status ra_append_tokens_paged(const void* q_in, const void* k_in, const void* v_in, const ra_paged_cache* cache, int n_q_heads,
+                                 int64_t T, int d, int64_t q_row, int64_t k_row, int64_t v_row, const void* q_weight, const void* k_weight,
+                                 double eps, const float* inv_freq, int rot_dim, int interleaved, float rot_scale,
+                                 const int32_t* first, const int32_t* n_new, void* stream, void* q_out);
+
+/* Rows first[s] + t, t < T, of K (values 0) or V (1) -> X [n_seq][n_kv_heads][T][128], side by side as ra_knn, ra_build_index,
+ * ra_quantize_keys and the walks read keys. Rows without a page come as zeroes (rows behind a sequence's last token, in its last page, as they are). */
+ra_status ra_gather_paged(const ra_paged_cache* cache, int values, int64_t T, int d, const int32_t* first, void* stream, void* X);
+
+/* ra_full_attention over a cache in pages: q [n_seq][n_q_heads][128] of type dt; rows [0, n) of sequence s that have a page, n =
+ * min(n_tokens[s], N) (device int32; NULL: N for every sequence), N <= table_pages page. A sequence without rows gets out = 0 and
+ * lse = -inf. Other rows are not looked at, whatever they hold. float32 accumulation; the weights of the softmax meet the values with all
+ * their 24 bits. With bfloat16, infinite values in rows that are attended come out as NaN.
+ * RA_EUNSUP from 2^24 tiles of up to 16 query heads of a KV head on, over N > 2^24 tokens from 2^21 on.
+ * workspace: device memory of at least ra_full_attention_paged_workspace_bytes(...) bytes, 16-byte aligned, which nothing else may use
+ * until the call has run; it needs no initialisation. */
+size_t ra_full_attention_paged_workspace_bytes(int n_seq, int n_q_heads, int n_kv_heads, int64_t N);
+ra_status ra_full_attention_paged(const void* q, const ra_paged_cache* cache, int n_q_heads, int64_t N, int d, const int32_t* n_tokens,
+                                  void* workspace, size_t workspace_bytes, void* stream, float* out, float* lse);
+
+/* ra_attend over a cache in pages (what follows ra_search or ra_search_q8 over gathered or 8-bit keys): Eq. 2 over Omega = ids and over W,
+ * their combination by Eq. 4-5 into out/lse, and the four partial outputs, each of which may be NULL. Lengths are each sequence's own:
+ * with n = min(n_tokens[s], N) and n_i = min(n_indexed[s], n) (device int32; NULL: N, and n) W = [0, sink) u [min(n - window, n_i), n):
+ * tokens behind the n_i that the index was built over are static. Entries of ids that are not in [0, n), or are members of W (they are
+ * attended there), are skipped; one that is given twice counts twice. Rows without a page are not attended. Weights have 24 bits.
+ * workspace: as above, of ra_attend_paged_workspace_bytes(...) bytes, `grows`: whether n_indexed is given. */
+size_t ra_attend_paged_workspace_bytes(int n_seq, int n_q_heads, int n_kv_heads, int64_t N, int grows, int sink, int window, int topk);
+ra_status ra_attend_paged(const void* q, const ra_paged_cache* cache, int n_q_heads, int64_t N, int d, const int32_t* n_tokens,
+                          const int32_t* n_indexed, int sink, int window, int topk, const int32_t* ids, void* workspace,
+                          size_t workspace_bytes, void* stream, float* out, float* lse, float* o_omega, float* lse_omega, float* o_w,
+                          float* lse_w);
+
 /* what: 0 n_seq, 1 n_q_heads, 2 n_kv_heads, 3 N, 4 deg, 5 bytes of device memory owned,
  * 6 whether ra_decode_step will use helper workgroups (1 / 0; synchronises the device),
  * 7 the seed-set size in use (RA_CFG_SEEDS; 0: single entry point),

@@ -38,6 +38,12 @@ class RaError(RuntimeError):
         self.status = status
 
 
+class _PagedCache(C.Structure):
+    """ra_paged_cache"""
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("table", C.c_void_p), ("table_stride", C.c_int64), ("dt", C.c_int32), ("n_seq", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("n_pages", C.c_int32), ("page", C.c_int32), ("table_pages", C.c_int32)]
+
+
 _lib = None
 
 
@@ -127,6 +133,19 @@ def lib() -> C.CDLL:
     L.ra_full_attention_q4.restype = i32
     L.ra_attend_q4.argtypes = [vp, vp, i32, vp, vp, vp, vp, i64, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]
     L.ra_attend_q4.restype = i32
+    cache = C.POINTER(_PagedCache)
+    L.ra_append_tokens_paged.argtypes = [vp, vp, vp, cache, i32, i64, i32, i64, i64, i64, vp, vp, C.c_double, vp, i32, i32, C.c_float, vp, vp, vp, vp]
+    L.ra_append_tokens_paged.restype = i32
+    L.ra_gather_paged.argtypes = [cache, i32, i64, i32, vp, vp, vp]
+    L.ra_gather_paged.restype = i32
+    L.ra_full_attention_paged_workspace_bytes.argtypes = [i32, i32, i32, i64]
+    L.ra_full_attention_paged_workspace_bytes.restype = C.c_size_t
+    L.ra_full_attention_paged.argtypes = [vp, cache, i32, i64, i32, vp, vp, C.c_size_t, vp, vp, vp]
+    L.ra_full_attention_paged.restype = i32
+    L.ra_attend_paged_workspace_bytes.argtypes = [i32, i32, i32, i64, i32, i32, i32, i32]
+    L.ra_attend_paged_workspace_bytes.restype = C.c_size_t
+    L.ra_attend_paged.argtypes = [vp, cache, i32, i64, i32, vp, vp, i32, i32, i32, vp, vp, C.c_size_t, vp, vp, vp, vp, vp, vp, vp]
+    L.ra_attend_paged.restype = i32
     for name in ("ra_knn", "ra_project", "ra_build_index", "ra_search", "ra_attend",
                  "ra_attend_noalloc", "ra_hbm_read_probe", "ra_hbm_gather_probe", "ra_decode_step", "ra_index_import",
                  "ra_index_export"):
@@ -749,4 +768,194 @@ def ra_attend_q4(q, idx: Index, k4, v4, sink: int, window: int, ids: torch.Tenso
     _check(_room(lib().ra_attend_q4, q_at, idx.handle, _dt(q), K4, K4s, V4, V4s, room if N is None else N, room, sink, window, shape[2],
                  ids.data_ptr(), _handle(stream, here), out.data_ptr(), lse.data_ptr(),
                  *([t.data_ptr() for t in extra] or (None, None, None, None))))
+    return (out, lse, *extra) if partials else (out, lse)
+
+
+class PagedCache:
+    """A cache in pages: K, V [n_pages][n_kv][page][128] (float32 or bfloat16, page a power of two; one of them may be None) and the
+    table int32 [n_seq][table_pages] whose entry [s][r // page] is the page of row r of sequence s (outside [0, n_pages): none). Tensors of the
+    current GPU, which stay the caller's: their contents, the table's among them, may change at any time, in stream order. Checked here, once."""
+
+    def __init__(self, K, V, table):
+        self._here = torch.cuda.current_device()
+        some = K if K is not None else V
+        if some is None:
+            raise ValueError("K or V is needed")
+        dt, shape = _dt(some), some.shape
+        for t in (K, V):
+            if t is not None and (t.dim() != 4 or t.shape != shape or t.shape[3] != 128 or not t.is_contiguous()):
+                raise ValueError("K and V must be contiguous [n_pages][n_kv][page][128], of one shape")
+            if t is not None and t.dtype is not some.dtype:
+                raise TypeError("K and V must share a dtype")
+        if table.dtype is not torch.int32 or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
+            raise ValueError("table must be an int32 tensor [n_seq][table_pages] whose rows are contiguous")
+        _here(K, V, table)
+        # (the stride of a dimension of one element says nothing)
+        stride = table.stride(0) if table.shape[0] > 1 else table.shape[1]
+        if stride < table.shape[1]:
+            raise ValueError("the rows of the table must not overlap")
+        self._K, self._V, self._table, self._some = K, V, table, some
+        self._at = _ptr(K), _ptr(V), table.data_ptr()
+        self._c = _PagedCache(*self._at, stride, dt, table.shape[0], shape[1], shape[0], shape[2], table.shape[1])
+        self._ref = C.byref(self._c)
+        self._dt, self._dtype, self._n_seq, self._n_kv, self._rows = dt, some.dtype, table.shape[0], shape[1], table.shape[1] * shape[2]
+
+    K = property(lambda s: s._K)
+    V = property(lambda s: s._V)
+    table = property(lambda s: s._table)
+    n_seq = property(lambda s: s._n_seq)
+    n_kv_heads = property(lambda s: s._n_kv)
+    page = property(lambda s: s._c.page)
+    rows = property(lambda s: s._rows, doc="Rows that a row of the table has entries for.")
+    dtype = property(lambda s: s._dtype)
+
+    def _of(self, here: int):
+        """What a call passes on, the tensors being where they were."""
+        if here != self._here:
+            raise ValueError(f"the cache must live on the current GPU ({here}), not on {self._here}")
+        if self._at != (_ptr(self._K), _ptr(self._V), self._table.data_ptr()):
+            raise ValueError("the cache's tensors have been given other memory: make another PagedCache")
+        return self._ref
+
+
+def ra_append_tokens_paged(q, k, v, first, cache: PagedCache, *, n_new=None, q_weight=None, k_weight=None, eps: float = 1e-6, inv_freq=None,
+                           interleaved: bool = False, rot_scale: float = 1.0, q_out=None, stream=None):
+    """ra_append_tokens into a cache in pages; cosines and sines times rot_scale. k and v may be None: nothing of K or V is
+    written. -> q_out [n_seq][n_q][T][128] (None without q), as there."""
+    some = q if q is not None else k if k is not None else v
+    if some is None:
+        raise ValueError("at least one of q, k and v is needed")
+    here = torch.cuda.current_device()
+    room_for = _for(stream, here)
+    ref = cache._of(here)
+    dtype, shape, n_seq, n_kv = cache._dtype, some.shape, cache._n_seq, cache._n_kv
+    if len(shape) != 4:
+        raise ValueError("q, k and v must be [n_seq][T][heads][128]")
+    T = shape[1]
+    if q is not None:
+        q_at, n_q, q_row = _token_rows(q, n_seq, T, dtype, here)
+    else:
+        q_at, n_q, q_row = None, n_kv, 0
+    k_at, n_k, k_row = _token_rows(k, n_seq, T, dtype, here) if k is not None else (None, n_kv, 0)
+    v_at, n_v, v_row = _token_rows(v, n_seq, T, dtype, here) if v is not None else (None, n_kv, 0)
+    if n_k != n_kv or n_v != n_kv:
+        raise ValueError("k and v must have the heads of the cache")
+    qw_at = _vector(q_weight, 128, dtype, here, "q_weight") if q_weight is not None else None
+    kw_at = _vector(k_weight, 128, dtype, here, "k_weight") if k_weight is not None else None
+    f_at, rot = None, 0
+    if inv_freq is not None:
+        rot = 2 * inv_freq.numel()
+        f_at = _vector(inv_freq, rot // 2, torch.float32, here, "inv_freq")
+    first_at = _vector(first, n_seq, torch.int32, here, "first") if first is not None else None
+    new_at = _vector(n_new, n_seq, torch.int32, here, "n_new") if n_new is not None else None
+    out_at = None
+    if q is None:
+        if q_out is not None:
+            raise ValueError("q_out goes with q")
+    else:
+        if q_out is None:
+            with room_for:
+                q_out = (torch.empty if n_new is None else torch.zeros)(n_seq, n_q, T, 128, dtype=dtype, device=here)
+        elif q_out.dtype is not dtype or q_out.shape != (n_seq, n_q, T, 128) or not q_out.is_contiguous() or q_out.get_device() != here:
+            raise ValueError("q_out must be contiguous [n_seq][n_q][T][128], of the dtype of q and where q is")
+        out_at = q_out.data_ptr()
+    _check(lib().ra_append_tokens_paged(q_at, k_at, v_at, ref, n_q, T, 128, q_row, k_row, v_row, qw_at, kw_at, eps, f_at, rot,
+                                        1 if interleaved else 0, rot_scale, first_at, new_at, _handle(stream, here), out_at))
+    return q_out
+
+
+def ra_gather_paged(cache: PagedCache, values: bool = False, first=None, rows: Optional[int] = None, out=None, stream=None):
+    """Rows first[s] .. first[s] + rows (None: from 0, all that the table has entries for) of K, or with `values` of V, side by side
+    -> [n_seq][n_kv][rows][128]; rows without a page are zero."""
+    here = torch.cuda.current_device()
+    room_for = _for(stream, here)
+    ref = cache._of(here)
+    shape = (cache._n_seq, cache._n_kv, cache._rows if rows is None else rows, 128)
+    if out is None:
+        with room_for:
+            out = torch.empty(shape, dtype=cache._dtype, device=here)
+    elif out.dtype is not cache._dtype or out.shape != shape or not out.is_contiguous() or out.get_device() != here:
+        raise ValueError("out must be contiguous [n_seq][n_kv][rows][128], of the cache's dtype and where it is")
+    _check(lib().ra_gather_paged(ref, 1 if values else 0, shape[2], 128, None if first is None else _vector(first, shape[0], torch.int32, here, "first"),
+                                 _handle(stream, here), out.data_ptr()))
+    return out
+
+
+def _paged_query(q, cache: PagedCache, here: int):
+    """Checks q -> its address, query heads and dimensions."""
+    q_at, n_seq, n_q, d = _query(q, here)
+    if n_seq != cache._n_seq:
+        raise ValueError(f"q has {n_seq} sequences, the table {cache._n_seq}")
+    if q.dtype is not cache._dtype:
+        raise TypeError("q and the cache must share a dtype")
+    return q_at, n_q, d
+
+
+def _workspace(given, need: int, room_for, here: int):
+    """The given workspace, or a new one of `need` bytes -> (it, its bytes)."""
+    if given is None:
+        need = max(1, need)
+        with room_for:
+            return torch.empty(need, dtype=torch.uint8, device=here), need
+    _dev(given)
+    _here(given)
+    return given, given.numel() * given.element_size()
+
+
+@functools.lru_cache(maxsize=256)
+def _full_paged_room(n_seq: int, n_q: int, n_kv: int, N: int) -> int:
+    """ra_full_attention_paged_workspace_bytes, a function of sizes alone."""
+    return lib().ra_full_attention_paged_workspace_bytes(n_seq, n_q, n_kv, N)
+
+
+def ra_full_attention_paged(q, cache: PagedCache, n_tokens=None, N: Optional[int] = None, stream=None, workspace=None, out=None, lse=None):
+    """Eq. 1 over the first n_tokens[s] rows (int32 [n_seq] on the GPU, at most N; None: N, by default cache.rows) of every sequence of a
+    cache in pages, those that have a page -> (out float32 [n_seq][n_q][128], lse float32 [n_seq][n_q])."""
+    here = torch.cuda.current_device()
+    room_for = _for(stream, here)
+    ref = cache._of(here)
+    q_at, n_q, d = _paged_query(q, cache, here)
+    n_seq = cache._n_seq
+    N = cache._rows if N is None else N
+    workspace, have = _workspace(workspace, 0 if workspace is not None else _full_paged_room(n_seq, n_q, cache._n_kv, N), room_for, here)
+    with room_for:
+        out, lse = _results(n_seq, n_q, d, here, out, lse)
+    _check(lib().ra_full_attention_paged(q_at, ref, n_q, N, d, None if n_tokens is None else _vector(n_tokens, n_seq, torch.int32, here, "n_tokens"),
+                                         workspace.data_ptr(), have, _handle(stream, here), out.data_ptr(), lse.data_ptr()))
+    return out, lse
+
+
+@functools.lru_cache(maxsize=256)
+def _attend_paged_room(n_seq: int, n_q: int, n_kv: int, N: int, grows: bool, sink: int, window: int, topk: int) -> int:
+    """ra_attend_paged_workspace_bytes, a function of sizes alone."""
+    return lib().ra_attend_paged_workspace_bytes(n_seq, n_q, n_kv, N, grows, sink, window, topk)
+
+
+def ra_attend_paged(q, cache: PagedCache, sink: int, window: int, ids: torch.Tensor, n_tokens=None, n_indexed=None, N: Optional[int] = None,
+                    stream=None, partials: bool = False, workspace=None, out=None, lse=None):
+    """ra_attend over a cache in pages, of n_tokens[s] rows (int32 [n_seq] on the GPU, at most N; None: N, by default cache.rows), the first
+    n_indexed[s] of which (None: all) an index was built over; those behind are static. ids in the static set are
+    skipped. -> (out, lse) or, with partials=True, (out, lse, o_omega, lse_omega, o_w, lse_w)."""
+    here = torch.cuda.current_device()
+    room_for = _for(stream, here)
+    ref = cache._of(here)
+    q_at, n_q, d = _paged_query(q, cache, here)
+    n_seq, shape = cache._n_seq, ids.shape
+    if ids.dtype is not torch.int32 or len(shape) != 3 or shape[0] != n_seq or shape[1] != n_q or not ids.is_contiguous() \
+            or ids.get_device() != here:
+        raise ValueError("ids must be contiguous int32 [n_seq][n_q][topk] on the current GPU")
+    N = cache._rows if N is None else N
+    need = 0 if workspace is not None else _attend_paged_room(n_seq, n_q, cache._n_kv, N, n_indexed is not None, sink, window, shape[2])
+    workspace, have = _workspace(workspace, need, room_for, here)
+    extra = ()
+    with room_for:
+        out, lse = _results(n_seq, n_q, d, here, out, lse)
+        if partials:
+            f = dict(dtype=torch.float32, device=here)
+            extra = (torch.empty((n_seq, n_q, d), **f), torch.empty((n_seq, n_q), **f),
+                     torch.empty((n_seq, n_q, d), **f), torch.empty((n_seq, n_q), **f))
+    _check(lib().ra_attend_paged(q_at, ref, n_q, N, d, None if n_tokens is None else _vector(n_tokens, n_seq, torch.int32, here, "n_tokens"),
+                                 None if n_indexed is None else _vector(n_indexed, n_seq, torch.int32, here, "n_indexed"), sink, window, shape[2],
+                                 ids.data_ptr(), workspace.data_ptr(), have, _handle(stream, here), out.data_ptr(), lse.data_ptr(),
+                                 *([t.data_ptr() for t in extra] or (None, None, None, None))))
     return (out, lse, *extra) if partials else (out, lse)

@@ -4,6 +4,7 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <cmath>
 #include <new>
 
 #include "common.h"
@@ -808,6 +809,28 @@ static ra_status check_rows(int n_seq, int n_kv, int64_t T, int64_t kv_stride) {
     return RA_OK;
 }
 
+static ra_status check_rotation(const float* inv_freq, int rot_dim) {
+    if (rot_dim < 0 || rot_dim > RA_D) RA_FAIL(RA_EINVAL, "rot_dim %d outside [0, %d]", rot_dim, RA_D);
+    if (rot_dim % 16) RA_FAIL(RA_EUNSUP, "rot_dim %d is not a multiple of 16", rot_dim);
+    if (rot_dim && !inv_freq) RA_FAIL(RA_EINVAL, "NULL argument: inv_freq");
+    return RA_OK;
+}
+
+static ra_status check_token_rows(const AppendArgs& a, ra_dtype dt) {
+    if ((a.weight[0] || a.weight[1]) && !(a.eps >= 0.)) RA_FAIL(RA_EINVAL, "eps must be non-negative");
+    const size_t esz = dt == RA_BF16 ? 2 : 4;
+    for (int i = 0; i < 3; ++i) {
+        RA_TRY(check_aligned(a.in[i], 16, "an input"));
+        RA_TRY(check_aligned(a.out[i], 16, "q_out, K or V"));
+        const int64_t least = (int64_t)(i ? a.n_kv : a.n_q) * RA_D;
+        if (a.in[i] && a.row[i] < least)
+            RA_FAIL(RA_ESHAPE, "tokens are %lld elements apart, their heads take %lld", (long long)a.row[i], (long long)least);
+        if (a.in[i] && a.row[i] * esz % 16) RA_FAIL(RA_EUNSUP, "tokens are %lld elements apart: not a multiple of 16 bytes", (long long)a.row[i]);
+    }
+    for (int i = 0; i < 2; ++i) RA_TRY(check_aligned(a.weight[i], esz, "a weight"));
+    return RA_OK;
+}
+
 extern "C" ra_status ra_append_tokens(const void* q_in, const void* k_in, const void* v_in, ra_dtype dt, int n_seq, int n_q,
                                       int n_kv, int64_t T, int d, int64_t q_row, int64_t k_row, int64_t v_row,
                                       const void* q_weight, const void* k_weight, double eps, const float* inv_freq, int rot_dim,
@@ -826,22 +849,10 @@ extern "C" ra_status ra_append_tokens(const void* q_in, const void* k_in, const 
     if (!v_in != (!V && !V4)) RA_FAIL(RA_EINVAL, "v_in goes with V or its 4-bit form");
     if (K4) RA_TRY(check_q4(K4, K4s, "K"));
     if (V4) RA_TRY(check_q4(V4, V4s, "V"));
-    if (rot_dim < 0 || rot_dim > RA_D) RA_FAIL(RA_EINVAL, "rot_dim %d outside [0, %d]", rot_dim, RA_D);
-    if (rot_dim % 16) RA_FAIL(RA_EUNSUP, "rot_dim %d is not a multiple of 16", rot_dim);
-    if (rot_dim && !inv_freq) RA_FAIL(RA_EINVAL, "NULL argument: inv_freq");
-    if ((q_weight || k_weight) && !(eps >= 0.)) RA_FAIL(RA_EINVAL, "eps must be non-negative");
-    const size_t esz = dt == RA_BF16 ? 2 : 4;
+    RA_TRY(check_rotation(inv_freq, rot_dim));
     AppendArgs a{{q_in, k_in, v_in}, {q_weight, k_weight}, {q_row, k_row, v_row}, {q_out, K, V}, {K4, V4}, {K4s, V4s},
                  inv_freq, first, n_new, eps, T, {kv_stride, kv4_stride}, n_seq, n_q, n_kv, rot_dim, interleaved != 0};
-    for (int i = 0; i < 3; ++i) {
-        RA_TRY(check_aligned(a.in[i], 16, "an input"));
-        RA_TRY(check_aligned(a.out[i], 16, "q_out, K or V"));
-        const int64_t least = (int64_t)(i ? n_kv : n_q) * RA_D;
-        if (a.in[i] && a.row[i] < least)
-            RA_FAIL(RA_ESHAPE, "tokens are %lld elements apart, their heads take %lld", (long long)a.row[i], (long long)least);
-        if (a.in[i] && a.row[i] * esz % 16) RA_FAIL(RA_EUNSUP, "tokens are %lld elements apart: not a multiple of 16 bytes", (long long)a.row[i]);
-    }
-    for (int i = 0; i < 2; ++i) RA_TRY(check_aligned(a.weight[i], esz, "a weight"));
+    RA_TRY(check_token_rows(a, dt));
     return ra_launch_append(a, dt, (hipStream_t)stream);
 }
 
@@ -927,4 +938,117 @@ extern "C" ra_status ra_attend_q4(const void* q, const ra_index* idx, ra_dtype d
     }
     return ra_launch_attend_q4(q, dt, Q4Cache{K4, K4s, V4, V4s, kv_stride}, ix->n_seq, ix->n_q, ix->n_kv, N, ix->N, sink, window, topk,
                                ids, ix->q4_ws, attend_tickets(ix), (hipStream_t)stream, out, lse, o_omega, lse_omega, o_w, lse_w);
+}
+
+// ---- a cache in pages ---------------------------------------------------------------------
+// `need`: bit 0 K, bit 1 V
+static ra_status check_paged(const ra_paged_cache* c, int need, PgCache* out) {
+    if (!c) RA_FAIL(RA_EINVAL, "NULL argument: the cache");
+    RA_TRY(check_dtype((ra_dtype)c->dt));
+    if (c->n_seq < 1 || c->n_kv_heads < 1 || c->n_pages < 1 || c->table_pages < 1)
+        RA_FAIL(RA_EINVAL, "n_seq, n_kv_heads, n_pages and table_pages must be positive");
+    if (c->page < 1) RA_FAIL(RA_EINVAL, "page must be positive");
+    if (c->page > RA_MAX_PAGE || (c->page & (c->page - 1))) RA_FAIL(RA_EUNSUP, "a page of %d rows: not a power of two up to %d", c->page, RA_MAX_PAGE);
+    if (!c->table) RA_FAIL(RA_EINVAL, "NULL argument: the table");
+    if ((need & 1) && !c->K) RA_FAIL(RA_EINVAL, "NULL argument: K");
+    if ((need & 2) && !c->V) RA_FAIL(RA_EINVAL, "NULL argument: V");
+    if (c->table_stride < c->table_pages)
+        RA_FAIL(RA_ESHAPE, "table_stride %lld is below table_pages = %d", (long long)c->table_stride, c->table_pages);
+    if ((int64_t)c->n_pages * c->page > 0x7fffffff || (int64_t)c->n_pages * c->page * c->n_kv_heads > 0x7fffffff)
+        RA_FAIL(RA_EUNSUP, "more than 2^31 - 1 rows in a pool");
+    if ((int64_t)c->table_pages * c->page > 0x7fffffff / 2) RA_FAIL(RA_EUNSUP, "more than 2^30 - 1 rows of a sequence");
+    RA_TRY(check_aligned(c->K, 16, "K"));
+    RA_TRY(check_aligned(c->V, 16, "V"));
+    RA_TRY(check_aligned(c->table, 4, "the table"));
+    *out = PgCache{c->K, c->V, c->table, c->table_stride, c->n_pages, __builtin_ctz((unsigned)c->page), c->table_pages};
+    return RA_OK;
+}
+
+extern "C" ra_status ra_append_tokens_paged(const void* q_in, const void* k_in, const void* v_in, const ra_paged_cache* cache, int n_q, int64_t T,
+                                            int d, int64_t q_row, int64_t k_row, int64_t v_row, const void* q_weight, const void* k_weight,
+                                            double eps, const float* inv_freq, int rot_dim, int interleaved, float rot_scale,
+                                            const int32_t* first, const int32_t* n_new, void* stream, void* q_out) {
+    PgCache c;
+    RA_TRY(check_paged(cache, (k_in ? 1 : 0) | (v_in ? 2 : 0), &c));
+    const ra_dtype dt = (ra_dtype)cache->dt;
+    const int n_seq = cache->n_seq, n_kv = cache->n_kv_heads;
+    RA_TRY(check_heads(n_seq, n_q, n_kv));
+    RA_TRY(check_dim(d));
+    RA_TRY(check_rows(n_seq, n_kv, T, cache->page));
+    if (!q_in && !k_in && !v_in) RA_FAIL(RA_EINVAL, "NULL argument: no input");
+    if (!q_in != !q_out) RA_FAIL(RA_EINVAL, "q_in and q_out go together");
+    RA_TRY(check_rotation(inv_freq, rot_dim));
+    if (!std::isfinite(rot_scale)) RA_FAIL(RA_EINVAL, "rot_scale must be finite");
+    AppendArgs a{{q_in, k_in, v_in}, {q_weight, k_weight}, {q_row, k_row, v_row},
+                 {q_out, k_in ? const_cast<void*>(cache->K) : nullptr, v_in ? const_cast<void*>(cache->V) : nullptr}, {nullptr, nullptr},
+                 {nullptr, nullptr}, inv_freq, first, n_new, eps, T, {cache->page, 1}, n_seq, n_q, n_kv, rot_dim, interleaved != 0};
+    RA_TRY(check_token_rows(a, dt));
+    return ra_launch_append_paged(a, c, rot_scale, dt, (hipStream_t)stream);
+}
+
+extern "C" ra_status ra_gather_paged(const ra_paged_cache* cache, int values, int64_t T, int d, const int32_t* first, void* stream, void* X) {
+    PgCache c;
+    RA_TRY(check_paged(cache, values ? 2 : 1, &c));
+    RA_TRY(check_dim(d));
+    if (!X) RA_FAIL(RA_EINVAL, "NULL argument");
+    RA_TRY(check_rows(cache->n_seq, cache->n_kv_heads, T, 1));
+    RA_TRY(check_aligned(X, 16, "X"));
+    return ra_launch_gather_paged(c, values ? cache->V : cache->K, (ra_dtype)cache->dt, cache->n_seq, cache->n_kv_heads, T, first,
+                                  (hipStream_t)stream, X);
+}
+
+// N rows of a sequence at most
+static ra_status check_paged_rows(const ra_paged_cache* c, int64_t N) {
+    if (N < 1) RA_FAIL(RA_EINVAL, "N must be positive");
+    if (N > (int64_t)c->table_pages * c->page)
+        RA_FAIL(RA_ESHAPE, "N = %lld is above the %lld rows that a row of the table has pages for", (long long)N, (long long)c->table_pages * c->page);
+    return RA_OK;
+}
+
+extern "C" size_t ra_full_attention_paged_workspace_bytes(int n_seq, int n_q, int n_kv, int64_t N) {
+    if (check_heads(n_seq, n_q, n_kv) != RA_OK || N < 1 || N > 0x7fffffff / 2) return 0;
+    return 256 + ra_full_paged_partial_floats(n_seq, n_q, n_kv, N) * sizeof(float);
+}
+
+extern "C" ra_status ra_full_attention_paged(const void* q, const ra_paged_cache* cache, int n_q, int64_t N, int d, const int32_t* n_tokens,
+                                             void* workspace, size_t workspace_bytes, void* stream, float* out, float* lse) {
+    if (!q || !out || !lse || !workspace) RA_FAIL(RA_EINVAL, "NULL argument");
+    PgCache c;
+    RA_TRY(check_paged(cache, 3, &c));
+    const int n_seq = cache->n_seq, n_kv = cache->n_kv_heads;
+    RA_TRY(check_heads(n_seq, n_q, n_kv));
+    RA_TRY(check_dim(d));
+    RA_TRY(check_paged_rows(cache, N));
+    RA_TRY(check_aligned(q, 16, "q"));
+    RA_TRY(check_aligned(workspace, 16, "workspace"));
+    if (workspace_bytes < ra_full_attention_paged_workspace_bytes(n_seq, n_q, n_kv, N))
+        RA_FAIL(RA_ESHAPE, "workspace of %zu B is smaller than ra_full_attention_paged_workspace_bytes", workspace_bytes);
+    return ra_launch_full_paged(q, (ra_dtype)cache->dt, c, n_seq, n_q, n_kv, N, n_tokens, (float*)workspace, (hipStream_t)stream, out, lse);
+}
+
+extern "C" size_t ra_attend_paged_workspace_bytes(int n_seq, int n_q, int n_kv, int64_t N, int grows, int sink, int window, int topk) {
+    if (check_heads(n_seq, n_q, n_kv) != RA_OK || N < 1 || N > 0x7fffffff / 2 || sink < 0 || window < 0 || topk < 1 || topk > RA_MAX_TOPK) return 0;
+    return 256 + ra_attend_paged_partial_floats(n_seq, n_q, n_kv, N, grows != 0, sink, window, topk) * sizeof(float);
+}
+
+extern "C" ra_status ra_attend_paged(const void* q, const ra_paged_cache* cache, int n_q, int64_t N, int d, const int32_t* n_tokens,
+                                     const int32_t* n_indexed, int sink, int window, int topk, const int32_t* ids, void* workspace,
+                                     size_t workspace_bytes, void* stream, float* out, float* lse, float* o_omega, float* lse_omega, float* o_w,
+                                     float* lse_w) {
+    if (!q || !ids || !out || !lse || !workspace) RA_FAIL(RA_EINVAL, "NULL argument");
+    PgCache c;
+    RA_TRY(check_paged(cache, 3, &c));
+    const int n_seq = cache->n_seq, n_kv = cache->n_kv_heads;
+    RA_TRY(check_heads(n_seq, n_q, n_kv));
+    RA_TRY(check_dim(d));
+    RA_TRY(check_paged_rows(cache, N));
+    if (sink < 0 || window < 0) RA_FAIL(RA_EINVAL, "sink and window must be non-negative");
+    if (topk < 1) RA_FAIL(RA_EINVAL, "topk must be positive");
+    if (topk > RA_MAX_TOPK) RA_FAIL(RA_EUNSUP, "topk %d exceeds RA_MAX_TOPK %d", topk, RA_MAX_TOPK);
+    RA_TRY(check_aligned(q, 16, "q"));
+    RA_TRY(check_aligned(workspace, 16, "workspace"));
+    if (workspace_bytes < ra_attend_paged_workspace_bytes(n_seq, n_q, n_kv, N, n_indexed != nullptr, sink, window, topk))
+        RA_FAIL(RA_ESHAPE, "workspace of %zu B is smaller than ra_attend_paged_workspace_bytes", workspace_bytes);
+    return ra_launch_attend_paged(q, (ra_dtype)cache->dt, c, n_seq, n_q, n_kv, N, n_tokens, n_indexed, sink, window, topk, ids, (float*)workspace,
+                                  (hipStream_t)stream, out, lse, o_omega, lse_omega, o_w, lse_w);
 }

@@ -172,6 +172,13 @@ struct Q4Cache {
     const uint8_t *k, *ks, *v, *vs;
     int64_t kv_stride;
 };
+// a cache in pages [n_pages][n_kv][1 << page_log2][128]; rows of the table are table_stride entries apart
+struct PgCache {
+    const void *k, *v;
+    const int32_t* table;
+    int64_t table_stride;
+    int n_pages, page_log2, table_pages;
+};
 struct AppendArgs {
     const void *in[3], *weight[2];          // q, k, v; q's and k's
     int64_t row[3];                         // elements from token to token
@@ -184,6 +191,17 @@ struct AppendArgs {
     int n_seq, n_q, n_kv, rot, interleaved;
 };
 ra_status ra_launch_append(const AppendArgs& a, ra_dtype dt, hipStream_t st);
+// the same with K and V in the pages of `pages` (of `a`, out[1] and out[2] only say whether there are any); cosines and sines times rot_scale
+ra_status ra_launch_append_paged(const AppendArgs& a, const PgCache& pages, float rot_scale, ra_dtype dt, hipStream_t st);
+ra_status ra_launch_gather_paged(const PgCache& c, const void* pages, ra_dtype dt, int n_seq, int n_kv, int64_t T, const int32_t* first,
+                                 hipStream_t st, void* X);
+size_t ra_full_paged_partial_floats(int n_seq, int n_q, int n_kv, int64_t N);
+ra_status ra_launch_full_paged(const void* q, ra_dtype dt, const PgCache& c, int n_seq, int n_q, int n_kv, int64_t N, const int32_t* n_tokens,
+                               float* partials, hipStream_t st, float* out, float* lse);
+size_t ra_attend_paged_partial_floats(int n_seq, int n_q, int n_kv, int64_t N, bool grows, int sink, int window, int topk);
+ra_status ra_launch_attend_paged(const void* q, ra_dtype dt, const PgCache& c, int n_seq, int n_q, int n_kv, int64_t N, const int32_t* n_tokens,
+                                 const int32_t* n_indexed, int sink, int window, int topk, const int32_t* ids, float* partials, hipStream_t st,
+                                 float* out, float* lse, float* o_omega, float* lse_omega, float* o_w, float* lse_w);
 ra_status ra_launch_quantize_kv4(const void* X, ra_dtype dt, int n_seq, int n_kv, int64_t T, const int32_t* first,
                                  const int32_t* n_new, int64_t kv_stride, hipStream_t st, uint8_t* codes, uint8_t* scale);
 ra_status ra_launch_dequantize_kv4(const uint8_t* codes, const uint8_t* scale, ra_dtype dt, int n_seq, int n_kv, int64_t T,

@@ -1,4 +1,4 @@
-// Tokens that enter a cache: norms of queries and keys per head, position rotation, the new rows (ra_append_tokens), and
+// Tokens that enter a cache: norms of queries and keys per head, position rotation, the new rows (ra_append_tokens, ra_append_tokens_paged), and
 // rows into 4 bits and back (ra_quantize_kv4, ra_dequantize_kv4). All of it moves rows: a lane has 16 bytes of one, 8 values of bfloat16 in
 // 16 lanes or 4 of float32 in 32, so that an instruction reads or writes whole lines (float32 rows in 16 lanes, two instructions
 // for halves of a line's every 32 bytes: 32674 x 5 x 2 of them into 4 bits and back 99.7 us). A block of 32 dimensions is four or eight lanes, and
@@ -130,8 +130,9 @@ __device__ __forceinline__ void turn(float (&v)[VALS], const float2 (&cs)[VALS],
 // 206, 223, 248, 283 of then 192; that 192 had a branch and a wait for shared memory per rotated value, with a branch around
 // both sides of a rotation it was 165. Two, four, eight or 16 tokens side by side in a workgroup 197, 200, 200, 205 of 192. With 512
 // threads 211, 768 273 (a turn that is not full is a longer one).
-template <int DT, int THREADS, bool ONCE>
-__global__ __launch_bounds__(THREADS, 8) void append_kernel(AppendArgs a, int split) {
+// PAGED: a token's K and V rows of all KV heads lie in one page, `page` rows from head to head; the page is asked for with the angles.
+template <int DT, int THREADS, bool ONCE, bool PAGED>
+__global__ __launch_bounds__(THREADS, 8) void append_kernel(AppendArgs a, int split, PgCache pages, float rot_scale) {
     __shared__ float2 s_cs[RA_D / 2];
     __shared__ float4 s_w[2][RA_D / 4];
     constexpr int VALS = KV_VALS<DT>, LANES = KV_LANES<DT>, GROUPS = THREADS / LANES;
@@ -140,15 +141,27 @@ __global__ __launch_bounds__(THREADS, 8) void append_kernel(AppendArgs a, int sp
     const int T = (int)a.T, tok = blockIdx.x / split, seq = tok / T, t = tok % T;
     if (a.n_new && t >= a.n_new[seq]) return;                       // (uniform)
     const int64_t pos = (int64_t)(a.first ? a.first[seq] : 0) + t;
-    const bool there[2] = {pos >= 0 && pos < a.stride[0], pos >= 0 && pos < a.stride[1]};
+    bool there[2] = {pos >= 0 && pos < a.stride[0], pos >= 0 && pos < a.stride[1]};
     const int n_rows = a.n_q + 2 * a.n_kv, step = GROUPS * split, rot = a.rot, half = rot / 2;
     // where the token's rows are, head 0's (none: no such input or output)
     auto at = [&](const void* p, size_t row) { return p ? reinterpret_cast<char*>(const_cast<void*>(p)) + row * esz : nullptr; };
     const char *in_q = at(a.in[0], tok * a.row[0]), *in_k = at(a.in[1], tok * a.row[1]), *in_v = at(a.in[2], tok * a.row[2]);
     char* out_q = at(a.out[0], ((size_t)seq * a.n_q * T + t) * RA_D);
-    const size_t row0 = (size_t)seq * a.n_kv * a.stride[0] + pos, head4 = (size_t)seq * a.n_kv * a.stride[1] + pos;
+    size_t row0 = (size_t)seq * a.n_kv * a.stride[0] + pos;
+    const size_t head4 = (size_t)seq * a.n_kv * a.stride[1] + pos;
+    if constexpr (PAGED) {                                          // (a.stride[0]: rows of a page; rows of the table: table_pages << page_log2)
+        there[0] = pos >= 0 && pos < ((int64_t)pages.table_pages << pages.page_log2);
+        there[1] = false;
+        const int page = there[0] ? pages.table[(size_t)seq * pages.table_stride + (pos >> pages.page_log2)] : -1;
+        there[0] = (uint32_t)page < (uint32_t)pages.n_pages;
+        row0 = ((size_t)page * a.n_kv << pages.page_log2) + (pos & (a.stride[0] - 1));
+    }
     char *out_k = at(a.out[1], row0 * RA_D), *out_v = at(a.out[2], row0 * RA_D);
-    if (tid < half) s_cs[tid] = cos_sin64((double)pos * (double)a.inv_freq[tid]);
+    if (tid < half) {
+        float2 cs = cos_sin64((double)pos * (double)a.inv_freq[tid]);
+        if constexpr (PAGED) cs = make_float2(cs.x * rot_scale, cs.y * rot_scale);
+        s_cs[tid] = cs;
+    }
 #pragma unroll
     for (int i = 0; i < 2; ++i)
         if (a.weight[i])                                           // (the last wavefronts first: the angles are the first one's)
@@ -212,7 +225,7 @@ __global__ __launch_bounds__(THREADS, 8) void append_kernel(AppendArgs a, int sp
             // (capacities are below 2^30 rows)
             char* out = which == 1 ? out_k : out_v;
             if (out && there[0]) kv_store(out + (uint64_t)(uint32_t)h * (uint32_t)a.stride[0] * (RA_D * esz), l, row);
-            if (a.codes[which - 1] && there[1]) {
+            if (!PAGED && a.codes[which - 1] && there[1]) {
                 float v[VALS];
                 kv_floats<DT>(row, v);
                 const uint64_t row4 = head4 + (uint64_t)(uint32_t)h * (uint32_t)a.stride[1];
@@ -222,7 +235,8 @@ __global__ __launch_bounds__(THREADS, 8) void append_kernel(AppendArgs a, int sp
     }
 }
 
-ra_status ra_launch_append(const AppendArgs& a, ra_dtype dt, hipStream_t st) {
+template <bool PAGED>
+static ra_status launch_append(const AppendArgs& a, const PgCache& pages, float rot_scale, ra_dtype dt, hipStream_t st) {
     const int64_t tokens = a.T * a.n_seq;
     if (tokens > (1 << 24) - 1) RA_FAIL(RA_EUNSUP, "more than 2^24 - 1 tokens in a call");
     if ((int64_t)a.n_q + 2 * (int64_t)a.n_kv > (1 << 24) - 1) RA_FAIL(RA_EUNSUP, "too many heads for one launch");
@@ -231,7 +245,8 @@ ra_status ra_launch_append(const AppendArgs& a, ra_dtype dt, hipStream_t st) {
     const int heads = a.n_q + 2 * a.n_kv, split = tokens <= 128 ? (heads + groups - 1) / groups : 1;
     const int64_t blocks = tokens * split;
     if (blocks > (1 << 24) - 1) RA_FAIL(RA_EUNSUP, "too many heads for one launch");
-#define KV_GO_1(DTV, THREADS, ONCE) hipLaunchKernelGGL((append_kernel<DTV, THREADS, ONCE>), dim3((unsigned)blocks), dim3(THREADS), 0, st, a, split)
+#define KV_GO_1(DTV, THREADS, ONCE) \
+    hipLaunchKernelGGL((append_kernel<DTV, THREADS, ONCE, PAGED>), dim3((unsigned)blocks), dim3(THREADS), 0, st, a, split, pages, rot_scale)
 #define KV_GO_T(DTV, THREADS)                                                                                        \
     do {                                                                                                             \
         if (tokens * bytes > KV_KEPT) KV_GO_1(DTV, THREADS, true); else KV_GO_1(DTV, THREADS, false);                \
@@ -253,6 +268,10 @@ ra_status ra_launch_append(const AppendArgs& a, ra_dtype dt, hipStream_t st) {
 #undef KV_GO
     RA_HIP(hipGetLastError());
     return RA_OK;
+}
+ra_status ra_launch_append(const AppendArgs& a, ra_dtype dt, hipStream_t st) { return launch_append<false>(a, PgCache{}, 1.f, dt, st); }
+ra_status ra_launch_append_paged(const AppendArgs& a, const PgCache& pages, float rot_scale, ra_dtype dt, hipStream_t st) {
+    return launch_append<true>(a, pages, rot_scale, dt, st);
 }
 
 // grid: x = rows of a head, GROUPS x FLY to a workgroup, y = head (with its sequence). A group of lanes takes FLY rows, whose
