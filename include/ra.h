@@ -383,14 +383,15 @@ ra_status ra_append_tokens_paged(const void* q_in, const void* k_in, const void*
                                  const int32_t* first, const int32_t* n_new, void* stream, void* q_out);
 
 /* Rows first[s] + t, t < T, of K (values 0) or V (1) -> X [n_seq][n_kv_heads][T][128], side by side as ra_knn, ra_build_index,
- * ra_quantize_keys and the walks read keys. Rows without a page come as zeroes (rows behind a sequence's last token, in its last page, as they are). */
+ * ra_quantize_keys and the walks read keys. Rows without a page come as zeroes (rows behind a sequence's last token, in its last page, as they are).
+ * RA_EUNSUP past 2^24 - 1 workgroups, one for 16 rows of a head (float32: 8). */
 ra_status ra_gather_paged(const ra_paged_cache* cache, int values, int64_t T, int d, const int32_t* first, void* stream, void* X);
 
 /* ra_full_attention over a cache in pages: q [n_seq][n_q_heads][128] of type dt; rows [0, n) of sequence s that have a page, n =
  * min(n_tokens[s], N) (device int32; NULL: N for every sequence), N <= table_pages page. A sequence without rows gets out = 0 and
  * lse = -inf. Other rows are not looked at, whatever they hold. float32 accumulation; the weights of the softmax meet the values with all
  * their 24 bits. With bfloat16, infinite values in rows that are attended come out as NaN.
- * RA_EUNSUP from 2^24 tiles of up to 16 query heads of a KV head on, over N > 2^24 tokens from 2^21 on.
+ * RA_EUNSUP from 2^23 tiles of up to 16 query heads of a KV head on, over N > 2^24 tokens from 2^21 on.
  * workspace: device memory of at least ra_full_attention_paged_workspace_bytes(...) bytes, 16-byte aligned, which nothing else may use
  * until the call has run; it needs no initialisation. */
 size_t ra_full_attention_paged_workspace_bytes(int n_seq, int n_q_heads, int n_kv_heads, int64_t N);
@@ -402,8 +403,8 @@ ra_status ra_full_attention_paged(const void* q, const ra_paged_cache* cache, in
  * with n = min(n_tokens[s], N) and n_i = min(n_indexed[s], n) (device int32; NULL: N, and n) W = [0, sink) u [min(n - window, n_i), n):
  * tokens behind the n_i that the index was built over are static. Entries of ids that are not in [0, n), or are members of W (they are
  * attended there), are skipped; one that is given twice counts twice. Rows without a page are not attended. Weights have 24 bits.
- * workspace: as above, of ra_attend_paged_workspace_bytes(...) bytes, `grows`: whether n_indexed is given. */
-size_t ra_attend_paged_workspace_bytes(int n_seq, int n_q_heads, int n_kv_heads, int64_t N, int grows, int sink, int window, int topk);
+ * workspace: as above, of ra_attend_paged_workspace_bytes(...) bytes. */
+size_t ra_attend_paged_workspace_bytes(ra_dtype dt, int n_seq, int n_q_heads, int n_kv_heads, int64_t N, int sink, int window, int topk);
 ra_status ra_attend_paged(const void* q, const ra_paged_cache* cache, int n_q_heads, int64_t N, int d, const int32_t* n_tokens,
                           const int32_t* n_indexed, int sink, int window, int topk, const int32_t* ids, void* workspace,
                           size_t workspace_bytes, void* stream, float* out, float* lse, float* o_omega, float* lse_omega, float* o_w,

@@ -142,7 +142,7 @@ def lib() -> C.CDLL:
     L.ra_full_attention_paged_workspace_bytes.restype = C.c_size_t
     L.ra_full_attention_paged.argtypes = [vp, cache, i32, i64, i32, vp, vp, C.c_size_t, vp, vp, vp]
     L.ra_full_attention_paged.restype = i32
-    L.ra_attend_paged_workspace_bytes.argtypes = [i32, i32, i32, i64, i32, i32, i32, i32]
+    L.ra_attend_paged_workspace_bytes.argtypes = [i32, i32, i32, i32, i64, i32, i32, i32]
     L.ra_attend_paged_workspace_bytes.restype = C.c_size_t
     L.ra_attend_paged.argtypes = [vp, cache, i32, i64, i32, vp, vp, i32, i32, i32, vp, vp, C.c_size_t, vp, vp, vp, vp, vp, vp, vp]
     L.ra_attend_paged.restype = i32
@@ -794,9 +794,10 @@ class PagedCache:
         stride = table.stride(0) if table.shape[0] > 1 else table.shape[1]
         if stride < table.shape[1]:
             raise ValueError("the rows of the table must not overlap")
-        self._K, self._V, self._table, self._some = K, V, table, some
-        self._at = _ptr(K), _ptr(V), table.data_ptr()
-        self._c = _PagedCache(*self._at, stride, dt, table.shape[0], shape[1], shape[0], shape[2], table.shape[1])
+        self._K, self._V, self._table = K, V, table
+        # where the tensors that there are were when this was checked
+        self._at = tuple((t.data_ptr, t.data_ptr()) for t in (K, V, table) if t is not None)
+        self._c = _PagedCache(_ptr(K), _ptr(V), table.data_ptr(), stride, dt, table.shape[0], shape[1], shape[0], shape[2], table.shape[1])
         self._ref = C.byref(self._c)
         self._dt, self._dtype, self._n_seq, self._n_kv, self._rows = dt, some.dtype, table.shape[0], shape[1], table.shape[1] * shape[2]
 
@@ -813,8 +814,9 @@ class PagedCache:
         """What a call passes on, the tensors being where they were."""
         if here != self._here:
             raise ValueError(f"the cache must live on the current GPU ({here}), not on {self._here}")
-        if self._at != (_ptr(self._K), _ptr(self._V), self._table.data_ptr()):
-            raise ValueError("the cache's tensors have been given other memory: make another PagedCache")
+        for now, then in self._at:
+            if now() != then:
+                raise ValueError("the cache's tensors have been given other memory: make another PagedCache")
         return self._ref
 
 
@@ -895,11 +897,21 @@ def _workspace(given, need: int, room_for, here: int):
     """The given workspace, or a new one of `need` bytes -> (it, its bytes)."""
     if given is None:
         need = max(1, need)
+        if room_for is _CURRENT:
+            return torch.empty(need, dtype=torch.uint8, device=here), need
         with room_for:
             return torch.empty(need, dtype=torch.uint8, device=here), need
     _dev(given)
     _here(given)
     return given, given.numel() * given.element_size()
+
+
+def _paged_results(n_seq: int, n_q: int, d: int, room_for, here: int, out, lse):
+    """_results, on the call's stream."""
+    if room_for is _CURRENT or (out is not None and lse is not None):
+        return _results(n_seq, n_q, d, here, out, lse)
+    with room_for:
+        return _results(n_seq, n_q, d, here, out, lse)
 
 
 @functools.lru_cache(maxsize=256)
@@ -918,17 +930,16 @@ def ra_full_attention_paged(q, cache: PagedCache, n_tokens=None, N: Optional[int
     n_seq = cache._n_seq
     N = cache._rows if N is None else N
     workspace, have = _workspace(workspace, 0 if workspace is not None else _full_paged_room(n_seq, n_q, cache._n_kv, N), room_for, here)
-    with room_for:
-        out, lse = _results(n_seq, n_q, d, here, out, lse)
+    out, lse = _paged_results(n_seq, n_q, d, room_for, here, out, lse)
     _check(lib().ra_full_attention_paged(q_at, ref, n_q, N, d, None if n_tokens is None else _vector(n_tokens, n_seq, torch.int32, here, "n_tokens"),
                                          workspace.data_ptr(), have, _handle(stream, here), out.data_ptr(), lse.data_ptr()))
     return out, lse
 
 
 @functools.lru_cache(maxsize=256)
-def _attend_paged_room(n_seq: int, n_q: int, n_kv: int, N: int, grows: bool, sink: int, window: int, topk: int) -> int:
+def _attend_paged_room(dt: int, n_seq: int, n_q: int, n_kv: int, N: int, sink: int, window: int, topk: int) -> int:
     """ra_attend_paged_workspace_bytes, a function of sizes alone."""
-    return lib().ra_attend_paged_workspace_bytes(n_seq, n_q, n_kv, N, grows, sink, window, topk)
+    return lib().ra_attend_paged_workspace_bytes(dt, n_seq, n_q, n_kv, N, sink, window, topk)
 
 
 def ra_attend_paged(q, cache: PagedCache, sink: int, window: int, ids: torch.Tensor, n_tokens=None, n_indexed=None, N: Optional[int] = None,
@@ -945,17 +956,17 @@ def ra_attend_paged(q, cache: PagedCache, sink: int, window: int, ids: torch.Ten
             or ids.get_device() != here:
         raise ValueError("ids must be contiguous int32 [n_seq][n_q][topk] on the current GPU")
     N = cache._rows if N is None else N
-    need = 0 if workspace is not None else _attend_paged_room(n_seq, n_q, cache._n_kv, N, n_indexed is not None, sink, window, shape[2])
+    need = 0 if workspace is not None else _attend_paged_room(cache._dt, n_seq, n_q, cache._n_kv, N, sink, window, shape[2])
     workspace, have = _workspace(workspace, need, room_for, here)
-    extra = ()
-    with room_for:
-        out, lse = _results(n_seq, n_q, d, here, out, lse)
-        if partials:
-            f = dict(dtype=torch.float32, device=here)
+    out, lse = _paged_results(n_seq, n_q, d, room_for, here, out, lse)
+    extra = (None, None, None, None)
+    if partials:
+        f = dict(dtype=torch.float32, device=here)
+        with room_for:
             extra = (torch.empty((n_seq, n_q, d), **f), torch.empty((n_seq, n_q), **f),
                      torch.empty((n_seq, n_q, d), **f), torch.empty((n_seq, n_q), **f))
     _check(lib().ra_attend_paged(q_at, ref, n_q, N, d, None if n_tokens is None else _vector(n_tokens, n_seq, torch.int32, here, "n_tokens"),
                                  None if n_indexed is None else _vector(n_indexed, n_seq, torch.int32, here, "n_indexed"), sink, window, shape[2],
                                  ids.data_ptr(), workspace.data_ptr(), have, _handle(stream, here), out.data_ptr(), lse.data_ptr(),
-                                 *([t.data_ptr() for t in extra] or (None, None, None, None))))
+                                 *map(_ptr, extra)))
     return (out, lse, *extra) if partials else (out, lse)

@@ -1026,9 +1026,9 @@ extern "C" ra_status ra_full_attention_paged(const void* q, const ra_paged_cache
     return ra_launch_full_paged(q, (ra_dtype)cache->dt, c, n_seq, n_q, n_kv, N, n_tokens, (float*)workspace, (hipStream_t)stream, out, lse);
 }
 
-extern "C" size_t ra_attend_paged_workspace_bytes(int n_seq, int n_q, int n_kv, int64_t N, int grows, int sink, int window, int topk) {
-    if (check_heads(n_seq, n_q, n_kv) != RA_OK || N < 1 || N > 0x7fffffff / 2 || sink < 0 || window < 0 || topk < 1 || topk > RA_MAX_TOPK) return 0;
-    return 256 + ra_attend_paged_partial_floats(n_seq, n_q, n_kv, N, grows != 0, sink, window, topk) * sizeof(float);
+extern "C" size_t ra_attend_paged_workspace_bytes(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N, int sink, int window, int topk) {
+    if (check_dtype(dt) != RA_OK || check_heads(n_seq, n_q, n_kv) != RA_OK || N < 1 || N > 0x7fffffff / 2 || sink < 0 || window < 0 || topk < 1 || topk > RA_MAX_TOPK) return 0;
+    return 256 + ra_attend_paged_partial_floats(dt, n_seq, n_q, n_kv, N, sink, window, topk) * sizeof(float);
 }
 
 extern "C" ra_status ra_attend_paged(const void* q, const ra_paged_cache* cache, int n_q, int64_t N, int d, const int32_t* n_tokens,
@@ -1047,7 +1047,7 @@ extern "C" ra_status ra_attend_paged(const void* q, const ra_paged_cache* cache,
     if (topk > RA_MAX_TOPK) RA_FAIL(RA_EUNSUP, "topk %d exceeds RA_MAX_TOPK %d", topk, RA_MAX_TOPK);
     RA_TRY(check_aligned(q, 16, "q"));
     RA_TRY(check_aligned(workspace, 16, "workspace"));
-    if (workspace_bytes < ra_attend_paged_workspace_bytes(n_seq, n_q, n_kv, N, n_indexed != nullptr, sink, window, topk))
+    if (workspace_bytes < ra_attend_paged_workspace_bytes((ra_dtype)cache->dt, n_seq, n_q, n_kv, N, sink, window, topk))
         RA_FAIL(RA_ESHAPE, "workspace of %zu B is smaller than ra_attend_paged_workspace_bytes", workspace_bytes);
     return ra_launch_attend_paged(q, (ra_dtype)cache->dt, c, n_seq, n_q, n_kv, N, n_tokens, n_indexed, sink, window, topk, ids, (float*)workspace,
                                   (hipStream_t)stream, out, lse, o_omega, lse_omega, o_w, lse_w);

@@ -198,7 +198,7 @@ ra_status ra_launch_gather_paged(const PgCache& c, const void* pages, ra_dtype d
 size_t ra_full_paged_partial_floats(int n_seq, int n_q, int n_kv, int64_t N);
 ra_status ra_launch_full_paged(const void* q, ra_dtype dt, const PgCache& c, int n_seq, int n_q, int n_kv, int64_t N, const int32_t* n_tokens,
                                float* partials, hipStream_t st, float* out, float* lse);
-size_t ra_attend_paged_partial_floats(int n_seq, int n_q, int n_kv, int64_t N, bool grows, int sink, int window, int topk);
+size_t ra_attend_paged_partial_floats(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N, int sink, int window, int topk);
 ra_status ra_launch_attend_paged(const void* q, ra_dtype dt, const PgCache& c, int n_seq, int n_q, int n_kv, int64_t N, const int32_t* n_tokens,
                                  const int32_t* n_indexed, int sink, int window, int topk, const int32_t* ids, float* partials, hipStream_t st,
                                  float* out, float* lse, float* o_omega, float* lse_omega, float* o_w, float* lse_w);

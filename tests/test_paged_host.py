@@ -74,7 +74,7 @@ def test_caches_that_are_refused(name, cache, status, needle):
     ("ra_attend_paged", dict(sink=-1), {}, 1, "non-negative"), ("ra_attend_paged", dict(window=-1), {}, 1, "non-negative"),
     ("ra_attend_paged", dict(topk=0), {}, 1, "topk"), ("ra_attend_paged", dict(topk=2049), {}, 6, "RA_MAX_TOPK"),
     ("ra_attend_paged", dict(q=_p(0x10008)), {}, 1, "aligned"), ("ra_attend_paged", dict(ws=_p(0x10008)), {}, 1, "aligned"),
-    ("ra_attend_paged", dict(ws_bytes=8), {}, 2, "workspace"), ("ra_attend_paged", dict(n_q=1 << 25, ws_bytes=1 << 62), {}, 6, "too many heads"),
+    ("ra_attend_paged", dict(ws_bytes=8, window=100), {}, 2, "workspace"), ("ra_attend_paged", dict(n_q=1 << 28, ws_bytes=1 << 62), {}, 6, "too many heads"),
 ])
 def test_calls_that_are_refused(name, change, cache, status, needle):
     _refused(name, change, cache, status, needle)
@@ -85,10 +85,9 @@ def test_workspace_sizes():
     full, attend = L.ra_full_attention_paged_workspace_bytes, L.ra_attend_paged_workspace_bytes
     assert full(1, 32, 8, 131072) > 256 and full(1, 4, 1, 1) == 256
     assert full(1, 32, 7, 1000) == 0 and full(1, 32, 8, 0) == 0 and full(1, 32, 8, 1 << 31) == 0 and full(0, 4, 1, 10) == 0
-    assert attend(1, 32, 8, 1000, 0, 4, 640, 100) >= 256 + 32 * 7 * 132 * 4
-    assert attend(1, 32, 8, 1000, 1, 0, 0, 1) > attend(1, 32, 8, 1000, 0, 0, 0, 1) >= 256 + 32 * 132 * 4
-    for bad in ((1, 32, 7, 1000, 0, 4, 640, 100), (1, 32, 8, 0, 0, 4, 640, 100), (1, 32, 8, 1000, 0, -1, 640, 100), (1, 32, 8, 1000, 0, 4, -1, 100),
-                (1, 32, 8, 1000, 0, 4, 640, 0), (1, 32, 8, 1000, 0, 4, 640, 2049)):
+    assert attend(1, 1, 32, 8, 1000, 4, 640, 100) >= 256 + 32 * 2 * 2 * 132 * 4 and attend(0, 1, 32, 8, 1000, 0, 0, 1) == 256
+    for bad in ((1, 1, 32, 7, 1000, 4, 640, 100), (1, 1, 32, 8, 0, 4, 640, 100), (1, 1, 32, 8, 1000, -1, 640, 100), (1, 1, 32, 8, 1000, 4, -1, 100),
+                (1, 1, 32, 8, 1000, 4, 640, 0), (1, 1, 32, 8, 1000, 4, 640, 2049), (2, 1, 32, 8, 1000, 4, 640, 100)):
         assert attend(*bad) == 0
 
 
