@@ -771,6 +771,26 @@ def ra_attend_q4(q, idx: Index, k4, v4, sink: int, window: int, ids: torch.Tenso
     return (out, lse, *extra) if partials else (out, lse)
 
 
+_short = None
+
+
+def _calls():
+    """Load _calls.so (once): the calls around a cache in pages made and checked by compiled code, with the same outcome, where nothing is
+    out of the ordinary; else they return None."""
+    global _short
+    if _short is None:
+        L = lib()
+        try:
+            from . import _calls as m
+        except ImportError as e:
+            raise RuntimeError("_calls.so is missing or broken: build it as libra.so") from e
+        at = [C.cast(f, C.c_void_p).value for f in (L.ra_append_tokens_paged, L.ra_full_attention_paged, L.ra_full_attention_paged_workspace_bytes,
+                                                    L.ra_attend_paged, L.ra_attend_paged_workspace_bytes)]
+        m.bind(_RAW or (lambda here: torch.cuda.current_stream(here).cuda_stream), *at)
+        _short = m
+    return _short
+
+
 class PagedCache:
     """A cache in pages: K, V [n_pages][n_kv][page][128] (float32 or bfloat16, page a power of two; one of them may be None) and the
     table int32 [n_seq][table_pages] whose entry [s][r // page] is the page of row r of sequence s (outside [0, n_pages): none). Tensors of the
@@ -799,6 +819,7 @@ class PagedCache:
         self._at = tuple((t.data_ptr, t.data_ptr()) for t in (K, V, table) if t is not None)
         self._c = _PagedCache(_ptr(K), _ptr(V), table.data_ptr(), stride, dt, table.shape[0], shape[1], shape[0], shape[2], table.shape[1])
         self._ref = C.byref(self._c)
+        self._core = _calls().cache(K, V, table, C.addressof(self._c), self._here)
         self._dt, self._dtype, self._n_seq, self._n_kv, self._rows = dt, some.dtype, table.shape[0], shape[1], table.shape[1] * shape[2]
 
     K = property(lambda s: s._K)
@@ -824,6 +845,11 @@ def ra_append_tokens_paged(q, k, v, first, cache: PagedCache, *, n_new=None, q_w
                            interleaved: bool = False, rot_scale: float = 1.0, q_out=None, stream=None):
     """ra_append_tokens into a cache in pages; cosines and sines times rot_scale. k and v may be None: nothing of K or V is
     written. -> q_out [n_seq][n_q][T][128] (None without q), as there."""
+    if stream is None:
+        got = _short.append(q, k, v, first, cache._core, n_new, q_weight, k_weight, eps, inv_freq, interleaved, rot_scale, q_out)
+        if got.__class__ is tuple:
+            return got[0]
+        _check(got or 0)
     some = q if q is not None else k if k is not None else v
     if some is None:
         raise ValueError("at least one of q, k and v is needed")
@@ -923,6 +949,11 @@ def _full_paged_room(n_seq: int, n_q: int, n_kv: int, N: int) -> int:
 def ra_full_attention_paged(q, cache: PagedCache, n_tokens=None, N: Optional[int] = None, stream=None, workspace=None, out=None, lse=None):
     """Eq. 1 over the first n_tokens[s] rows (int32 [n_seq] on the GPU, at most N; None: N, by default cache.rows) of every sequence of a
     cache in pages, those that have a page -> (out float32 [n_seq][n_q][128], lse float32 [n_seq][n_q])."""
+    if stream is None:
+        got = _short.full(q, cache._core, n_tokens, N, workspace, out, lse)
+        if got.__class__ is tuple:
+            return got
+        _check(got or 0)
     here = torch.cuda.current_device()
     room_for = _for(stream, here)
     ref = cache._of(here)
@@ -947,6 +978,11 @@ def ra_attend_paged(q, cache: PagedCache, sink: int, window: int, ids: torch.Ten
     """ra_attend over a cache in pages, of n_tokens[s] rows (int32 [n_seq] on the GPU, at most N; None: N, by default cache.rows), the first
     n_indexed[s] of which (None: all) an index was built over; those behind are static. ids in the static set are
     skipped. -> (out, lse) or, with partials=True, (out, lse, o_omega, lse_omega, o_w, lse_w)."""
+    if stream is None and not partials:
+        got = _short.attend(q, cache._core, sink, window, ids, n_tokens, n_indexed, N, workspace, out, lse)
+        if got.__class__ is tuple:
+            return got
+        _check(got or 0)
     here = torch.cuda.current_device()
     room_for = _for(stream, here)
     ref = cache._of(here)

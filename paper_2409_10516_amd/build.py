@@ -1,12 +1,14 @@
-"""Compile the HIP sources under csrc/ into libra.so next to this file (gfx950 only)."""
+"""Compile the HIP sources under csrc/ into libra.so next to this file (gfx950 only), and the host code of the binding into _calls.so."""
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libra.so")
+CALLS = os.path.join(HERE, "_calls.so")      # host code: short-cuts of binding.py (csrc/calls.cpp)
 SOURCES = ["api.hip", "attend.hip", "search.hip", "decode.hip", "flat.hip", "knn.hip", "knn_order.hip", "knn_filter.hip", "project.hip",
            "quant.hip", "kv4.hip", "q4.hip", "paged.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
@@ -17,6 +19,15 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=o
 # list either way); without this every fmaxf of the selection's max tree first canonicalises
 # its inputs with an instruction of its own
 EXTRA = {"knn.hip": ["-fno-honor-nans"]}
+
+
+def _calls_command():
+    import torch
+    at = os.path.dirname(torch.__file__)
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+            "-I", os.path.join(ROOT, "include"), "-I", os.path.join(at, "include"), "-I", os.path.join(at, "include", "torch", "csrc", "api", "include"),
+            "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "calls.cpp"), "-o", CALLS,
+            "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
 
 
 def build(verbose=True):
@@ -30,6 +41,10 @@ def build(verbose=True):
         if verbose:
             print(" ".join(cmd), flush=True)
         procs.append((s, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
+    cmd = _calls_command()
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    procs.append(("calls.cpp", subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
     for s, p in procs:
         out = p.communicate()[0].decode()
         noise = "is not a recognized feature for this target"
@@ -37,7 +52,7 @@ def build(verbose=True):
         if out.strip() and verbose:
             print(out)
         if p.returncode:
-            raise RuntimeError(f"hipcc failed on {s}:\n{out}")
+            raise RuntimeError(f"the compiler failed on {s}:\n{out}")
     cmd = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB]
     if verbose:
         print(" ".join(cmd), flush=True)

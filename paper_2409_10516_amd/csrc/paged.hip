@@ -375,7 +375,7 @@ static PgCut pg_cut(int n_seq, int n_q, int n_kv, int64_t N) {
     const int64_t jobs = (int64_t)n_seq * n_kv * x.tiles;
     // (from PG_MOST_UNITS jobs on there is no list: its units, and the threads of the second kernel, 128 for each of up to 16 heads, fit 32 bits)
     x.whole = N <= 640 || N <= (jobs < 128 ? 16 * jobs : 2048) || (jobs >= PG_MOST_UNITS && N <= PG_MOST_ROWS);
-    x.unit_log2 = 6;
+    x.unit_log2 = jobs * N <= 2 * PG_UNIT * PG_MOST_WORKGROUPS ? 6 : 7;
     static_assert(PG_UNIT == 1 << 6, "rows of a unit");
     x.refused = x.whole && jobs >= 1 << 23 ? "too many heads for one launch: 2^23 tiles of up to 16 query heads"
                 : !x.whole && jobs >= PG_MOST_UNITS ? "too many heads for one launch: 2^21 tiles of up to 16 query heads over more than 2^24 tokens" : nullptr;
