@@ -387,24 +387,6 @@ __global__ __launch_bounds__(Q4_THREADS, DT == RA_BF16 ? 3 : 2) void q4_full_ker
     }
 }
 
-// A head's records, those of a row of workgroups: their sums, their maxima and sums of weights, and how many.
-struct Q4Records { const float* sums; const float2* ml; int have; };
-__device__ __forceinline__ Q4Records q4_records(const float* partials, size_t head, int n_seq, int n_q, int n_kv, int N,
-                                                const int32_t* n_tokens, int tiles, int unit_log2, int heads, int grid) {
-    const int seq = (int)(head / n_q), group = n_q / n_kv, h = (int)(head % n_q), jobs = n_kv * tiles;
-    const int job = h / group * tiles + h % group / heads;
-    const RowList x = row_list(n_tokens, n_seq, seq, N, unit_log2, jobs, grid);
-    const uint32_t units = row_units(x.n, unit_log2);
-    int have = 0, wg0 = 0;
-    if (units) {
-        const uint32_t unit0 = x.first + job * units;
-        wg0 = (int)x.owner(unit0);
-        have = (int)x.owner(unit0 + units - 1) - wg0 + 1;
-    }
-    const size_t places = (size_t)grid + (size_t)n_seq * jobs, at = h % group % heads * places + (size_t)wg0 + (size_t)seq * jobs + job;
-    return {partials + at * RA_D, reinterpret_cast<const float2*>(partials + heads * places * RA_D) + at, have};
-}
-
 // What is combined: grid: x = DIMS dimensions of a head. One record or a few (of most heads, in a batch): a thread per dimension, all records
 // on their way at once. More: groups of DIMS threads take records in turn, the first of which are on their way before the weights are known.
 // Workgroups of 32 dimensions where few heads have many records each (131072 tokens of 8 KV heads: with 1024 threads 32.5 us a
@@ -423,7 +405,7 @@ __global__ __launch_bounds__(THREADS) void q4_full_merge_kernel(const float* __r
     const int tid = threadIdx.x, t = tid % DIMS, slice = tid / DIMS, lane = tid & 63;
     const size_t head = blockIdx.x / (RA_D / DIMS);
     const int dim = blockIdx.x % (RA_D / DIMS) * DIMS + t;
-    const Q4Records x = q4_records(partials, head, n_seq, n_q, n_kv, N, n_tokens, tiles, unit_log2, heads, grid);
+    const FullRecords x = full_records(partials, head, n_seq, n_q, n_kv, N, n_tokens, tiles, unit_log2, heads, grid);
     const int have = x.have;
     float mx = -INFINITY, ll = 0.f, a = 0.f;
     if (DIMS == RA_D && have <= Q4_MERGE_FEW) {

@@ -94,6 +94,24 @@ __device__ __forceinline__ int row_seq_of(const RowList& x, const int32_t* n_tok
     }
 }
 
+// A head's records, those of a row of workgroups: their sums, their maxima and sums of weights, and how many.
+struct FullRecords { const float* sums; const float2* ml; int have; };
+__device__ __forceinline__ FullRecords full_records(const float* partials, size_t head, int n_seq, int n_q, int n_kv, int N,
+                                                const int32_t* n_tokens, int tiles, int unit_log2, int heads, int grid) {
+    const int seq = (int)(head / n_q), group = n_q / n_kv, h = (int)(head % n_q), jobs = n_kv * tiles;
+    const int job = h / group * tiles + h % group / heads;
+    const RowList x = row_list(n_tokens, n_seq, seq, N, unit_log2, jobs, grid);
+    const uint32_t units = row_units(x.n, unit_log2);
+    int have = 0, wg0 = 0;
+    if (units) {
+        const uint32_t unit0 = x.first + job * units;
+        wg0 = (int)x.owner(unit0);
+        have = (int)x.owner(unit0 + units - 1) - wg0 + 1;
+    }
+    const size_t places = (size_t)grid + (size_t)n_seq * jobs, at = h % group % heads * places + (size_t)wg0 + (size_t)seq * jobs + job;
+    return {partials + at * RA_D, reinterpret_cast<const float2*>(partials + heads * places * RA_D) + at, have};
+}
+
 // ---- records of two sets ----------------------------------------------------------------
 struct SetOut {
     uint32_t* tickets;                  // one word per query head (ticket.h), or null
