@@ -394,7 +394,7 @@ ra_status ra_gather_paged(const ra_paged_cache* cache, int values, int64_t T, in
  * RA_EUNSUP from 2^23 tiles of up to 16 query heads of a KV head on, over N > 2^24 tokens from 2^21 on.
  * workspace: device memory of at least ra_full_attention_paged_workspace_bytes(...) bytes, 16-byte aligned, which nothing else may use
  * until the call has run; it needs no initialisation. */
-size_t ra_full_attention_paged_workspace_bytes(int n_seq, int n_q_heads, int n_kv_heads, int64_t N);
+size_t ra_full_attention_paged_workspace_bytes(ra_dtype dt, int n_seq, int n_q_heads, int n_kv_heads, int64_t N);
 ra_status ra_full_attention_paged(const void* q, const ra_paged_cache* cache, int n_q_heads, int64_t N, int d, const int32_t* n_tokens,
                                   void* workspace, size_t workspace_bytes, void* stream, float* out, float* lse);
 
@@ -403,6 +403,7 @@ ra_status ra_full_attention_paged(const void* q, const ra_paged_cache* cache, in
  * with n = min(n_tokens[s], N) and n_i = min(n_indexed[s], n) (device int32; NULL: N, and n) W = [0, sink) u [min(n - window, n_i), n):
  * tokens behind the n_i that the index was built over are static. Entries of ids that are not in [0, n), or are members of W (they are
  * attended there), are skipped; one that is given twice counts twice. Rows without a page are not attended. Weights have 24 bits.
+ * RA_EUNSUP past 2^22 - 1 workgroups, one for up to 16 query heads of a KV head at least.
  * workspace: as above, of ra_attend_paged_workspace_bytes(...) bytes. */
 size_t ra_attend_paged_workspace_bytes(ra_dtype dt, int n_seq, int n_q_heads, int n_kv_heads, int64_t N, int sink, int window, int topk);
 ra_status ra_attend_paged(const void* q, const ra_paged_cache* cache, int n_q_heads, int64_t N, int d, const int32_t* n_tokens,

@@ -138,7 +138,7 @@ def lib() -> C.CDLL:
     L.ra_append_tokens_paged.restype = i32
     L.ra_gather_paged.argtypes = [cache, i32, i64, i32, vp, vp, vp]
     L.ra_gather_paged.restype = i32
-    L.ra_full_attention_paged_workspace_bytes.argtypes = [i32, i32, i32, i64]
+    L.ra_full_attention_paged_workspace_bytes.argtypes = [i32, i32, i32, i32, i64]
     L.ra_full_attention_paged_workspace_bytes.restype = C.c_size_t
     L.ra_full_attention_paged.argtypes = [vp, cache, i32, i64, i32, vp, vp, C.c_size_t, vp, vp, vp]
     L.ra_full_attention_paged.restype = i32
@@ -941,9 +941,9 @@ def _paged_results(n_seq: int, n_q: int, d: int, room_for, here: int, out, lse):
 
 
 @functools.lru_cache(maxsize=256)
-def _full_paged_room(n_seq: int, n_q: int, n_kv: int, N: int) -> int:
+def _full_paged_room(dt: int, n_seq: int, n_q: int, n_kv: int, N: int) -> int:
     """ra_full_attention_paged_workspace_bytes, a function of sizes alone."""
-    return lib().ra_full_attention_paged_workspace_bytes(n_seq, n_q, n_kv, N)
+    return lib().ra_full_attention_paged_workspace_bytes(dt, n_seq, n_q, n_kv, N)
 
 
 def ra_full_attention_paged(q, cache: PagedCache, n_tokens=None, N: Optional[int] = None, stream=None, workspace=None, out=None, lse=None):
@@ -960,7 +960,7 @@ def ra_full_attention_paged(q, cache: PagedCache, n_tokens=None, N: Optional[int
     q_at, n_q, d = _paged_query(q, cache, here)
     n_seq = cache._n_seq
     N = cache._rows if N is None else N
-    workspace, have = _workspace(workspace, 0 if workspace is not None else _full_paged_room(n_seq, n_q, cache._n_kv, N), room_for, here)
+    workspace, have = _workspace(workspace, 0 if workspace is not None else _full_paged_room(cache._dt, n_seq, n_q, cache._n_kv, N), room_for, here)
     out, lse = _paged_results(n_seq, n_q, d, room_for, here, out, lse)
     _check(lib().ra_full_attention_paged(q_at, ref, n_q, N, d, None if n_tokens is None else _vector(n_tokens, n_seq, torch.int32, here, "n_tokens"),
                                          workspace.data_ptr(), have, _handle(stream, here), out.data_ptr(), lse.data_ptr()))

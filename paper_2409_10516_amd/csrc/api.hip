@@ -1005,9 +1005,9 @@ static ra_status check_paged_rows(const ra_paged_cache* c, int64_t N) {
     return RA_OK;
 }
 
-extern "C" size_t ra_full_attention_paged_workspace_bytes(int n_seq, int n_q, int n_kv, int64_t N) {
-    if (check_heads(n_seq, n_q, n_kv) != RA_OK || N < 1 || N > 0x7fffffff / 2) return 0;
-    return 256 + ra_full_paged_partial_floats(n_seq, n_q, n_kv, N) * sizeof(float);
+extern "C" size_t ra_full_attention_paged_workspace_bytes(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N) {
+    if (check_dtype(dt) != RA_OK || check_heads(n_seq, n_q, n_kv) != RA_OK || N < 1 || N > 0x7fffffff / 2) return 0;
+    return 256 + ra_full_paged_partial_floats(dt, n_seq, n_q, n_kv, N) * sizeof(float);
 }
 
 extern "C" ra_status ra_full_attention_paged(const void* q, const ra_paged_cache* cache, int n_q, int64_t N, int d, const int32_t* n_tokens,
@@ -1021,7 +1021,7 @@ extern "C" ra_status ra_full_attention_paged(const void* q, const ra_paged_cache
     RA_TRY(check_paged_rows(cache, N));
     RA_TRY(check_aligned(q, 16, "q"));
     RA_TRY(check_aligned(workspace, 16, "workspace"));
-    if (workspace_bytes < ra_full_attention_paged_workspace_bytes(n_seq, n_q, n_kv, N))
+    if (workspace_bytes < ra_full_attention_paged_workspace_bytes((ra_dtype)cache->dt, n_seq, n_q, n_kv, N))
         RA_FAIL(RA_ESHAPE, "workspace of %zu B is smaller than ra_full_attention_paged_workspace_bytes", workspace_bytes);
     return ra_launch_full_paged(q, (ra_dtype)cache->dt, c, n_seq, n_q, n_kv, N, n_tokens, (float*)workspace, (hipStream_t)stream, out, lse);
 }

@@ -154,7 +154,7 @@ PyObject* full(PyObject*, PyObject* const* a, Py_ssize_t n) {
         void *ws, *st;
         size_t have;
         Results r;
-        if (!room(*c, a[4], a[4] == Py_None ? full_room(c->c.n_seq, (int)n_q, c->c.n_kv_heads, N) : 0, &own, &ws, &have) ||
+        if (!room(*c, a[4], a[4] == Py_None ? full_room((ra_dtype)c->c.dt, c->c.n_seq, (int)n_q, c->c.n_kv_heads, N) : 0, &own, &ws, &have) ||
             !r.take(*c, a[5], a[6], c->c.n_seq, n_q, d) || !stream_of(*c, &st))
             return nullptr;
         ra_status rc;

@@ -195,7 +195,7 @@ ra_status ra_launch_append(const AppendArgs& a, ra_dtype dt, hipStream_t st);
 ra_status ra_launch_append_paged(const AppendArgs& a, const PgCache& pages, float rot_scale, ra_dtype dt, hipStream_t st);
 ra_status ra_launch_gather_paged(const PgCache& c, const void* pages, ra_dtype dt, int n_seq, int n_kv, int64_t T, const int32_t* first,
                                  hipStream_t st, void* X);
-size_t ra_full_paged_partial_floats(int n_seq, int n_q, int n_kv, int64_t N);
+size_t ra_full_paged_partial_floats(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N);
 ra_status ra_launch_full_paged(const void* q, ra_dtype dt, const PgCache& c, int n_seq, int n_q, int n_kv, int64_t N, const int32_t* n_tokens,
                                float* partials, hipStream_t st, float* out, float* lse);
 size_t ra_attend_paged_partial_floats(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N, int sink, int window, int topk);

@@ -2,9 +2,9 @@
 // the static set W of Sec. 3.3 with their combination by Eq. 4-5 (ra_attend_paged), and rows side by side again (ra_gather_paged).
 // What puts tokens into pages is with the other calls that append (kv4.hip).
 //
-// Rows are cut into parts; a workgroup turns one part into a record (128 weighted sums, the running maximum of
-// z log2(e), the sum of weights), and a head's records are combined by a second kernel. Weights are powers of two,
-// p = 2^(c <q, k> - m) with c = log2(e) / sqrt(d): one multiply-add and one instruction each.
+// Rows are cut into parts; a workgroup turns one part into a record (128 weighted sums, the maximum of z log2(e), the sum of weights), and a
+// head's records are combined by a second kernel. Weights are powers of two, p = 2^(c (<q, k> - m)) with c = log2(e) / sqrt(d) and m the running
+// maximum of <q, k>: the difference first, so that its rounding goes by the difference and equal logits have equal weights however large they are.
 #include "common.h"
 #include "records.h"
 
@@ -12,7 +12,8 @@
 #define PG_GATHER_THREADS 256
 #define PG_HEADS 16                 // query heads of a tile: columns of the matrix instructions
 #define PG_C ((float)(1.4426950408889634 / 11.313708498984761))
-#define PG_LOWEST (-1.7e38f)        // below every logit: a maximum that nothing has moved yet
+#define PG_LOWEST (-3.402823466e38f)        // no logit is below it: a maximum that nothing has moved yet
+#define PG_LAG (8.f / PG_C)         // by how much a product may exceed it, a weight of 2^8
 
 template <int DT> constexpr int PG_ROW = RA_D * (DT == RA_BF16 ? 2 : 4);         // bytes of a row
 template <int DT> constexpr int PG_PIECES = PG_ROW<DT> / 64;                     // of 16 bytes that a lane has of a chunk's keys, and of its values
@@ -49,7 +50,7 @@ struct PgWave {
     static constexpr int PIECES = PG_PIECES<DT>;
     pg_u32x4 q[PIECES];
     pg_f32x4 acc[8];            // bfloat16: [m][x] is dimension 8 (4 kg + x) + m; float32: [4 h + c][x] is 64 h + 4 (4 kg + x) + c
-    float m, l;                 // l: of the lane's own rows
+    float m, l;                 // the maximum of <q, k>, and the weights' sum, of the lane's own rows
 
     // queries of heads 0 .. n - 1 of a tile, 128 values each; columns past them are the first one's, and nobody asks for them
     __device__ __forceinline__ void start(const void* q0, int n, int lane) {
@@ -84,17 +85,17 @@ struct PgWave {
                     S[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[e]), __uint_as_float(q[i][e]), S[e], 0, 0, 0);
         }
         const bool mine = !ONE || r == head;
-        float z[4], top = PG_LOWEST;
+        float z[4], top = -INFINITY;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             z[j] = DT == RA_BF16 ? S[0][j] + S[1][j] : (S[0][j] + S[1][j]) + (S[PIECES / 2 - 2][j] + S[PIECES / 2 - 1][j]);
             z[j] = mine && (c.there >> j) & 1u ? z[j] : -INFINITY;
             top = fmaxf(top, z[j]);
         }
-        if (__builtin_amdgcn_ballot_w64(top * PG_C > m + 8.f) != 0ull) {
+        if (__builtin_amdgcn_ballot_w64(top > m + PG_LAG) != 0ull) {
             top = fmaxf(top, __uint_as_float(lane_xor32<16>(__float_as_uint(top), lane)));
             top = fmaxf(top, __uint_as_float(lane_xor32<32>(__float_as_uint(top), lane)));
-            const float now = fmaxf(m, top * PG_C), corr = __builtin_amdgcn_exp2f(m - now);
+            const float now = fmaxf(m, top), corr = __builtin_amdgcn_exp2f((m - now) * PG_C);
             m = now;
             l *= corr;
 #pragma unroll
@@ -103,7 +104,7 @@ struct PgWave {
         float x[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            x[j] = __builtin_amdgcn_exp2f(fmaf(z[j], PG_C, -m));
+            x[j] = __builtin_amdgcn_exp2f((z[j] - m) * PG_C);
             l += x[j];
         }
         if constexpr (DT == RA_BF16) {
@@ -153,8 +154,9 @@ struct PgWave {
 };
 
 #define PG_PAD (RA_D + 4)
+template <int WAVES>
 struct PgLds {
-    float a[PG_WAVES][PG_HEADS][PG_PAD], m[PG_WAVES][PG_HEADS], l[PG_WAVES][PG_HEADS];
+    float a[WAVES][PG_HEADS][PG_PAD], m[WAVES][PG_HEADS], l[WAVES][PG_HEADS];
     // (a wavefront's keys and later its sums lie in the same place)
     __device__ __forceinline__ pg_u32x4* stage(int wv) { return reinterpret_cast<pg_u32x4*>(&a[wv][0][0]); }
 };
@@ -162,8 +164,8 @@ static_assert(sizeof(float[PG_HEADS][PG_PAD]) >= PG_CHUNK * PG_ROW<RA_BF16> && s
               sizeof(float[PG_HEADS][PG_PAD]) % 16 == 0, "a chunk of keys fits");
 
 // A wavefront's state for the first n heads into shared memory; a head without rows has the maximum -infinity.
-template <int DT>
-__device__ __forceinline__ void pg_leave(const PgWave<DT>& s, PgLds& lds, int n, int wv, int lane) {
+template <int DT, int WAVES>
+__device__ __forceinline__ void pg_leave(const PgWave<DT>& s, PgLds<WAVES>& lds, int n, int wv, int lane) {
     const int kg = lane >> 4, col = lane & 15;
     float l = s.l + __uint_as_float(lane_xor32<16>(__float_as_uint(s.l), lane));
     l += __uint_as_float(lane_xor32<32>(__float_as_uint(l), lane));
@@ -182,23 +184,25 @@ __device__ __forceinline__ void pg_leave(const PgWave<DT>& s, PgLds& lds, int n,
         }
 }
 // dimension d of head h from the states of the first `of_w` wavefronts, and of the others. No branches: all that is read is on its way at once.
-__device__ __forceinline__ void pg_together(const PgLds& lds, int of_w, int h, int d, RecSum (&x)[2]) {
-    float m[PG_WAVES], l[PG_WAVES], a[PG_WAVES];
+template <int WAVES>
+__device__ __forceinline__ void pg_together(const PgLds<WAVES>& lds, int of_w, int h, int d, RecSum (&x)[2]) {
+    float m[WAVES], l[WAVES], a[WAVES];
 #pragma unroll
-    for (int w = 0; w < PG_WAVES; ++w) { m[w] = lds.m[w][h]; l[w] = lds.l[w][h]; a[w] = lds.a[w][h][d]; }
+    for (int w = 0; w < WAVES; ++w) { m[w] = lds.m[w][h]; l[w] = lds.l[w][h]; a[w] = lds.a[w][h][d]; }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         x[i] = RecSum{-INFINITY, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < PG_WAVES; ++w) x[i].m = fmaxf(x[i].m, (w < of_w) == (i == 0) ? m[w] : -INFINITY);
+        for (int w = 0; w < WAVES; ++w) x[i].m = fmaxf(x[i].m, (w < of_w) == (i == 0) ? m[w] : -INFINITY);
         const float base = x[i].m > -INFINITY ? x[i].m : 0.f;
 #pragma unroll
-        for (int w = 0; w < PG_WAVES; ++w) {                // (a wavefront without rows has sums of zero)
+        for (int w = 0; w < WAVES; ++w) {                // (a wavefront without rows has sums of zero)
             const bool is = (w < of_w) == (i == 0);
-            const float wt = is ? __builtin_amdgcn_exp2f(m[w] - base) : 0.f;
+            const float wt = is ? __builtin_amdgcn_exp2f((m[w] - base) * PG_C) : 0.f;
             x[i].a = fmaf(is ? a[w] : 0.f, wt, x[i].a);
             x[i].l = fmaf(is ? l[w] : 0.f, wt, x[i].l);
         }
+        x[i].m *= PG_C;
     }
 }
 
@@ -288,7 +292,7 @@ __global__ __launch_bounds__(PG_WAVES * RA_WAVE, DT == RA_BF16 ? 4 : 2) void pg_
                                                                 const int32_t* __restrict__ n_tokens, int tiles, int unit_log2, int whole,
                                                                 float* __restrict__ partials, float* __restrict__ out, float* __restrict__ lse) {
     extern __shared__ __align__(16) char pg_lds[];
-    PgLds& lds = *reinterpret_cast<PgLds*>(pg_lds);
+    PgLds<PG_WAVES>& lds = *reinterpret_cast<PgLds<PG_WAVES>*>(pg_lds);
     const int jobs = n_kv * tiles, group = n_q / n_kv, wg = blockIdx.x;
     uint32_t at = 0, end = 1, first = 0;
     int seq = wg / jobs;
@@ -425,12 +429,13 @@ __global__ __launch_bounds__(RA_D * PG_MERGE_SLICES) void pg_full_merge_kernel(c
 
 #define PG_MOST_ROWS (1 << 24)      // of one job that a workgroup takes alone
 struct PgCut { int tiles, workgroups, unit_log2; bool whole; const char* refused; };       // refused: why, or null
-static PgCut pg_cut(int n_seq, int n_q, int n_kv, int64_t N) {
+static PgCut pg_cut(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N) {
     PgCut x;
     x.tiles = (int)(((int64_t)(n_q / n_kv) + PG_HEADS - 1) / PG_HEADS);
     const int64_t jobs = (int64_t)n_seq * n_kv * x.tiles;
     // (from PG_MOST_UNITS jobs on there is no list: its units, and the threads of the second kernel, 128 for each of up to 16 heads, fit 32 bits)
-    x.whole = N <= 640 || N <= (jobs < 128 ? 16 * jobs : 2048) || (jobs >= PG_MOST_UNITS && N <= PG_MOST_ROWS);
+    const int64_t few = dt == RA_BF16 ? 640 : 320, per_job = dt == RA_BF16 ? 16 : 4;
+    x.whole = N <= few || (N <= 2048 && N <= per_job * jobs) || (jobs >= PG_MOST_UNITS && N <= PG_MOST_ROWS);
     x.unit_log2 = jobs * N <= 2 * PG_UNIT * PG_MOST_WORKGROUPS ? 6 : 7;
     static_assert(PG_UNIT == 1 << 6, "rows of a unit");
     x.refused = x.whole && jobs >= 1 << 23 ? "too many heads for one launch: 2^23 tiles of up to 16 query heads"
@@ -443,20 +448,20 @@ static PgCut pg_cut(int n_seq, int n_q, int n_kv, int64_t N) {
     return x;
 }
 
-size_t ra_full_paged_partial_floats(int n_seq, int n_q, int n_kv, int64_t N) {
-    const PgCut x = pg_cut(n_seq, n_q, n_kv, N);
+size_t ra_full_paged_partial_floats(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N) {
+    const PgCut x = pg_cut(dt, n_seq, n_q, n_kv, N);
     return x.whole || x.refused ? 0 : ((size_t)x.workgroups + (size_t)n_seq * n_kv * x.tiles) * PG_HEADS * (RA_D + 2);
 }
 
 ra_status ra_launch_full_paged(const void* q, ra_dtype dt, const PgCache& c, int n_seq, int n_q, int n_kv, int64_t N, const int32_t* n_tokens,
                                float* partials, hipStream_t st, float* out, float* lse) {
-    const PgCut x = pg_cut(n_seq, n_q, n_kv, N);
+    const PgCut x = pg_cut(dt, n_seq, n_q, n_kv, N);
     if (x.refused) RA_FAIL(RA_EUNSUP, "%s", x.refused);
 #define PG_GO(DTV, SMALL)                                                                                                                             \
     do {                                                                                                                                              \
         constexpr auto kernel = &pg_full_kernel<DTV, SMALL>;                                                                                          \
-        RA_LDS_OPT_IN(*kernel, sizeof(PgLds));                                                                                              \
-        hipLaunchKernelGGL(*kernel, dim3(x.workgroups), dim3(PG_WAVES * RA_WAVE), sizeof(PgLds), st, q, c, c.table, n_seq, n_q, n_kv, (int)N, \
+        RA_LDS_OPT_IN(*kernel, sizeof(PgLds<PG_WAVES>));                                                                                              \
+        hipLaunchKernelGGL(*kernel, dim3(x.workgroups), dim3(PG_WAVES * RA_WAVE), sizeof(PgLds<PG_WAVES>), st, q, c, c.table, n_seq, n_q, n_kv, (int)N, \
                            n_tokens, x.tiles, x.unit_log2, (int)x.whole, partials, out, lse);                                                         \
     } while (0)
     if (c.page_log2 < 4) { if (dt == RA_BF16) PG_GO(RA_BF16, true); else PG_GO(RA_F32, true); }
@@ -492,12 +497,12 @@ __device__ __forceinline__ PgSets pg_sets(const int32_t* n_tokens, const int32_t
 // A job is a KV head of a sequence, and up to 16 of its query heads: chunks of W, for all of the heads, and of each head's Omega. It is cut into
 // `parts` workgroups, each of which takes an equal stretch of either list and shares its wavefronts out between the two.
 // They leave a record of each set per head, or, where a job is one workgroup's, the results. grid: jobs x parts.
-template <int DT>
-__global__ __launch_bounds__(PG_WAVES * RA_WAVE, DT == RA_BF16 ? 4 : 2) void pg_attend_kernel(
+template <int DT, int WAVES>
+__global__ __launch_bounds__(WAVES * RA_WAVE, DT == RA_BF16 ? 4 : 2) void pg_attend_kernel(
     const void* __restrict__ q, PgCache c, int n_q, int n_kv, int N, const int32_t* __restrict__ n_tokens, const int32_t* __restrict__ n_indexed,
     int sink, int window, int topk, const int32_t* __restrict__ ids, int parts, int tiles, float* __restrict__ partials, SetOut o) {
     extern __shared__ __align__(16) char pg_lds[];
-    PgLds& lds = *reinterpret_cast<PgLds*>(pg_lds);
+    PgLds<WAVES>& lds = *reinterpret_cast<PgLds<WAVES>*>(pg_lds);
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid / RA_WAVE);
     const int group = n_q / n_kv, part = blockIdx.x % parts, job = blockIdx.x / parts, kv_head = job / tiles, seq = kv_head / n_kv;
     const int first = job % tiles * PG_HEADS, heads = group - first < PG_HEADS ? group - first : PG_HEADS;
@@ -508,11 +513,11 @@ __global__ __launch_bounds__(PG_WAVES * RA_WAVE, DT == RA_BF16 ? 4 : 2) void pg_
     auto cut = [&](int chunks, int p) { return (int)((int64_t)chunks * p / parts); };
     const int w0 = cut(in_w, part), ws = cut(in_w, part + 1) - w0, g0 = cut(in_om, part), gs = cut(in_om, part + 1) - g0;
     // wavefronts of W's chunks; the others have Omega's
-    int of_w = (PG_WAVES * ws + (ws + gs) / 2) / (ws + gs > 0 ? ws + gs : 1);
+    int of_w = (WAVES * ws + (ws + gs) / 2) / (ws + gs > 0 ? ws + gs : 1);
     if (of_w < 1 && ws > 0) of_w = 1;
-    if (of_w > PG_WAVES - 1 && gs > 0) of_w = PG_WAVES - 1;
+    if (of_w > WAVES - 1 && gs > 0) of_w = WAVES - 1;
     const bool om = wv >= of_w;
-    const int step = om ? PG_WAVES - of_w : of_w, chunks = om ? gs : ws, r = lane & 15;
+    const int step = om ? WAVES - of_w : of_w, chunks = om ? gs : ws, r = lane & 15;
     PgWave<DT> st;
     st.start(reinterpret_cast<const char*>(q) + head0 * PG_ROW<DT>, heads, lane);
     PgChunk<DT> a;
@@ -551,7 +556,7 @@ __global__ __launch_bounds__(PG_WAVES * RA_WAVE, DT == RA_BF16 ? 4 : 2) void pg_
     }
     pg_leave(st, lds, heads, wv, lane);
     __syncthreads();
-    for (int y = tid; y < heads * RA_D; y += PG_WAVES * RA_WAVE) {
+    for (int y = tid; y < heads * RA_D; y += WAVES * RA_WAVE) {
         const int hd = y / RA_D, d = y % RA_D;
         RecSum both[2];
         pg_together(lds, of_w, hd, d, both);
@@ -618,16 +623,18 @@ ra_status ra_launch_attend_paged(const void* q, ra_dtype dt, const PgCache& c, i
     int tiles;
     const int parts = pg_parts(dt, n_seq, n_q, n_kv, N, sink, window, topk, &tiles);
     const int64_t blocks = (int64_t)n_seq * n_kv * tiles * parts;
-    if (blocks > (1 << 23) - 1) RA_FAIL(RA_EUNSUP, "too many heads for one launch");
+    if (blocks > (1 << 22) - 1) RA_FAIL(RA_EUNSUP, "too many heads for one launch");
     const SetOut o{nullptr, out, lse, o_omega, lse_omega, o_w, lse_w};
-#define PG_GO(DTV)                                                                                                                              \
+#define PG_GO(DTV, W)                                                                                                                           \
     do {                                                                                                                                        \
-        constexpr auto kernel = &pg_attend_kernel<DTV>;                                                                                         \
-        RA_LDS_OPT_IN(*kernel, sizeof(PgLds));                                                                                                  \
-        hipLaunchKernelGGL(*kernel, dim3((unsigned)blocks), dim3(PG_WAVES * RA_WAVE), sizeof(PgLds), st, q, c, n_q, n_kv, (int)N, n_tokens,     \
+        constexpr auto kernel = &pg_attend_kernel<DTV, W>;                                                                                      \
+        RA_LDS_OPT_IN(*kernel, sizeof(PgLds<W>));                                                                                               \
+        hipLaunchKernelGGL(*kernel, dim3((unsigned)blocks), dim3(W * RA_WAVE), sizeof(PgLds<W>), st, q, c, n_q, n_kv, (int)N, n_tokens,         \
                            n_indexed, sink, window, topk, ids, parts, tiles, partials, o);                                                      \
     } while (0)
-    if (dt == RA_BF16) PG_GO(RA_BF16); else PG_GO(RA_F32);
+    if (dt == RA_F32) PG_GO(RA_F32, PG_WAVES);
+    else if (parts == 1) PG_GO(RA_BF16, 2 * PG_WAVES);
+    else PG_GO(RA_BF16, PG_WAVES);
 #undef PG_GO
     RA_HIP(hipGetLastError());
     if (parts == 1) return RA_OK;

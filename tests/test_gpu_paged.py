@@ -190,6 +190,25 @@ def test_flat_and_sharp_softmax(dtype, scale):
         check(out[0, h], lse[0, h], to_np(q[0, h]), *c.rows(0, 0, range(3001)))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_logits_near_the_lowest_number(dtype):
+    """All logits about -3e37, chunks without rows in front of them: equal weights."""
+    c = Cache([300], 1, 16, dtype, seed=10)
+    c.K.zero_()
+    c.K[..., 3] = -1.5e19
+    table = ints(c.table)
+    table[0, :9] = -1
+    q = torch.zeros((1, 2, 128))
+    q[..., 3] = 2.0e19
+    cache = ra.PagedCache(c.K, c.V, table)
+    ids = torch.arange(300, dtype=torch.int32, device=DEV).expand(1, 2, -1).contiguous()
+    V = c.rows(0, 0, range(144, 300))[1]
+    for out, lse in (ra.ra_full_attention_paged(q.to(dtype).to(DEV), cache, N=300), ra.ra_attend_paged(q.to(dtype).to(DEV), cache, 2, 20, ids, N=300)):
+        # (weights of 1, 156 of them: their sums and the division lose at most 160 roundings)
+        assert (np.abs(out[0].cpu().numpy() - V.mean(0)) <= 160 * U * np.abs(V).mean(0)).all()
+        assert np.allclose(lse.cpu().numpy(), -3.0e38 / np.sqrt(128), rtol=2.0 ** -7)
+
+
 # ---- the retrieved and the static set ------------------------------------------------------------
 ATTEND = [  # n_q, n_kv, page, lens, indexed (None: not given), sink, window, topk, holes
     (4, 2, 16, [300], None, 4, 32, 10, 0), (6, 2, 8, [700, 1, 0, 33], [650, 1, 0, 20], 4, 10, 129, 0), (3, 3, 64, [90, 50], None, 100, 100, 7, 0),
@@ -374,6 +393,37 @@ def test_gather(dtype, lens, n_kv, page, T, first):
 
 
 # ---- tables, pools, streams ----------------------------------------------------------------------------
+def test_calls_on_a_given_stream_are_the_same_calls():
+    """A stream given by hand goes through the checks in Python, none through compiled ones: every call, with results given and not."""
+    c = Cache([300, 77], 2, 16, torch.bfloat16, seed=14)
+    q, n, ids = queries(2, 4, torch.bfloat16, 14).to(DEV), ints([300, 77]), torch.randint(0, 300, (2, 4, 9), dtype=torch.int32, device=DEV)
+    x = torch.randn((2, 3, 8, 128), device=DEV).bfloat16()
+    w, f = torch.rand(128, device=DEV).bfloat16(), torch.from_numpy(_inv_freq(64)).to(DEV)
+    here = torch.cuda.current_stream()
+    res = lambda: dict(out=torch.empty((2, 4, 128), device=DEV), lse=torch.empty((2, 4), device=DEV),  # noqa: E731
+                       workspace=torch.empty(1 << 22, dtype=torch.uint8, device=DEV))
+    for N in (None, 200):
+        for n_tokens in (None, n):
+            a, b = ({**(res() if i else {})} for i in range(2))
+            one, two = ra.ra_full_attention_paged(q, c.gpu, n_tokens, N, **a), ra.ra_full_attention_paged(q, c.gpu, n_tokens, N, stream=here, **b)
+            assert all(torch.equal(torch.nan_to_num(x), torch.nan_to_num(y)) for x, y in zip(one, two))
+            for indexed in (None, ints([250, 70])):
+                one, two = (ra.ra_attend_paged(q, c.gpu, 3, 40, ids, n_tokens, indexed, N, stream=s, **kw) for s, kw in ((None, res()), (here, {})))
+                assert all(torch.equal(torch.nan_to_num(x), torch.nan_to_num(y)) for x, y in zip(one, two))
+    for parts in ((0, 1, 2), (0,), (1,), (2, 1)):
+        for n_new in (None, ints([2, 3])):
+            got = []
+            for s in (None, here):
+                t = [v if i in parts else None for i, v in enumerate(x.split((4, 2, 2), dim=2))]
+                cache = ra.PagedCache(torch.zeros_like(c.K), torch.zeros_like(c.V), ints(c.table))
+                out = ra.ra_append_tokens_paged(*t, ints([5, 60]), cache, n_new=n_new, q_weight=w, k_weight=w, eps=1e-5, inv_freq=f, interleaved=True,
+                                                rot_scale=1.5, stream=s)
+                got.append((out, cache.K, cache.V))
+            for one, two in zip(*got):
+                assert (one is None and two is None) or torch.equal(one, two)
+            assert (got[0][0] is None) == (0 not in parts) and (got[0][1] != 0).any() == (1 in parts) and (got[0][2] != 0).any() == (2 in parts)
+
+
 def test_tables_that_are_parts_of_larger_ones():
     c = Cache([300, 250, 100], 2, 16, torch.bfloat16, seed=8)
     big = torch.full((7, 50), 9, dtype=torch.int32, device=DEV)

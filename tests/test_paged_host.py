@@ -83,8 +83,8 @@ def test_calls_that_are_refused(name, change, cache, status, needle):
 def test_workspace_sizes():
     L = ra.lib()
     full, attend = L.ra_full_attention_paged_workspace_bytes, L.ra_attend_paged_workspace_bytes
-    assert full(1, 32, 8, 131072) > 256 and full(1, 4, 1, 1) == 256
-    assert full(1, 32, 7, 1000) == 0 and full(1, 32, 8, 0) == 0 and full(1, 32, 8, 1 << 31) == 0 and full(0, 4, 1, 10) == 0
+    assert full(1, 1, 32, 8, 131072) > 256 and full(0, 1, 4, 1, 1) == 256 and full(2, 1, 4, 1, 1) == 0
+    assert full(1, 1, 32, 7, 1000) == 0 and full(1, 1, 32, 8, 0) == 0 and full(1, 1, 32, 8, 1 << 31) == 0 and full(1, 0, 4, 1, 10) == 0
     assert attend(1, 1, 32, 8, 1000, 4, 640, 100) >= 256 + 32 * 2 * 2 * 132 * 4 and attend(0, 1, 32, 8, 1000, 0, 0, 1) == 256
     for bad in ((1, 1, 32, 7, 1000, 4, 640, 100), (1, 1, 32, 8, 0, 4, 640, 100), (1, 1, 32, 8, 1000, -1, 640, 100), (1, 1, 32, 8, 1000, 4, -1, 100),
                 (1, 1, 32, 8, 1000, 4, 640, 0), (1, 1, 32, 8, 1000, 4, 640, 2049), (2, 1, 32, 8, 1000, 4, 640, 100)):
