@@ -444,7 +444,8 @@ static PgCut pg_cut(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N) {
     if (x.whole || x.refused) return x;
     auto units = [&] { return jobs * ((N + ((int64_t)1 << x.unit_log2) - 1) >> x.unit_log2); };
     while (units() > PG_MOST_UNITS) ++x.unit_log2;
-    x.workgroups = (int)(units() < PG_MOST_WORKGROUPS ? units() : PG_MOST_WORKGROUPS);
+    const int64_t most = (units() + ROW_LEAST_UNITS - 1) / ROW_LEAST_UNITS;           // (with more, some would have nothing to do)
+    x.workgroups = (int)(most < PG_MOST_WORKGROUPS ? most : PG_MOST_WORKGROUPS);
     return x;
 }
 
