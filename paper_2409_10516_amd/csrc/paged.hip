@@ -32,13 +32,18 @@ typedef uint32_t pg_u32x4 __attribute__((ext_vector_type(4), may_alias));
 //   sums    O[dimension][head] += V^T P. The lane's weights are of rows 4 kg + i, so they go in as they come out; V^T wants the same rows:
 //           lane (kg, r) has 16 bytes of each (16 lanes read a row, or half of a float32 one).
 // Keys are read like values, whole lines an instruction, and turn into the first product's layout through shared memory of the wavefront's
-// own, a piece p of row r at place p ^ r of the row, so that neither side meets in a bank.
+// own, a piece p of row r at place p ^ r of the row, so that neither side meets in a bank (no conflicts counted). Read in that layout from memory, 64
+// bytes of each of 16 rows an instruction, half of a line is fetched again where rows are not kept (65536 float32 rows of 8 heads 124 us a call,
+// this way 103; bfloat16 96, 94).
 // bfloat16: v_mfma_f32_16x16x32_bf16 for the logits, sums of exact products, and v_mfma_f32_16x16x16_bf16 for the sums. A float32 weight
 // goes in as three terms of bfloat16, the first as rounded, the next what the rounding left: all of its 24 bits. (An infinite value times the
 // lesser terms is not a number.)
 // float32: v_mfma_f32_16x16x4_f32, products and sums in float32.
 // The running maximum of a head moves only when a logit exceeds it by more than 8 (in powers of two), which keeps the
 // lanes' exchange and the scaling of sums out of nearly every chunk.
+// What bounds it is the memory: of a dispatch of 84 us over 131072 rows of 8 heads the vector instructions take a fifth and the matrix
+// instructions less; the same loads without the products take as long. One compute unit by itself takes in 57 GB a second: 9 ns a row, whatever
+// is on its way (the next chunk, or two, asked for ahead: 93.6 and 94.4 us a call, as it is 91.6).
 template <int DT>
 struct PgChunk {
     pg_u32x4 k[PG_PIECES<DT>], v[PG_PIECES<DT>];             // piece r of rows 4 kg + i at [i], float32: pieces r and 16 + r at [2 i] and [2 i + 1]
@@ -276,10 +281,12 @@ __device__ __forceinline__ void pg_fetch(PgChunk<DT>& c, const PgRows<DT>& src, 
 }
 
 // ---- attention over all tokens -----------------------------------------------------------------
-// The work is a list: per sequence, KV head and tile of its query heads (a job) the job's rows in units of 64 or, for lists that
-// would be too long for 32 bits, a power of two of these. Workgroups
+// The work is a list: per sequence, KV head and tile of its query heads (a job) the job's rows in units of 64, of 128 (a round of a workgroup's
+// wavefronts) where there are more than that for each, or, for lists that would be too long for 32 bits, a power of two of these. Workgroups
 // take equal stretches of that list, whatever the lengths of the sequences are, and leave a record per job they touched, at place
-// (workgroup + job): going along the list, one or the other grows by one at a time.
+// (workgroup + job): going along the list, one or the other grows by one at a time. One workgroup of eight wavefronts per compute unit (us a call,
+// 131072 rows of 8 heads and 16 sequences of up to 32768: 91.5, 170.6; two of eight 93.2, 173.2, one of 16 93.2, 172.9, two, three and four of
+// four wavefronts 92.0, 93.9 and 94.5, 170.7, 172 and 176.3).
 // Records lie per head of a tile, then place: sums [16][places][128], then maxima and sums of weights [16][places][2], so that
 // what is combined lies in a row.
 // A launch of as many workgroups as jobs (`whole`) gives each its job, and the workgroup writes the result.
@@ -288,9 +295,9 @@ __device__ __forceinline__ void pg_fetch(PgChunk<DT>& c, const PgRows<DT>& src, 
 #define PG_MOST_WORKGROUPS 256      // one per compute unit
 
 template <int DT, bool SMALL>
-__global__ __launch_bounds__(PG_WAVES * RA_WAVE, DT == RA_BF16 ? 4 : 2) void pg_full_kernel(const void* __restrict__ q, PgCache c, const int32_t* __restrict__ table, int n_seq, int n_q, int n_kv, int N,
-                                                                const int32_t* __restrict__ n_tokens, int tiles, int unit_log2, int whole,
-                                                                float* __restrict__ partials, float* __restrict__ out, float* __restrict__ lse) {
+__global__ __launch_bounds__(PG_WAVES * RA_WAVE, DT == RA_BF16 ? 4 : 2) void pg_full_kernel(
+    const void* __restrict__ q, PgCache c, const int32_t* __restrict__ table, int n_seq, int n_q, int n_kv, int N, const int32_t* __restrict__ n_tokens,
+    int tiles, int unit_log2, int whole, float* __restrict__ partials, float* __restrict__ out, float* __restrict__ lse) {
     extern __shared__ __align__(16) char pg_lds[];
     PgLds<PG_WAVES>& lds = *reinterpret_cast<PgLds<PG_WAVES>*>(pg_lds);
     const int jobs = n_kv * tiles, group = n_q / n_kv, wg = blockIdx.x;
@@ -427,6 +434,11 @@ __global__ __launch_bounds__(RA_D * PG_MERGE_SLICES) void pg_full_merge_kernel(c
     if (d == 0) lse[head] = x.m > -INFINITY ? x.m * REC_LN2 + logf(x.l) : -INFINITY;
 }
 
+// How a call is cut. Each job is one workgroup's, and there is no second launch, where its rows are few or the jobs many enough to fill the part: by
+// themselves and shared out, us, bfloat16: 8 jobs of 250 rows 5.3, 7.8, of 500 7.5, 7.8, of 1000 11.1, 8.0; 128 of 500 9.3, 12.5, of 1000 16.3, 18.7,
+// of 2000 27.5, 28.3; 512 of 500 24.5, 31.2, of 2000 86.3, 91.2; float32: 8 of 250 8.8, 9.5, of 400 12.2, 11.1; 128 of 250 11.0, 13.3, of 500 19.5,
+// 19.2, of 1000 32.3, 29.5; 512 of 500 54.8, 59.3, of 2000 185, 191. No more than 2048 rows: the lengths are known on the device only, and what a
+// job that is longer than the others takes alone is 9 ns a row (float32: 26).
 #define PG_MOST_ROWS (1 << 24)      // of one job that a workgroup takes alone
 struct PgCut { int tiles, workgroups, unit_log2; bool whole; const char* refused; };       // refused: why, or null
 static PgCut pg_cut(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N) {
@@ -497,7 +509,9 @@ __device__ __forceinline__ PgSets pg_sets(const int32_t* n_tokens, const int32_t
 
 // A job is a KV head of a sequence, and up to 16 of its query heads: chunks of W, for all of the heads, and of each head's Omega. It is cut into
 // `parts` workgroups, each of which takes an equal stretch of either list and shares its wavefronts out between the two.
-// They leave a record of each set per head, or, where a job is one workgroup's, the results. grid: jobs x parts.
+// They leave a record of each set per head, or, where a job is one workgroup's, the results. grid: jobs x parts. What bounds it is the way from the
+// lengths and ids to the table and from there to the rows, three trips, and the second launch; where jobs are many, scattered rows (256 jobs of 644
+// static rows and 4 x 100 ids, 137 MB, 34 us).
 template <int DT, int WAVES>
 __global__ __launch_bounds__(WAVES * RA_WAVE, DT == RA_BF16 ? 4 : 2) void pg_attend_kernel(
     const void* __restrict__ q, PgCache c, int n_q, int n_kv, int N, const int32_t* __restrict__ n_tokens, const int32_t* __restrict__ n_indexed,
@@ -601,8 +615,12 @@ __global__ __launch_bounds__(2 * RA_D * SLICES) void pg_merge_kernel(const float
     rec_write(set, head, d, o);
 }
 
-// How a job is cut: a round of chunks for a workgroup's wavefronts each, up to so many workgroups that each has a compute unit to itself; one
-// where the jobs are many. Tokens that have come since the index was built are not counted, nobody here knows how many they are.
+// How a job is cut: half a round of chunks for a workgroup's wavefronts each, up to so many workgroups that each has a compute unit to itself
+// (us, a whole round and half of one: 8 jobs of 644 static rows and 4 x 100 ids 9.8, 9.7, with 2000 static rows 12.6, 10.6, with 30000
+// 59.5, 41.5, float32 13.9, 12.6; 16 query heads of one KV head 12.0, 13.1). Tokens that have come since the index was built are not counted, nobody
+// here knows how many they are.
+// Many jobs are one workgroup's each (128 of them, bfloat16, by themselves with 16 wavefronts 18.2, with eight 19.9, in two 19.6 and a launch more;
+// 64 14.8, in four 13.5; float32, which has registers for eight wavefronts: 128 48, in two 40).
 static int pg_parts(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N, int sink, int window, int topk, int* tiles) {
     const int group = n_q / n_kv, heads = group < PG_HEADS ? group : PG_HEADS;
     *tiles = (group + PG_HEADS - 1) / PG_HEADS;
