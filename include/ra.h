@@ -403,7 +403,7 @@ ra_status ra_full_attention_paged(const void* q, const ra_paged_cache* cache, in
  * with n = min(n_tokens[s], N) and n_i = min(n_indexed[s], n) (device int32; NULL: N, and n) W = [0, sink) u [min(n - window, n_i), n):
  * tokens behind the n_i that the index was built over are static. Entries of ids that are not in [0, n), or are members of W (they are
  * attended there), are skipped; one that is given twice counts twice. Rows without a page are not attended. Weights have 24 bits.
- * RA_EUNSUP past 2^22 - 1 workgroups, one for up to 16 query heads of a KV head at least.
+ * RA_EUNSUP past 65535 sequences, 65535 tiles of up to 16 query heads of a KV head, or 2^22 - 1 of both.
  * workspace: as above, of ra_attend_paged_workspace_bytes(...) bytes. */
 size_t ra_attend_paged_workspace_bytes(ra_dtype dt, int n_seq, int n_q_heads, int n_kv_heads, int64_t N, int sink, int window, int topk);
 ra_status ra_attend_paged(const void* q, const ra_paged_cache* cache, int n_q_heads, int64_t N, int d, const int32_t* n_tokens,

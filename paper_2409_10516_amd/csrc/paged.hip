@@ -162,6 +162,7 @@ struct PgWave {
 template <int WAVES>
 struct PgLds {
     float a[WAVES][PG_HEADS][PG_PAD], m[WAVES][PG_HEADS], l[WAVES][PG_HEADS];
+    int row[WAVES][PG_CHUNK], page[WAVES][PG_CHUNK];         // the sparse set's: rows and pages of Omega's first chunks
     // (a wavefront's keys and later its sums lie in the same place)
     __device__ __forceinline__ pg_u32x4* stage(int wv) { return reinterpret_cast<pg_u32x4*>(&a[wv][0][0]); }
 };
@@ -497,9 +498,12 @@ ra_status ra_launch_full_paged(const void* q, ra_dtype dt, const PgCache& c, int
 // W of a sequence, [0, s) u [w, n); ranges that meet make everything static. The host knows neither n nor how many tokens came after
 // the index was built; what the parts of a job take is worked out here.
 struct PgSets { int s, w, count; };         // count: rows of W
-__device__ __forceinline__ PgSets pg_sets(const int32_t* n_tokens, const int32_t* n_indexed, int seq, int N, int sink, int window) {
+// lens: n_tokens[seq] in lane 0 and n_indexed[seq] in lane 1
+__device__ __forceinline__ PgSets pg_sets(int lens, bool has_tokens, bool has_indexed, int N, int sink, int window) {
     PgSets x;
-    const int n = seq_rows(n_tokens, seq, N), indexed = n_indexed ? seq_rows(n_indexed, seq, n) : n;
+    const int given = __builtin_amdgcn_readlane(lens, 0), given_indexed = __builtin_amdgcn_readlane(lens, 1);
+    auto upto = [](int v, int most) { return v < 0 ? 0 : v < most ? v : most; };
+    const int n = has_tokens ? upto(given, N) : N, indexed = has_indexed ? upto(given_indexed, n) : n;
     x.s = sink < n ? sink : n;
     const int w = window < n ? n - window : 0, late = w < indexed ? w : indexed;
     x.w = late > x.s ? late : x.s;
@@ -509,59 +513,84 @@ __device__ __forceinline__ PgSets pg_sets(const int32_t* n_tokens, const int32_t
 
 // A job is a KV head of a sequence, and up to 16 of its query heads: chunks of W, for all of the heads, and of each head's Omega. It is cut into
 // `parts` workgroups, each of which takes an equal stretch of either list and shares its wavefronts out between the two.
-// They leave a record of each set per head, or, where a job is one workgroup's, the results. grid: jobs x parts. What bounds it is the way from the
+// They leave a record of each set per head, or, where a job is one workgroup's, the results. grid: x = part, y = KV head (with its tile), z = sequence. What bounds it is the way from the
 // lengths and ids to the table and from there to the rows, three trips, and the second launch; where jobs are many, scattered rows (256 jobs of 644
 // static rows and 4 x 100 ids, 137 MB, 34 us).
 template <int DT, int WAVES>
 __global__ __launch_bounds__(WAVES * RA_WAVE, DT == RA_BF16 ? 4 : 2) void pg_attend_kernel(
-    const void* __restrict__ q, PgCache c, int n_q, int n_kv, int N, const int32_t* __restrict__ n_tokens, const int32_t* __restrict__ n_indexed,
-    int sink, int window, int topk, const int32_t* __restrict__ ids, int parts, int tiles, float* __restrict__ partials, SetOut o) {
+    const void* __restrict__ q, PgCache c, const int32_t* __restrict__ table, int group, int n_kv, int N, const int32_t* __restrict__ n_tokens,
+    const int32_t* __restrict__ n_indexed, int sink, int window, int topk, int per_head, const int32_t* __restrict__ ids, int tiles,
+    float* __restrict__ partials, SetOut o) {
     extern __shared__ __align__(16) char pg_lds[];
     PgLds<WAVES>& lds = *reinterpret_cast<PgLds<WAVES>*>(pg_lds);
-    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid / RA_WAVE);
-    const int group = n_q / n_kv, part = blockIdx.x % parts, job = blockIdx.x / parts, kv_head = job / tiles, seq = kv_head / n_kv;
-    const int first = job % tiles * PG_HEADS, heads = group - first < PG_HEADS ? group - first : PG_HEADS;
-    const size_t head0 = (size_t)seq * n_q + (size_t)(kv_head % n_kv) * group + first;
-    const PgSets set = pg_sets(n_tokens, n_indexed, seq, N, sink, window);
-    const PgRows<DT> src(c, c.table, seq, kv_head % n_kv, n_kv);
-    const int per_head = (topk + PG_CHUNK - 1) / PG_CHUNK, in_w = (set.count + PG_CHUNK - 1) / PG_CHUNK, in_om = heads * per_head;
-    auto cut = [&](int chunks, int p) { return (int)((int64_t)chunks * p / parts); };
-    const int w0 = cut(in_w, part), ws = cut(in_w, part + 1) - w0, g0 = cut(in_om, part), gs = cut(in_om, part + 1) - g0;
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid / RA_WAVE), r = lane & 15;
+    const int part = blockIdx.x, parts = gridDim.x, seq = blockIdx.z;
+    const int kv_head = tiles == 1 ? (int)blockIdx.y : (int)blockIdx.y / tiles, first = tiles == 1 ? 0 : (int)blockIdx.y % tiles * PG_HEADS;
+    const int heads = group - first < PG_HEADS ? group - first : PG_HEADS;
+    const size_t head0 = ((size_t)seq * n_kv + kv_head) * group + first;
+    const PgRows<DT> src(c, table, seq, kv_head, n_kv);
+    // the lengths, one lane's load each; the table's first entry where one is not given
+    const int32_t *at_tokens = n_tokens ? n_tokens + seq : table, *at_indexed = n_indexed ? n_indexed + seq : table;
+    const int lens = *(lane & 1 ? at_indexed : at_tokens);
+    // the part's stretch of a list
+    auto cut = [&](uint32_t chunks, int& from, int& many) {
+        const uint32_t each = chunks / (uint32_t)parts, more = chunks - each * parts;
+        from = (int)(each * part + min((uint32_t)part, more));
+        many = (int)(each + ((uint32_t)part < more ? 1u : 0u));
+    };
+    int w0, ws, g0, gs;
+    const int in_om = heads * per_head;
+    cut(in_om, g0, gs);
+    // chunk i of the part's Omega: row r of it (-1 past a head's list)
+    auto id_of = [&](int i) {
+        const uint32_t x = g0 + i < in_om ? g0 + i : in_om - 1, h = x / (uint32_t)per_head;
+        const int j = (int)(x - h * per_head) * PG_CHUNK + r, id = ids[(head0 + h) * topk + (j < topk ? j : topk - 1)];
+        return j < topk ? id : -1;
+    };
+    // (a row's page is asked for before it is known whether the row is one)
+    auto page_of = [&](int row) { return src.page_of(row < 0 ? 0 : row); };
+    // What Omega's wavefronts begin with is asked for by all, while the lengths that say which these are are on their way (one sequence of 8 KV heads
+    // 8.9 -> 8.5 us; where a job is one workgroup's of 16 wavefronts, all of which would wait for it, 17.9 -> 18.9).
+    constexpr bool EARLY = WAVES == PG_WAVES;
+    if (EARLY && wv < gs) {
+        const int row = id_of(wv), page = page_of(row);
+        if (lane < PG_CHUNK) {
+            lds.row[wv][r] = row;
+            lds.page[wv][r] = page;
+        }
+    }
+    const PgSets set = pg_sets(lens, n_tokens != nullptr, n_indexed != nullptr, N, sink, window);
+    cut((set.count + PG_CHUNK - 1) / PG_CHUNK, w0, ws);
     // wavefronts of W's chunks; the others have Omega's
-    int of_w = (WAVES * ws + (ws + gs) / 2) / (ws + gs > 0 ? ws + gs : 1);
+    int of_w = (int)((uint32_t)(WAVES * ws + (ws + gs) / 2) / (uint32_t)(ws + gs > 0 ? ws + gs : 1));
     if (of_w < 1 && ws > 0) of_w = 1;
     if (of_w > WAVES - 1 && gs > 0) of_w = WAVES - 1;
     const bool om = wv >= of_w;
-    const int step = om ? WAVES - of_w : of_w, chunks = om ? gs : ws, r = lane & 15;
+    const int step = om ? WAVES - of_w : of_w, chunks = om ? gs : ws;
+    auto w_row_of = [&](int i) {
+        const int j = (w0 + i) * PG_CHUNK + r;
+        return j < set.s ? j : set.w - set.s + j;
+    };
+    int i = om ? wv - of_w : wv, row = om ? 0 : w_row_of(i), page = om ? 0 : src.page_of(row);
     PgWave<DT> st;
     st.start(reinterpret_cast<const char*>(q) + head0 * PG_ROW<DT>, heads, lane);
+    if (EARLY) __syncthreads();
     PgChunk<DT> a;
     // What leads to the next chunk's rows, their entries of the table and before these the ids, is asked for ahead of the current chunk's rows:
     // loads come back in order, and who waits for one behind the rows waits for the rows.
     if (!om) {
-        auto row_of = [&](int i) {
-            const int j = (w0 + i) * PG_CHUNK + r;
-            return j < set.s ? j : set.w - set.s + j;
-        };
-        int i = wv, row = row_of(i), page = i < chunks ? src.page_of(row) : 0;
         for (; i < chunks; i += step) {
-            const int next = row_of(i + step), next_page = src.page_of(next);
+            const int next = w_row_of(i + step), next_page = src.page_of(next);
             pg_fetch<false>(a, src, (w0 + i) * PG_CHUNK + r < set.count ? src.number(page, row) : -1, lane);
             st.template add<false>(a, lds.stage(wv), lane);
             row = next;
             page = next_page;
         }
-    } else {
-        auto row_of = [&](int i) {                           // (-1 past a head's list)
-            const int x = g0 + i < in_om ? g0 + i : in_om - 1, j = x % per_head * PG_CHUNK + r;
-            const int id = ids[(head0 + x / per_head) * topk + (j < topk ? j : topk - 1)];
-            return j < topk ? id : -1;
-        };
-        // (a row's page is asked for before it is known whether the row is one)
-        auto page_of = [&](int row) { return src.page_of(row < 0 ? 0 : row); };
-        int i = wv - of_w, row = row_of(i), next = row_of(i + step), page = page_of(row);
-        for (; i < chunks; i += step) {
-            const int next_page = page_of(next), after = row_of(i + 2 * step);
+    } else if (i < chunks) {
+        row = EARLY ? lds.row[i][r] : id_of(i);
+        page = EARLY ? lds.page[i][r] : page_of(row);
+        for (int next = i + step < chunks ? id_of(i + step) : -1; i < chunks; i += step) {
+            const int next_page = page_of(next), after = id_of(i + 2 * step);
             pg_fetch<false>(a, src, row >= set.s && row < set.w ? src.number(page, row) : -1, lane);      // (members of W are attended there)
             st.template add<true>(a, lds.stage(wv), lane, (g0 + i) / per_head);
             row = next;
@@ -641,15 +670,15 @@ ra_status ra_launch_attend_paged(const void* q, ra_dtype dt, const PgCache& c, i
                                  float* out, float* lse, float* o_omega, float* lse_omega, float* o_w, float* lse_w) {
     int tiles;
     const int parts = pg_parts(dt, n_seq, n_q, n_kv, N, sink, window, topk, &tiles);
-    const int64_t blocks = (int64_t)n_seq * n_kv * tiles * parts;
-    if (blocks > (1 << 22) - 1) RA_FAIL(RA_EUNSUP, "too many heads for one launch");
+    const int64_t per_seq = (int64_t)n_kv * tiles;
+    if (n_seq > 65535 || per_seq > 65535 || n_seq * per_seq * parts > (1 << 22) - 1) RA_FAIL(RA_EUNSUP, "too many heads for one launch");
     const SetOut o{nullptr, out, lse, o_omega, lse_omega, o_w, lse_w};
 #define PG_GO(DTV, W)                                                                                                                           \
     do {                                                                                                                                        \
         constexpr auto kernel = &pg_attend_kernel<DTV, W>;                                                                                      \
         RA_LDS_OPT_IN(*kernel, sizeof(PgLds<W>));                                                                                               \
-        hipLaunchKernelGGL(*kernel, dim3((unsigned)blocks), dim3(W * RA_WAVE), sizeof(PgLds<W>), st, q, c, n_q, n_kv, (int)N, n_tokens,         \
-                           n_indexed, sink, window, topk, ids, parts, tiles, partials, o);                                                      \
+        hipLaunchKernelGGL(*kernel, dim3(parts, (unsigned)per_seq, n_seq), dim3(W * RA_WAVE), sizeof(PgLds<W>), st, q, c, c.table, n_q / n_kv,  \
+                           n_kv, (int)N, n_tokens, n_indexed, sink, window, topk, (topk + PG_CHUNK - 1) / PG_CHUNK, ids, tiles, partials, o);   \
     } while (0)
     if (dt == RA_F32) PG_GO(RA_F32, PG_WAVES);
     else if (parts == 1) PG_GO(RA_BF16, 2 * PG_WAVES);
