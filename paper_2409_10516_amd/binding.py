@@ -784,8 +784,8 @@ def _calls():
             from . import _calls as m
         except ImportError as e:
             raise RuntimeError("_calls.so is missing or broken: build it as libra.so") from e
-        at = [C.cast(f, C.c_void_p).value for f in (L.ra_append_tokens_paged, L.ra_full_attention_paged, L.ra_full_attention_paged_workspace_bytes,
-                                                    L.ra_attend_paged, L.ra_attend_paged_workspace_bytes)]
+        at = [C.cast(f, C.c_void_p).value for f in (L.ra_append_tokens_paged, L.ra_gather_paged, L.ra_full_attention_paged,
+                                                    L.ra_full_attention_paged_workspace_bytes, L.ra_attend_paged, L.ra_attend_paged_workspace_bytes)]
         m.bind(_RAW or (lambda here: torch.cuda.current_stream(here).cuda_stream), *at)
         _short = m
     return _short
@@ -895,6 +895,11 @@ def ra_append_tokens_paged(q, k, v, first, cache: PagedCache, *, n_new=None, q_w
 def ra_gather_paged(cache: PagedCache, values: bool = False, first=None, rows: Optional[int] = None, out=None, stream=None):
     """Rows first[s] .. first[s] + rows (None: from 0, all that the table has entries for) of K, or with `values` of V, side by side
     -> [n_seq][n_kv][rows][128]; rows without a page are zero."""
+    if stream is None:
+        got = _short.gather(cache._core, values, first, rows, out)
+        if got.__class__ is tuple:
+            return got[0]
+        _check(got or 0)
     here = torch.cuda.current_device()
     room_for = _for(stream, here)
     ref = cache._of(here)

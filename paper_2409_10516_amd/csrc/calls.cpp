@@ -25,6 +25,7 @@ struct Cache {
 PyObject* raw_stream = nullptr;     // device -> handle of its current stream
 PyObject* device_number[64];
 decltype(&ra_append_tokens_paged) append_call = nullptr;
+decltype(&ra_gather_paged) gather_call = nullptr;
 decltype(&ra_full_attention_paged) full_call = nullptr;
 decltype(&ra_full_attention_paged_workspace_bytes) full_room = nullptr;
 decltype(&ra_attend_paged) attend_call = nullptr;
@@ -260,7 +261,38 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
                          (const int32_t*)first, (const int32_t*)n_new, st, out);
         Py_END_ALLOW_THREADS
         if (rc != RA_OK) return PyLong_FromLong(rc);
-        return PyTuple_Pack(1, made.defined() ? py::reinterpret_steal<py::object>(THPVariable_Wrap(made)).ptr() : a[12]);
+        PyObject* o = made.defined() ? THPVariable_Wrap(made) : Py_NewRef(a[12]);
+        PyObject* t1 = o ? PyTuple_Pack(1, o) : nullptr;
+        Py_XDECREF(o);
+        return t1;
+    });
+}
+
+// (cache, values, first, rows, out)
+PyObject* gather(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return careful([&]() -> PyObject* {
+        const Cache* c = n == 5 ? cache_of(a[0]) : nullptr;
+        const void *first, *out;
+        int64_t rows = 0;
+        if (!c || !PyBool_Check(a[1]) || !maybe(*c, a[2], at::kInt, {c->c.n_seq}, &first)) return nullptr;
+        if (a[3] == Py_None) rows = (int64_t)c->c.table_pages * c->c.page;
+        else if (!number(a[3], &rows)) return nullptr;
+        if (rows < 0) return nullptr;
+        const int64_t shape[4] = {c->c.n_seq, c->c.n_kv_heads, rows, 128};
+        at::Tensor made;
+        void* st;
+        if (a[4] == Py_None) out = (made = make(*c, shape, c->type)).const_data_ptr();
+        else out = data(*c, a[4], c->type, shape);
+        if (!out || !stream_of(*c, &st)) return nullptr;
+        ra_status rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = gather_call(&c->c, a[1] == Py_True, rows, 128, (const int32_t*)first, st, const_cast<void*>(out));
+        Py_END_ALLOW_THREADS
+        if (rc != RA_OK) return PyLong_FromLong(rc);
+        PyObject* o = made.defined() ? THPVariable_Wrap(made) : Py_NewRef(a[4]);
+        PyObject* t = o ? PyTuple_Pack(1, o) : nullptr;
+        Py_XDECREF(o);
+        return t;
     });
 }
 
@@ -282,17 +314,18 @@ PyObject* cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return PyCapsule_New(c, "paged", drop);
 }
 
-// (a device's current stream, addresses of the five functions)
+// (a device's current stream, addresses of the six functions)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (n != 6) return PyErr_Format(PyExc_TypeError, "bind takes 6 arguments");
-    void* at[5];
-    for (int i = 0; i < 5; ++i) at[i] = PyLong_AsVoidPtr(a[i + 1]);
+    if (n != 7) return PyErr_Format(PyExc_TypeError, "bind takes 7 arguments");
+    void* at[6];
+    for (int i = 0; i < 6; ++i) at[i] = PyLong_AsVoidPtr(a[i + 1]);
     if (PyErr_Occurred()) return nullptr;
     append_call = reinterpret_cast<decltype(append_call)>(at[0]);
-    full_call = reinterpret_cast<decltype(full_call)>(at[1]);
-    full_room = reinterpret_cast<decltype(full_room)>(at[2]);
-    attend_call = reinterpret_cast<decltype(attend_call)>(at[3]);
-    attend_room = reinterpret_cast<decltype(attend_room)>(at[4]);
+    gather_call = reinterpret_cast<decltype(gather_call)>(at[1]);
+    full_call = reinterpret_cast<decltype(full_call)>(at[2]);
+    full_room = reinterpret_cast<decltype(full_room)>(at[3]);
+    attend_call = reinterpret_cast<decltype(attend_call)>(at[4]);
+    attend_room = reinterpret_cast<decltype(attend_room)>(at[5]);
     for (int i = 0; i < 64; ++i)
         if (!device_number[i] && !(device_number[i] = PyLong_FromLong(i))) return nullptr;
     Py_XSETREF(raw_stream, Py_NewRef(a[0]));
@@ -300,7 +333,7 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 #define RA_METHOD(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(NAME)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {RA_METHOD(bind), RA_METHOD(cache), RA_METHOD(append), RA_METHOD(full), RA_METHOD(attend), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {RA_METHOD(bind), RA_METHOD(cache), RA_METHOD(append), RA_METHOD(gather), RA_METHOD(full), RA_METHOD(attend), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

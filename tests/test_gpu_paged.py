@@ -410,6 +410,10 @@ def test_calls_on_a_given_stream_are_the_same_calls():
             for indexed in (None, ints([250, 70])):
                 one, two = (ra.ra_attend_paged(q, c.gpu, 3, 40, ids, n_tokens, indexed, N, stream=s, **kw) for s, kw in ((None, res()), (here, {})))
                 assert all(torch.equal(torch.nan_to_num(x), torch.nan_to_num(y)) for x, y in zip(one, two))
+    for first, rows, values in ((None, None, False), (ints([3, -2]), 40, True), (ints([290, 0]), 33, False)):
+        one, two = (ra.ra_gather_paged(c.gpu, values=values, first=first, rows=rows, stream=s) for s in (None, here))
+        three = ra.ra_gather_paged(c.gpu, values, first, rows, out=torch.empty_like(one))
+        assert torch.equal(torch.nan_to_num(one), torch.nan_to_num(two)) and torch.equal(torch.nan_to_num(one), torch.nan_to_num(three))
     for parts in ((0, 1, 2), (0,), (1,), (2, 1)):
         for n_new in (None, ints([2, 3])):
             got = []
