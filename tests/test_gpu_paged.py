@@ -215,7 +215,8 @@ ATTEND = [  # n_q, n_kv, page, lens, indexed (None: not given), sink, window, to
     (5, 1, 16, [1500], None, 0, 0, 200, 0), (16, 2, 32, [260, 264, 5, 31], [200, 264, 0, 31], 1, 31, 64, 0), (20, 1, 16, [4000], None, 128, 1400, 300, 0),
     (16, 1, 16, [9001], [1001], 4, 640, 100, 0), (8, 2, 4, [3001, 2000], [900, 2000], 4, 500, 40, 0.3), (17, 1, 1, [700, 600], [500, 600], 5, 20, 33, 0.3),
     (32, 8, 64, [2000, 1500], None, 4, 640, 100, 0.2), (16, 2, 16, [900] * 9, [800] * 9, 3, 20, 50, 0), (2, 1, 16, [2000] * 40, [1500] * 40, 3, 20, 300, 0),
-    (1, 1, 16, [1], None, 0, 0, 1, 0), (1, 1, 16, [3000], None, 0, 1, 2048, 0),
+    (1, 1, 16, [1], None, 0, 0, 1, 0), (1, 1, 16, [3000], None, 0, 1, 2048, 0), (2, 1, 16, list(range(130)), [n // 2 for n in range(130)], 1, 9, 20, 0),
+    (40, 1, 8, [500] * 70, None, 4, 64, 33, 0.1), (16, 8, 64, [700, 3] * 20, [600, 1] * 20, 4, 64, 100, 0),
 ]
 
 
@@ -245,6 +246,33 @@ def test_sparse_and_static_attention(case, dtype):
                 check(o[s, h], l[s, h], to_np(q[s, h]), *c.rows(s, g, rows.tolist()))
     again = ra.ra_attend_paged(*args, **kw)
     assert np.array_equal(again[0].cpu().numpy(), got[0]) and np.array_equal(again[1].cpu().numpy(), got[1])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n_seq", [1, 130])
+def test_rows_that_are_no_numbers_are_their_heads_alone(dtype, n_seq):
+    """A retrieved row with a NaN key or an infinite or NaN value makes NaN of the heads that retrieved it and of their retrieved set, whether
+    the job is one workgroup's or several; the others are what they were."""
+    c = Cache([900] * n_seq, 2, 16, dtype, seed=17)
+    q = queries(n_seq, 8, dtype, 17).to(DEV)
+    n, g = ints([900] * n_seq), torch.Generator(device=DEV).manual_seed(4)
+    ids = torch.randint(10, 400, (n_seq, 8, 40), dtype=torch.int32, device=DEV, generator=g)
+    ids[:, 2, 7], ids[:, 5, 39] = 500, 600
+    ref = ra.ra_attend_paged(q, c.gpu, 4, 100, ids, n, partials=True)
+    for s in range(n_seq):
+        p, slot = int(c.table[s][500 // 16]), 500 % 16
+        c.V[p, 0, slot, 3] = float("nan")
+        p, slot = int(c.table[s][600 // 16]), 600 % 16
+        c.K[p, 1, slot, 100] = float("nan")
+        c.V[p, 1, slot] = float("inf")
+    got = ra.ra_attend_paged(q, c.gpu, 4, 100, ids, n, partials=True)
+    others = [h for h in range(8) if h not in (2, 5)]
+    for i, (a, b) in enumerate(zip(got, ref)):
+        assert torch.equal(a[:, others], b[:, others])
+        if i >= 4:                                          # (the static set's)
+            assert torch.equal(a, b)
+    assert torch.isnan(got[0][:, 2, 3]).all() and torch.isfinite(got[0][:, 2, 4:]).all() and torch.isnan(got[2][:, 2, 3]).all()
+    assert torch.isnan(got[0][:, 5]).all() and torch.isnan(got[1][:, 5]).all() and torch.isnan(got[3][:, 5]).all()
 
 
 def test_attention_without_lengths_and_over_fewer_rows():

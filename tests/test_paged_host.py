@@ -75,6 +75,10 @@ def test_caches_that_are_refused(name, cache, status, needle):
     ("ra_attend_paged", dict(topk=0), {}, 1, "topk"), ("ra_attend_paged", dict(topk=2049), {}, 6, "RA_MAX_TOPK"),
     ("ra_attend_paged", dict(q=_p(0x10008)), {}, 1, "aligned"), ("ra_attend_paged", dict(ws=_p(0x10008)), {}, 1, "aligned"),
     ("ra_attend_paged", dict(ws_bytes=8, window=100), {}, 2, "workspace"), ("ra_attend_paged", dict(n_q=1 << 28, ws_bytes=1 << 62), {}, 6, "too many heads"),
+    ("ra_attend_paged", dict(ws_bytes=1 << 62), dict(n_seq=65536), 6, "too many heads"),
+    ("ra_attend_paged", dict(n_q=65536, ws_bytes=1 << 62), dict(n_kv_heads=65536), 6, "too many heads"),
+    ("ra_attend_paged", dict(n_q=2048, ws_bytes=1 << 62), dict(n_seq=2048, n_kv_heads=2048), 6, "too many heads"),
+    ("ra_full_attention_paged", dict(n_q=4, N=100), dict(n_seq=1 << 22, n_kv_heads=2, n_pages=1), 6, "too many heads"),
 ])
 def test_calls_that_are_refused(name, change, cache, status, needle):
     _refused(name, change, cache, status, needle)
