@@ -379,7 +379,7 @@ typedef struct {                    /* host memory, read before the call returns
  * frequencies are the caller's, in inv_freq). k_in and v_in may be NULL: nothing of K or V is written. Limits as for ra_append_tokens. */
 ra_status ra_append_tokens_paged(const void* q_in, const void* k_in, const void* v_in, const ra_paged_cache* cache, int n_q_heads,
                                  int64_t T, int d, int64_t q_row, int64_t k_row, int64_t v_row, const void* q_weight, const void* k_weight,
-                                 double eps, const float* inv_freq, int rot_dim, int interleaved, float rot_scale,
+                                 double eps, const float* inv_freq, int rot_dim, int interleaved, double rot_scale,
                                  const int32_t* first, const int32_t* n_new, void* stream, void* q_out);
 
 /* Rows first[s] + t, t < T, of K (values 0) or V (1) -> X [n_seq][n_kv_heads][T][128], side by side as ra_knn, ra_build_index,
@@ -402,7 +402,7 @@ ra_status ra_full_attention_paged(const void* q, const ra_paged_cache* cache, in
  * their combination by Eq. 4-5 into out/lse, and the four partial outputs, each of which may be NULL. Lengths are each sequence's own:
  * with n = min(n_tokens[s], N) and n_i = min(n_indexed[s], n) (device int32; NULL: N, and n) W = [0, sink) u [min(n - window, n_i), n):
  * tokens behind the n_i that the index was built over are static. Entries of ids that are not in [0, n), or are members of W (they are
- * attended there), are skipped; one that is given twice counts twice. Rows without a page are not attended. Weights have 24 bits.
+ * attended there), are skipped; one that is given twice counts twice. Rows without a page are not attended. Weights and infinite values as above.
  * RA_EUNSUP past 65535 sequences, 65535 tiles of up to 16 query heads of a KV head, or 2^22 - 1 of both.
  * workspace: as above, of ra_attend_paged_workspace_bytes(...) bytes. */
 size_t ra_attend_paged_workspace_bytes(ra_dtype dt, int n_seq, int n_q_heads, int n_kv_heads, int64_t N, int sink, int window, int topk);

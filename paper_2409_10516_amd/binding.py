@@ -134,7 +134,7 @@ def lib() -> C.CDLL:
     L.ra_attend_q4.argtypes = [vp, vp, i32, vp, vp, vp, vp, i64, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]
     L.ra_attend_q4.restype = i32
     cache = C.POINTER(_PagedCache)
-    L.ra_append_tokens_paged.argtypes = [vp, vp, vp, cache, i32, i64, i32, i64, i64, i64, vp, vp, C.c_double, vp, i32, i32, C.c_float, vp, vp, vp, vp]
+    L.ra_append_tokens_paged.argtypes = [vp, vp, vp, cache, i32, i64, i32, i64, i64, i64, vp, vp, C.c_double, vp, i32, i32, C.c_double, vp, vp, vp, vp]
     L.ra_append_tokens_paged.restype = i32
     L.ra_gather_paged.argtypes = [cache, i32, i64, i32, vp, vp, vp]
     L.ra_gather_paged.restype = i32

@@ -966,7 +966,7 @@ static ra_status check_paged(const ra_paged_cache* c, int need, PgCache* out) {
 
 extern "C" ra_status ra_append_tokens_paged(const void* q_in, const void* k_in, const void* v_in, const ra_paged_cache* cache, int n_q, int64_t T,
                                             int d, int64_t q_row, int64_t k_row, int64_t v_row, const void* q_weight, const void* k_weight,
-                                            double eps, const float* inv_freq, int rot_dim, int interleaved, float rot_scale,
+                                            double eps, const float* inv_freq, int rot_dim, int interleaved, double rot_scale,
                                             const int32_t* first, const int32_t* n_new, void* stream, void* q_out) {
     PgCache c;
     RA_TRY(check_paged(cache, (k_in ? 1 : 0) | (v_in ? 2 : 0), &c));

@@ -257,7 +257,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
         ra_status rc;
         Py_BEGIN_ALLOW_THREADS
         rc = append_call(t[0].at, t[1].at, t[2].at, &c->c, (int)(t[0].at ? t[0].heads : n_kv), T, 128, t[0].row, t[1].row, t[2].row, qw, kw,
-                         PyFloat_AS_DOUBLE(a[8]), (const float*)freq, (int)rot, a[10] == Py_True, (float)PyFloat_AS_DOUBLE(a[11]),
+                         PyFloat_AS_DOUBLE(a[8]), (const float*)freq, (int)rot, a[10] == Py_True, PyFloat_AS_DOUBLE(a[11]),
                          (const int32_t*)first, (const int32_t*)n_new, st, out);
         Py_END_ALLOW_THREADS
         if (rc != RA_OK) return PyLong_FromLong(rc);

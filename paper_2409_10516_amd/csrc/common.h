@@ -192,7 +192,7 @@ struct AppendArgs {
 };
 ra_status ra_launch_append(const AppendArgs& a, ra_dtype dt, hipStream_t st);
 // the same with K and V in the pages of `pages` (of `a`, out[1] and out[2] only say whether there are any); cosines and sines times rot_scale
-ra_status ra_launch_append_paged(const AppendArgs& a, const PgCache& pages, float rot_scale, ra_dtype dt, hipStream_t st);
+ra_status ra_launch_append_paged(const AppendArgs& a, const PgCache& pages, double rot_scale, ra_dtype dt, hipStream_t st);
 ra_status ra_launch_gather_paged(const PgCache& c, const void* pages, ra_dtype dt, int n_seq, int n_kv, int64_t T, const int32_t* first,
                                  hipStream_t st, void* X);
 size_t ra_full_paged_partial_floats(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N);

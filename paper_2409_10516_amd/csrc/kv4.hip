@@ -87,9 +87,9 @@ __device__ __forceinline__ double rsqrt64(double x) {
     return y > 0. && y < INFINITY ? z : y;               // (zero and infinity are their own)
 }
 
-// The sine and cosine of x, to float32: x less the nearest multiple of pi / 2, in two parts, and the series of both about zero,
+// The sine and cosine of x times `scale`, rounded once to float32: x less the nearest multiple of pi / 2, in two parts, and the series of both about zero,
 // to terms below 2^-44 of the result at pi / 4.
-__device__ __forceinline__ float2 cos_sin64(double x) {
+__device__ __forceinline__ float2 cos_sin64(double x, double scale) {
     const double n = rint(x * 0.63661977236758134308);
     const double r = fma(-n, 6.123233995736766036e-17, fma(-n, 1.57079632679489655800, x)), t = r * r;
     double s = fma(t, 1. / 6227020800., -1. / 39916800.), c = fma(t, -1. / 87178291200., 1. / 479001600.);
@@ -100,7 +100,7 @@ __device__ __forceinline__ float2 cos_sin64(double x) {
     s = fma(t * r, s, r); c = fma(t, c, -0.5);
     c = fma(t, c, 1.);
     const int k = (int)((long long)n & 3);               // quarter turns
-    const float fs = (float)(k & 1 ? c : s), fc = (float)(k & 1 ? s : c);
+    const float fs = (float)((k & 1 ? c : s) * scale), fc = (float)((k & 1 ? s : c) * scale);
     return make_float2(k == 1 || k == 2 ? -fc : fc, k & 2 ? -fs : fs);
 }
 
@@ -133,7 +133,7 @@ __device__ __forceinline__ void turn(float (&v)[VALS], const float2 (&cs)[VALS],
 // PAGED: a token's K and V rows of all KV heads lie in one page, a page's rows from head to head; its entry of the table is asked for ahead of the
 // angles. It costs nothing that shows: the 32K prompt into pages of 64 rows 142 to 150 us, without pages 145, a decoded token 3.0.
 template <int DT, int THREADS, bool ONCE, bool PAGED>
-__global__ __launch_bounds__(THREADS, 8) void append_kernel(AppendArgs a, int split, PgCache pages, float rot_scale) {
+__global__ __launch_bounds__(THREADS, 8) void append_kernel(AppendArgs a, int split, PgCache pages, double rot_scale) {
     __shared__ float2 s_cs[RA_D / 2];
     __shared__ float4 s_w[2][RA_D / 4];
     constexpr int VALS = KV_VALS<DT>, LANES = KV_LANES<DT>, GROUPS = THREADS / LANES;
@@ -158,11 +158,7 @@ __global__ __launch_bounds__(THREADS, 8) void append_kernel(AppendArgs a, int sp
         row0 = ((size_t)page * a.n_kv << pages.page_log2) + (pos & (a.stride[0] - 1));
     }
     char *out_k = at(a.out[1], row0 * RA_D), *out_v = at(a.out[2], row0 * RA_D);
-    if (tid < half) {
-        float2 cs = cos_sin64((double)pos * (double)a.inv_freq[tid]);
-        if constexpr (PAGED) cs = make_float2(cs.x * rot_scale, cs.y * rot_scale);
-        s_cs[tid] = cs;
-    }
+    if (tid < half) s_cs[tid] = cos_sin64((double)pos * (double)a.inv_freq[tid], PAGED ? rot_scale : 1.);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
         if (a.weight[i])                                           // (the last wavefronts first: the angles are the first one's)
@@ -237,7 +233,7 @@ __global__ __launch_bounds__(THREADS, 8) void append_kernel(AppendArgs a, int sp
 }
 
 template <bool PAGED>
-static ra_status launch_append(const AppendArgs& a, const PgCache& pages, float rot_scale, ra_dtype dt, hipStream_t st) {
+static ra_status launch_append(const AppendArgs& a, const PgCache& pages, double rot_scale, ra_dtype dt, hipStream_t st) {
     const int64_t tokens = a.T * a.n_seq;
     if (tokens > (1 << 24) - 1) RA_FAIL(RA_EUNSUP, "more than 2^24 - 1 tokens in a call");
     if ((int64_t)a.n_q + 2 * (int64_t)a.n_kv > (1 << 24) - 1) RA_FAIL(RA_EUNSUP, "too many heads for one launch");
@@ -270,8 +266,8 @@ static ra_status launch_append(const AppendArgs& a, const PgCache& pages, float 
     RA_HIP(hipGetLastError());
     return RA_OK;
 }
-ra_status ra_launch_append(const AppendArgs& a, ra_dtype dt, hipStream_t st) { return launch_append<false>(a, PgCache{}, 1.f, dt, st); }
-ra_status ra_launch_append_paged(const AppendArgs& a, const PgCache& pages, float rot_scale, ra_dtype dt, hipStream_t st) {
+ra_status ra_launch_append(const AppendArgs& a, ra_dtype dt, hipStream_t st) { return launch_append<false>(a, PgCache{}, 1., dt, st); }
+ra_status ra_launch_append_paged(const AppendArgs& a, const PgCache& pages, double rot_scale, ra_dtype dt, hipStream_t st) {
     return launch_append<true>(a, pages, rot_scale, dt, st);
 }
 

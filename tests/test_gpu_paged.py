@@ -349,8 +349,8 @@ def test_append(dtype, n_q, n_kv, T, page, rot, inter, norm, scale):
         for rows, weight, is_q in ((q, w[0], True), (k, w[1], False)):
             ref, size = OK.head_rows(to_np(rows[s, :n].cpu()), pos, **(opt | dict(weight=None if weight is None else to_np(weight.cpu()))))
             if rot:
-                ref[..., :rot] *= np.float32(scale)
-                size[..., :rot] *= abs(np.float32(scale))
+                ref[..., :rot] *= scale
+                size[..., :rot] *= abs(scale)
             if is_q:
                 _row_close(gotQ[s, :, :n].transpose(1, 0, 2), ref, size, dtype)
             else:
