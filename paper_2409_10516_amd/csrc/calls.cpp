@@ -35,20 +35,29 @@ int current_device() { return c10::impl::getDeviceGuardImpl(c10::DeviceType::CUD
 
 void drop(PyObject* capsule) { delete static_cast<Cache*>(PyCapsule_GetPointer(capsule, "paged")); }
 
-// what is asked of a call's cache: tensors that are where they were, on the current device
+// what is asked of a call's cache: tensors that are where they were, on the current device. (Tensors that share their memory until they are written to
+// get their own here, as they do where Python asks for an address, and are somewhere else then.)
 const Cache* cache_of(PyObject* o) {
     const Cache* c = static_cast<const Cache*>(PyCapsule_GetPointer(o, "paged"));
     if (!c || current_device() != c->device) return nullptr;
     for (int i = 0; i < 3; ++i)
-        if (c->t[i].defined() && c->t[i].const_data_ptr() != c->at[i]) return nullptr;
+        if (c->t[i].defined() && c->t[i].mutable_data_ptr() != c->at[i]) return nullptr;
     return c;
+}
+bool is(const Cache& c, const at::Tensor& t, at::ScalarType type, at::IntArrayRef shape) {
+    return t.is_cuda() && t.device().index() == c.device && t.scalar_type() == type && t.sizes() == shape && t.is_contiguous();
 }
 // the address of a contiguous tensor of a type and shape on the cache's device, null if it is not one
 const void* data(const Cache& c, PyObject* o, at::ScalarType type, at::IntArrayRef shape) {
     if (!THPVariable_Check(o)) return nullptr;
     const at::Tensor& t = THPVariable_Unpack(o);
-    if (!t.is_cuda() || t.device().index() != c.device || t.scalar_type() != type || t.sizes() != shape || !t.is_contiguous()) return nullptr;
-    return t.const_data_ptr();
+    return is(c, t, type, shape) ? t.const_data_ptr() : nullptr;
+}
+// the same of one that is written to, whose memory is its own then
+void* place(const Cache& c, PyObject* o, at::ScalarType type, at::IntArrayRef shape) {
+    if (!THPVariable_Check(o)) return nullptr;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    return is(c, t, type, shape) ? t.mutable_data_ptr() : nullptr;
 }
 // the same, where None will do: false if it is neither
 bool maybe(const Cache& c, PyObject* o, at::ScalarType type, at::IntArrayRef shape, const void** at) {
@@ -106,7 +115,7 @@ struct Results {
         for (int i = 0; i < 2; ++i) {
             const at::IntArrayRef s(shape, 3 - i);
             if (given[i] == Py_None) made[i] = make(c, s, at::kFloat);
-            at[i] = given[i] == Py_None ? made[i].data_ptr<float>() : static_cast<float*>(const_cast<void*>(data(c, given[i], at::kFloat, s)));
+            at[i] = given[i] == Py_None ? made[i].data_ptr<float>() : static_cast<float*>(place(c, given[i], at::kFloat, s));
             if (!at[i]) return false;
         }
         return true;
@@ -247,7 +256,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
                 made = make(*c, {n_seq, t[0].heads, T, 128}, c->type);
                 if (n_new) made.zero_();
                 out = made.mutable_data_ptr();
-            } else if (!(out = const_cast<void*>(data(*c, a[12], c->type, {n_seq, t[0].heads, T, 128})))) {
+            } else if (!(out = place(*c, a[12], c->type, {n_seq, t[0].heads, T, 128}))) {
                 return nullptr;
             }
         } else if (a[12] != Py_None) {
@@ -272,7 +281,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* gather(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return careful([&]() -> PyObject* {
         const Cache* c = n == 5 ? cache_of(a[0]) : nullptr;
-        const void *first, *out;
+        const void* first;
         int64_t rows = 0;
         if (!c || !PyBool_Check(a[1]) || !maybe(*c, a[2], at::kInt, {c->c.n_seq}, &first)) return nullptr;
         if (a[3] == Py_None) rows = (int64_t)c->c.table_pages * c->c.page;
@@ -280,13 +289,13 @@ PyObject* gather(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (rows < 0) return nullptr;
         const int64_t shape[4] = {c->c.n_seq, c->c.n_kv_heads, rows, 128};
         at::Tensor made;
-        void* st;
-        if (a[4] == Py_None) out = (made = make(*c, shape, c->type)).const_data_ptr();
-        else out = data(*c, a[4], c->type, shape);
+        void *out, *st;
+        if (a[4] == Py_None) out = (made = make(*c, shape, c->type)).mutable_data_ptr();
+        else out = place(*c, a[4], c->type, shape);
         if (!out || !stream_of(*c, &st)) return nullptr;
         ra_status rc;
         Py_BEGIN_ALLOW_THREADS
-        rc = gather_call(&c->c, a[1] == Py_True, rows, 128, (const int32_t*)first, st, const_cast<void*>(out));
+        rc = gather_call(&c->c, a[1] == Py_True, rows, 128, (const int32_t*)first, st, out);
         Py_END_ALLOW_THREADS
         if (rc != RA_OK) return PyLong_FromLong(rc);
         PyObject* o = made.defined() ? THPVariable_Wrap(made) : Py_NewRef(a[4]);
@@ -302,7 +311,7 @@ PyObject* cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Cache* c = new Cache;
     for (int i = 0; i < 3; ++i) {
         if (THPVariable_Check(a[i])) c->t[i] = THPVariable_Unpack(a[i]);
-        c->at[i] = c->t[i].defined() ? c->t[i].const_data_ptr() : nullptr;
+        c->at[i] = c->t[i].defined() ? c->t[i].mutable_data_ptr() : nullptr;
     }
     if (const void* from = PyLong_AsVoidPtr(a[3])) c->c = *static_cast<const ra_paged_cache*>(from);
     c->device = (int)PyLong_AsLong(a[4]);
