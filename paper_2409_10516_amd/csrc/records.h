@@ -151,9 +151,10 @@ __device__ __forceinline__ RecSum rec_add_up(const float* rec, int first, int la
         x.l *= corr;
 #pragma unroll
         for (int u = 0; u < FLY; ++u) {
-            const float w = i0 + u * by < last ? __builtin_amdgcn_exp2f(m[u] - mx) : 0.f;
-            x.a = fmaf(a[u], w, x.a);
-            x.l = fmaf(l[u], w, x.l);
+            const bool is = i0 + u * by < last;             // (a trip that is not full reads its first record again, whose sum may be infinite)
+            const float w = __builtin_amdgcn_exp2f(m[u] - mx);
+            x.a = fmaf(is ? a[u] : 0.f, w, x.a);
+            x.l = fmaf(is ? l[u] : 0.f, w, x.l);
         }
         x.m = mx;
     }

@@ -1,0 +1,73 @@
+"""Attention over a cache in pages where values are infinite under finite keys: an infinity, NaN where both meet, and nothing else changes."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2409_10516_amd as ra
+from oracle import attention as OA, paged as OP
+from tests.test_gpu_paged import DEV, Cache, check, ints, queries
+from tests.util import to_np
+
+pytestmark = pytest.mark.gpu
+
+
+def _again(c):
+    """The oracle's copy of pools that have been written to."""
+    c.np = [to_np(x.cpu()).astype(np.float64) for x in (c.K, c.V)]
+
+
+def _check(out, lse, q, K, V):
+    """The infinities of a dimension decide it (a weight below 2^-126 of the largest would be zero, and zero times infinity is not a number: there is none
+    here); the others, and lse, are what they are without."""
+    z = K @ q
+    assert ((z - z.max()) / np.sqrt(128) > -80.).all()
+    up, down, rest = (V == np.inf).any(axis=0), (V == -np.inf).any(axis=0), np.where(np.isinf(V), 0.0, V)
+    assert np.isnan(out[up & down]).all() and (out[up & ~down] == np.inf).all() and (out[down & ~up] == -np.inf).all()
+    check(np.where(up | down, OA.full_attention(q, K, rest)[0], out), lse, q, K, rest)
+
+
+def _put(c, s, kv, rows, dims):
+    for i, (r, d) in enumerate(zip(rows, dims)):
+        c.V[int(c.table[s][r // c.page]), kv, r % c.page, d] = float("inf") if i % 2 else -float("inf")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32])
+@pytest.mark.parametrize("page", [4, 16, 64])
+@pytest.mark.parametrize("n,n_q", [(1, 2), (16, 2), (300, 2), (300, 17), (5003, 2)])
+def test_full_attention(dtype, page, n, n_q):
+    """One workgroup's rows, and many a head's."""
+    c = Cache([n, n // 2], 1, page, dtype, seed=n)
+    rng = np.random.default_rng(n)
+    for s in range(2):
+        rows = rng.permutation(c.lens[s])[:40]
+        _put(c, s, 0, rows, range(len(rows)))
+        _put(c, s, 0, rows[:2], (127, 127))                  # (both)
+    _again(c)
+    q = queries(2, n_q, dtype, n)
+    out, lse = (t.cpu().numpy() for t in ra.ra_full_attention_paged(q.to(DEV), c.gpu, ints(c.lens)))
+    for s in range(2):
+        for h in range(n_q):
+            _check(out[s, h], lse[s, h], to_np(q[s, h]), *c.rows(s, 0, range(c.lens[s]))) if c.lens[s] else None
+
+
+@pytest.mark.parametrize("dtype", [torch.float32])
+@pytest.mark.parametrize("n_seq,window", [(1, 40), (1, 100), (1, 700), (20, 300), (130, 100), (130, 700)])
+def test_sparse_and_static_attention(dtype, n_seq, window):
+    """In either set, whether a job is one workgroup's or several whose records fill the trips of what combines them, or do not."""
+    n = 900
+    c = Cache([n] * n_seq, 2, 16, dtype, seed=17)
+    q, rng = queries(n_seq, 8, dtype, 17), np.random.default_rng(window)
+    ids = np.stack([rng.permutation(np.arange(4, n - window))[:40] for _ in range(n_seq * 8)]).reshape(n_seq, 8, 40).astype(np.int32)
+    near = np.r_[0:4, n - window:n]
+    for s in range(n_seq):
+        rows = rng.permutation(near)[:40]
+        _put(c, s, 0, rows, range(len(rows)))
+        for h in (5, 6):                                     # (a row of one head's may be another's too)
+            _put(c, s, 1, ids[s, h, ::2], range(60, 80))
+    _again(c)
+    got = [t.cpu().numpy() for t in ra.ra_attend_paged(q.to(DEV), c.gpu, 4, window, torch.from_numpy(ids).to(DEV), ints([n] * n_seq), partials=True)]
+    for s in sorted({0, n_seq // 2, n_seq - 1}):
+        for h in range(8):
+            W, om = OP.sets(n, n, 4, window, ids[s, h].tolist())
+            for (o, l), rows in zip((got[0:2], got[2:4], got[4:6]), (np.concatenate([W, om]), om, W)):
+                _check(o[s, h], l[s, h], to_np(q[s, h]), *c.rows(s, h // 4, rows.tolist()))
