@@ -209,9 +209,9 @@ ra_status ra_launch_dequantize_kv4(const uint8_t* codes, const uint8_t* scale, r
 size_t ra_full_q4_partial_floats(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N);
 ra_status ra_launch_full_q4(const void* q, ra_dtype dt, const Q4Cache& c, int n_seq, int n_q, int n_kv, int64_t N,
                             const int32_t* n_tokens, float* partials, hipStream_t st, float* out, float* lse);
-// combines the records that a list of rows left (records.h), those of tiles of `heads` query heads; N rows at most per sequence
+// combines the records that a list of rows left (records.h), those of tiles of `heads` query heads; N rows at most per sequence; `unit`: of their maxima
 ra_status ra_launch_full_merge(const float* partials, int n_seq, int n_q, int n_kv, int64_t N, const int32_t* n_tokens, int tiles, int unit_log2,
-                               int heads, int workgroups, hipStream_t st, float* out, float* lse);
+                               int heads, int workgroups, float unit, hipStream_t st, float* out, float* lse);
 size_t ra_attend_q4_partial_floats(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N, int64_t Ng, int sink, int window, int topk);
 ra_status ra_launch_attend_q4(const void* q, ra_dtype dt, const Q4Cache& c, int n_seq, int n_q, int n_kv, int64_t N, int64_t Ng,
                               int sink, int window, int topk, const int32_t* ids, float* partials, uint32_t* tickets,

@@ -2,9 +2,11 @@
 // the static set W of Sec. 3.3 with their combination by Eq. 4-5 (ra_attend_paged), and rows side by side again (ra_gather_paged).
 // What puts tokens into pages is with the other calls that append (kv4.hip).
 //
-// Rows are cut into parts; a workgroup turns one part into a record (128 weighted sums, the maximum of z log2(e), the sum of weights), and a
+// Rows are cut into parts; a workgroup turns one part into a record (128 weighted sums, the maximum of <q, k>, the sum of weights), and a
 // head's records are combined by a second kernel. Weights are powers of two, p = 2^(c (<q, k> - m)) with c = log2(e) / sqrt(d) and m the running
-// maximum of <q, k>: the difference first, so that its rounding goes by the difference and equal logits have equal weights however large they are.
+// maximum of <q, k>: the difference first, here and where records and sets are combined, so that its rounding goes by the difference and equal
+// logits have equal weights however large they are and wherever their rows were. (A maximum may lag behind its rows' by PG_LAG. With
+// records' maxima multiplied by c first, means over 131072 rows whose products are 2^24 were off by up to 1.8 %.)
 #include "common.h"
 #include "records.h"
 
@@ -208,7 +210,6 @@ __device__ __forceinline__ void pg_together(const PgLds<WAVES>& lds, int of_w, i
             x[i].a = fmaf(is ? a[w] : 0.f, wt, x[i].a);
             x[i].l = fmaf(is ? l[w] : 0.f, wt, x[i].l);
         }
-        x[i].m *= PG_C;
     }
 }
 
@@ -370,7 +371,7 @@ __global__ __launch_bounds__(PG_WAVES * RA_WAVE, DT == RA_BF16 ? 4 : 2) void pg_
                 if (d == 0) reinterpret_cast<float2*>(partials + PG_HEADS * places * RA_D)[hd * places + place] = make_float2(all.m, all.l);
             } else {
                 out[(head0 + hd) * RA_D + d] = all.m > -INFINITY ? all.a / all.l : 0.f;
-                if (d == 0) lse[head0 + hd] = all.m > -INFINITY ? all.m * REC_LN2 + logf(all.l) : -INFINITY;
+                if (d == 0) lse[head0 + hd] = all.m > -INFINITY ? all.m * PG_C * REC_LN2 + logf(all.l) : -INFINITY;
             }
         }
         if (whole) return;
@@ -406,13 +407,13 @@ __global__ __launch_bounds__(RA_D * PG_MERGE_SLICES) void pg_full_merge_kernel(c
 #pragma unroll
         for (int u = 0; u < FLY; ++u) mx = fmaxf(mx, m[u]);
         if (mx == -INFINITY) continue;
-        const float corr = __builtin_amdgcn_exp2f(x.m - mx);
+        const float corr = __builtin_amdgcn_exp2f((x.m - mx) * PG_C);
         x.a *= corr;
         x.l *= corr;
 #pragma unroll
         for (int u = 0; u < FLY; ++u) {
             const bool is = m[u] > -INFINITY;
-            const float w = __builtin_amdgcn_exp2f(m[u] - mx);
+            const float w = __builtin_amdgcn_exp2f((m[u] - mx) * PG_C);
             x.a = fmaf(is ? a[u] : 0.f, w, x.a);
             x.l = fmaf(is ? l[u] : 0.f, w, x.l);
         }
@@ -427,12 +428,12 @@ __global__ __launch_bounds__(RA_D * PG_MERGE_SLICES) void pg_full_merge_kernel(c
     const float base = x.m > -INFINITY ? x.m : 0.f;
 #pragma unroll
     for (int i = 0; i < SLICES; ++i) {
-        const float w = __builtin_amdgcn_exp2f(s_part[i][d].m - base);
+        const float w = __builtin_amdgcn_exp2f((s_part[i][d].m - base) * PG_C);
         x.a = fmaf(s_part[i][d].a, w, x.a);
         x.l = fmaf(s_part[i][d].l, w, x.l);
     }
     out[head * RA_D + d] = x.m > -INFINITY ? x.a / x.l : 0.f;
-    if (d == 0) lse[head] = x.m > -INFINITY ? x.m * REC_LN2 + logf(x.l) : -INFINITY;
+    if (d == 0) lse[head] = x.m > -INFINITY ? x.m * PG_C * REC_LN2 + logf(x.l) : -INFINITY;
 }
 
 // How a call is cut. Each job is one workgroup's, and there is no second launch, where its rows are few or the jobs many enough to fill the part: by
@@ -487,7 +488,7 @@ ra_status ra_launch_full_paged(const void* q, ra_dtype dt, const PgCache& c, int
     // records per head, were all sequences as long as the longest
     const int records = x.workgroups / (n_seq * n_kv * x.tiles);
     if (records <= PG_MERGE_FEW || records > 8 * PG_MERGE_SLICES)
-        return ra_launch_full_merge(partials, n_seq, n_q, n_kv, N, n_tokens, x.tiles, x.unit_log2, PG_HEADS, x.workgroups, st, out, lse);
+        return ra_launch_full_merge(partials, n_seq, n_q, n_kv, N, n_tokens, x.tiles, x.unit_log2, PG_HEADS, x.workgroups, PG_C, st, out, lse);
     hipLaunchKernelGGL(pg_full_merge_kernel, dim3(n_seq * n_q), dim3(RA_D * PG_MERGE_SLICES), 0, st, partials, n_seq, n_q, n_kv, (int)N, n_tokens,
                        x.tiles, x.unit_log2, x.workgroups, out, lse);
     RA_HIP(hipGetLastError());
@@ -605,7 +606,7 @@ __global__ __launch_bounds__(WAVES * RA_WAVE, DT == RA_BF16 ? 4 : 2) void pg_att
         RecSum both[2];
         pg_together(lds, of_w, hd, d, both);
         if (parts == 1) {
-            rec_write(both, head0 + hd, d, o);
+            rec_write(both, head0 + hd, d, PG_C, o);
             continue;
         }
 #pragma unroll
@@ -623,7 +624,7 @@ __global__ __launch_bounds__(2 * RA_D * SLICES) void pg_merge_kernel(const float
     __shared__ RecSum s_part[SLICES][2][RA_D];
     const size_t head = blockIdx.x;
     const int d = threadIdx.x % RA_D, i = threadIdx.x / RA_D % 2, slice = threadIdx.x / (2 * RA_D);
-    s_part[slice][i][d] = rec_add_up<false>(partials + (head * 2 + i) * parts * REC_FLOATS, slice, parts, SLICES, d);
+    s_part[slice][i][d] = rec_add_up<false>(partials + (head * 2 + i) * parts * REC_FLOATS, slice, parts, SLICES, d, PG_C);
     __syncthreads();
     if (threadIdx.x >= RA_D) return;
     RecSum set[2];
@@ -635,13 +636,13 @@ __global__ __launch_bounds__(2 * RA_D * SLICES) void pg_merge_kernel(const float
         const float base = x.m > -INFINITY ? x.m : 0.f;
 #pragma unroll
         for (int y = 0; y < SLICES; ++y) {
-            const float w = __builtin_amdgcn_exp2f(s_part[y][k][d].m - base);
+            const float w = __builtin_amdgcn_exp2f((s_part[y][k][d].m - base) * PG_C);
             x.a = fmaf(s_part[y][k][d].a, w, x.a);
             x.l = fmaf(s_part[y][k][d].l, w, x.l);
         }
         set[k] = x;
     }
-    rec_write(set, head, d, o);
+    rec_write(set, head, d, PG_C, o);
 }
 
 // How a job is cut: half a round of chunks for a workgroup's wavefronts each, up to so many workgroups that each has a compute unit to itself

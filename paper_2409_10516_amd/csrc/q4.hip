@@ -396,7 +396,7 @@ __global__ __launch_bounds__(Q4_THREADS, DT == RA_BF16 ? 3 : 2) void q4_full_ker
 template <int THREADS, int DIMS>
 __global__ __launch_bounds__(THREADS) void q4_full_merge_kernel(const float* __restrict__ partials, int n_seq, int n_q, int n_kv,
                                                                          int N, const int32_t* __restrict__ n_tokens, int tiles,
-                                                                         int unit_log2, int heads, int grid, float* __restrict__ out,
+                                                                         int unit_log2, int heads, int grid, float unit, float* __restrict__ out,
                                                                          float* __restrict__ lse) {
     constexpr int WAVES = THREADS / RA_WAVE, SL = THREADS / DIMS, FLY = DIMS == RA_D ? 16 : 32;
     constexpr int MOST = DIMS == RA_D ? ROW_MOST_WORKGROUPS : ROW_MOST_WORKGROUPS / 3 * 2;       // records of a head
@@ -424,7 +424,7 @@ __global__ __launch_bounds__(THREADS) void q4_full_merge_kernel(const float* __r
         const float base = mx > -INFINITY ? mx : 0.f;
 #pragma unroll
         for (int u = 0; u < Q4_MERGE_FEW; ++u) {
-            const float w = __builtin_amdgcn_exp2f(m[u] - base);
+            const float w = __builtin_amdgcn_exp2f((m[u] - base) * unit);
             a = fmaf(r[u], w, a);
             ll = fmaf(l[u], w, ll);
         }
@@ -448,7 +448,7 @@ __global__ __launch_bounds__(THREADS) void q4_full_merge_kernel(const float* __r
         for (int w = 0; w < WAVES; ++w) mx = fmaxf(mx, s_m[w]);
 #pragma unroll
         for (int i = 0; i < MINE; ++i) {
-            const float w = mx > -INFINITY ? __builtin_amdgcn_exp2f(m[i] - mx) : 0.f;
+            const float w = mx > -INFINITY ? __builtin_amdgcn_exp2f((m[i] - mx) * unit) : 0.f;
             s_w[tid + i * THREADS] = w;
             ll = fmaf(l[i], w, ll);
         }
@@ -475,7 +475,7 @@ __global__ __launch_bounds__(THREADS) void q4_full_merge_kernel(const float* __r
         for (int i = 1; i < SL; ++i) a += s_a[i][t];
     }
     out[head * RA_D + dim] = mx > -INFINITY ? a / ll : 0.f;
-    if (dim == 0) lse[head] = mx > -INFINITY ? mx * REC_LN2 + logf(ll) : -INFINITY;
+    if (dim == 0) lse[head] = mx > -INFINITY ? mx * unit * REC_LN2 + logf(ll) : -INFINITY;
 }
 
 // ---- the retrieved set and the static set -------------------------------------------------------
@@ -590,7 +590,7 @@ __global__ __launch_bounds__(Q4_THREADS, 3) void q4_attend_kernel(const void* __
         }
         __syncthreads();
         for (int y = tid; y < heads * RA_D; y += Q4_THREADS)
-            if (s_last[y / RA_D]) rec_finish<true>(partials + (head0 + y / RA_D) * P * REC_FLOATS, nS, nG, head0 + y / RA_D, y % RA_D, o);
+            if (s_last[y / RA_D]) rec_finish<true>(partials + (head0 + y / RA_D) * P * REC_FLOATS, nS, nG, head0 + y / RA_D, y % RA_D, 1.f, o);
     }
 }
 
@@ -601,11 +601,11 @@ __global__ __launch_bounds__(RA_D * SLICES) void q4_merge_kernel(const float* __
     const float* rec = partials + head * (nS + nG) * REC_FLOATS;
     const int d = threadIdx.x % RA_D, slice = threadIdx.x / RA_D;
     if constexpr (SLICES == 1) {
-        rec_finish<false>(rec, nS, nG, head, d, o);
+        rec_finish<false>(rec, nS, nG, head, d, 1.f, o);
     } else {
         __shared__ RecSum s_part[SLICES][2][RA_D];
-        s_part[slice][0][d] = rec_add_up<false>(rec, slice, nS, SLICES, d);
-        s_part[slice][1][d] = rec_add_up<false>(rec, nS + slice, nS + nG, SLICES, d);
+        s_part[slice][0][d] = rec_add_up<false>(rec, slice, nS, SLICES, d, 1.f);
+        s_part[slice][1][d] = rec_add_up<false>(rec, nS + slice, nS + nG, SLICES, d, 1.f);
         __syncthreads();
         if (slice) return;
         RecSum set[2];
@@ -623,7 +623,7 @@ __global__ __launch_bounds__(RA_D * SLICES) void q4_merge_kernel(const float* __
             }
             set[i] = x;
         }
-        rec_write(set, head, d, o);
+        rec_write(set, head, d, 1.f, o);
     }
 }
 
@@ -678,10 +678,10 @@ size_t ra_full_q4_partial_floats(ra_dtype dt, int n_seq, int n_q, int n_kv, int6
 
 #define Q4_FEW_RECORDS 32
 ra_status ra_launch_full_merge(const float* partials, int n_seq, int n_q, int n_kv, int64_t N, const int32_t* n_tokens, int tiles, int unit_log2,
-                               int heads, int workgroups, hipStream_t st, float* out, float* lse) {
+                               int heads, int workgroups, float unit, hipStream_t st, float* out, float* lse) {
 #define Q4_MERGE(THREADS, DIMS)                                                                                                                  \
     hipLaunchKernelGGL((q4_full_merge_kernel<THREADS, DIMS>), dim3(n_seq * n_q * (RA_D / DIMS)), dim3(THREADS), 0, st, partials, n_seq, n_q, n_kv, \
-                       (int)N, n_tokens, tiles, unit_log2, heads, workgroups, out, lse)
+                       (int)N, n_tokens, tiles, unit_log2, heads, workgroups, unit, out, lse)
     // records per head, were all sequences as long as the longest
     if (workgroups / (n_seq * n_kv * tiles) > Q4_FEW_RECORDS) Q4_MERGE(512, 32);
     else if ((int64_t)n_seq * n_q <= 1024) Q4_MERGE(512, RA_D);
@@ -702,7 +702,7 @@ ra_status ra_launch_full_q4(const void* q, ra_dtype dt, const Q4Cache& c, int n_
 #undef Q4_GO
     RA_HIP(hipGetLastError());
     if (x.whole) return RA_OK;
-    return ra_launch_full_merge(partials, n_seq, n_q, n_kv, N, n_tokens, x.tiles, x.unit_log2, q4_heads(n_q / n_kv), x.workgroups, st, out, lse);
+    return ra_launch_full_merge(partials, n_seq, n_q, n_kv, N, n_tokens, x.tiles, x.unit_log2, q4_heads(n_q / n_kv), x.workgroups, 1.f, st, out, lse);
 }
 
 // W = [0, s) u [w, N) of Sec. 3.3, with what came after the index was built; ranges that meet make everything static

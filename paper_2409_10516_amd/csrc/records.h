@@ -3,7 +3,9 @@
 #pragma once
 #include "common.h"
 
-#define REC_FLOATS (RA_D + 4)           // floats of a record of a set's part: sums, maximum (of z log2(e)), sum of weights, 2 pad
+#define REC_FLOATS (RA_D + 4)           // floats of a record of a set's part: sums, maximum, sum of weights, 2 pad
+// A record's maximum is in units whose multiple by `unit` is z log2(e): those of z log2(e) itself (1), or of the products <q, k>. What is combined takes
+// differences of maxima first and then the multiple, so that in units of exact products equal logits have equal weights however large they are.
 #define REC_LN2 0.6931471805599453f
 #define ROW_LEAST_UNITS 2u           // units that are worth a workgroup
 #define ROW_MOST_WORKGROUPS 768      // three per compute unit
@@ -131,7 +133,7 @@ __device__ __forceinline__ float rec_get(const float* p) {
 // Dimension d of a head's records [first, last), every `by`th: their maximum, sum of weights and weighted sum.
 struct RecSum { float m, l, a; };
 template <bool COHERENT>
-__device__ __forceinline__ RecSum rec_add_up(const float* rec, int first, int last, int by, int d) {
+__device__ __forceinline__ RecSum rec_add_up(const float* rec, int first, int last, int by, int d, float unit) {
     constexpr int FLY = 8;
     RecSum x{-INFINITY, 0.f, 0.f};
     for (int i0 = first; i0 < last; i0 += FLY * by) {
@@ -146,13 +148,13 @@ __device__ __forceinline__ RecSum rec_add_up(const float* rec, int first, int la
 #pragma unroll
         for (int u = 0; u < FLY; ++u) mx = fmaxf(mx, m[u]);
         if (mx == -INFINITY) continue;
-        const float corr = __builtin_amdgcn_exp2f(x.m - mx);
+        const float corr = __builtin_amdgcn_exp2f((x.m - mx) * unit);
         x.a *= corr;
         x.l *= corr;
 #pragma unroll
         for (int u = 0; u < FLY; ++u) {
             const bool is = i0 + u * by < last;             // (a trip that is not full reads its first record again, whose sum may be infinite)
-            const float w = __builtin_amdgcn_exp2f(m[u] - mx);
+            const float w = __builtin_amdgcn_exp2f((m[u] - mx) * unit);
             x.a = fmaf(is ? a[u] : 0.f, w, x.a);
             x.l = fmaf(is ? l[u] : 0.f, w, x.l);
         }
@@ -161,29 +163,29 @@ __device__ __forceinline__ RecSum rec_add_up(const float* rec, int first, int la
     return x;
 }
 // Eq. 4 for the static set and for Omega, Eq. 5 for both
-__device__ __forceinline__ void rec_write(const RecSum (&set)[2], size_t head, int d, const SetOut& o) {
+__device__ __forceinline__ void rec_write(const RecSum (&set)[2], size_t head, int d, float unit, const SetOut& o) {
     float* o_set[2] = {o.o_w, o.o_om};
     float* l_set[2] = {o.lse_w, o.lse_om};
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const bool empty = set[i].m == -INFINITY;
         if (o_set[i]) o_set[i][head * RA_D + d] = empty ? 0.f : set[i].a / set[i].l;
-        if (l_set[i] && d == 0) l_set[i][head] = empty ? -INFINITY : set[i].m * REC_LN2 + logf(set[i].l);
+        if (l_set[i] && d == 0) l_set[i][head] = empty ? -INFINITY : set[i].m * unit * REC_LN2 + logf(set[i].l);
     }
     const float mx = fmaxf(set[0].m, set[1].m);
     float out = 0.f, lse = -INFINITY;
     if (mx > -INFINITY) {
-        const float e0 = __builtin_amdgcn_exp2f(set[0].m - mx), e1 = __builtin_amdgcn_exp2f(set[1].m - mx);
+        const float e0 = __builtin_amdgcn_exp2f((set[0].m - mx) * unit), e1 = __builtin_amdgcn_exp2f((set[1].m - mx) * unit);
         const float l = set[0].l * e0 + set[1].l * e1;
         out = (set[0].a * e0 + set[1].a * e1) / l;
-        lse = mx * REC_LN2 + logf(l);
+        lse = mx * unit * REC_LN2 + logf(l);
     }
     o.out[head * RA_D + d] = out;
     if (d == 0) o.lse[head] = lse;
 }
 // dimension d of a head from its records, nS of the static set and nG of Omega
 template <bool COHERENT>
-__device__ __forceinline__ void rec_finish(const float* rec, int nS, int nG, size_t head, int d, const SetOut& o) {
-    const RecSum set[2] = {rec_add_up<COHERENT>(rec, 0, nS, 1, d), rec_add_up<COHERENT>(rec, nS, nS + nG, 1, d)};
-    rec_write(set, head, d, o);
+__device__ __forceinline__ void rec_finish(const float* rec, int nS, int nG, size_t head, int d, float unit, const SetOut& o) {
+    const RecSum set[2] = {rec_add_up<COHERENT>(rec, 0, nS, 1, d, unit), rec_add_up<COHERENT>(rec, nS, nS + nG, 1, d, unit)};
+    rec_write(set, head, d, unit, o);
 }
