@@ -50,7 +50,15 @@ template <int DT>
 struct PgChunk {
     pg_u32x4 k[PG_PIECES<DT>], v[PG_PIECES<DT>];             // piece r of rows 4 kg + i at [i], float32: pieces r and 16 + r at [2 i] and [2 i + 1]
     uint32_t there;             // bit j: the lane's row j of v is one that is attended
+    uint64_t at[4];             // where the lane's rows of v are: bytes from the first, or (consecutive rows) the address of the first and bytes from there
 };
+
+// between what lanes of a wavefront store and others of it read, and the next stores there: the hardware keeps the wavefront's order, this keeps
+// the compiler's
+__device__ __forceinline__ void pg_wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
 
 template <int DT>
 struct PgWave {
@@ -71,15 +79,22 @@ struct PgWave {
         l = 0.f;
     }
 
-    // `stage`: a chunk's keys in shared memory. ONE: the rows are head `head`'s alone, and other heads' sums stay as they are, whatever the rows hold.
-    template <bool ONE>
-    __device__ __forceinline__ void add(const PgChunk<DT>& c, pg_u32x4* stage, int lane, int head = 0) {
+    // `stage`: a chunk's keys in shared memory. `values` asks for the chunk's, with the keys, or (LATE) when these are in shared memory
+    // (us, with the keys and later: 65536 float32 rows of 8 heads 106, 102, 128 float32 jobs of 1000 rows 33.7, 32.2, 128 sparse float32 jobs 39.4, 37.4; 64
+    // and 128 bfloat16 jobs whose static rows' values come so 13.9, 13.6 and 18.6, 18.0, but 8 with 30000 static rows 36.4, 40.1). ONE: the rows are head
+    // `head`'s alone, and other heads' sums stay as they are, whatever the rows hold.
+    template <bool ONE, bool LATE, class F>
+    __device__ __forceinline__ void add(PgChunk<DT>& c, F values, pg_u32x4* stage, int lane, int head = 0) {
         const int kg = lane >> 4, r = lane & 15;
+        if (!LATE) values(c);
+        pg_wave_sync();                                     // (the chunk before has been read)
 #pragma unroll
         for (int j = 0; j < PIECES; ++j) {
             const int row = 4 * kg + j / (PIECES / 4), piece = 16 * (j % (PIECES / 4)) + r;
             stage[row * (PG_ROW<DT> / 16) + (piece ^ row)] = c.k[j];
         }
+        pg_wave_sync();
+        if (LATE) values(c);
         pg_f32x4 S[PIECES / 2] = {};        // (several sums: fewer roundings one after another, and an instruction waits for the one before it)
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
@@ -177,6 +192,7 @@ __device__ __forceinline__ void pg_leave(const PgWave<DT>& s, PgLds<WAVES>& lds,
     const int kg = lane >> 4, col = lane & 15;
     float l = s.l + __uint_as_float(lane_xor32<16>(__float_as_uint(s.l), lane));
     l += __uint_as_float(lane_xor32<32>(__float_as_uint(l), lane));
+    pg_wave_sync();                                         // (the last chunk's keys, in whose place the sums go, have been read)
     if (col >= n) return;
     // a sum that is not a number keeps a maximum that is one, or it would count as empty
     if (kg == 0) {
@@ -250,14 +266,26 @@ __device__ __forceinline__ void pg_fetch(PgChunk<DT>& c, const PgRows<DT>& src, 
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int n = __shfl(number, 4 * kg + j);
-        const uint64_t at = row(n) + 16 * r;
+        c.at[j] = row(n) + 16 * r;
         c.there |= (n >= 0 ? 1u : 0u) << j;
 #pragma unroll
-        for (int h = 0; h < PG_PIECES<DT> / 4; ++h) {
-            c.k[PG_PIECES<DT> / 4 * j + h] = pg_load<ONCE>(src.k + at + 256 * h);
-            c.v[PG_PIECES<DT> / 4 * j + h] = pg_load<ONCE>(src.v + at + 256 * h);
-        }
+        for (int h = 0; h < PG_PIECES<DT> / 4; ++h) c.k[PG_PIECES<DT> / 4 * j + h] = pg_load<ONCE>(src.k + c.at[j] + 256 * h);
     }
+}
+template <bool ONCE, int DT>
+__device__ __forceinline__ void pg_values(PgChunk<DT>& c, const PgRows<DT>& src) {
+#pragma unroll
+    for (int j = 0; j < PG_PIECES<DT>; ++j) c.v[j] = pg_load<ONCE>(src.v + c.at[j / (PG_PIECES<DT> / 4)] + j % (PG_PIECES<DT> / 4) * 256);
+}
+
+// a lane's pieces of consecutive rows, its first `by` behind the scalar `base`
+template <int DT>
+__device__ __forceinline__ void pg_consecutive(pg_u32x4 (&x)[PG_PIECES<DT>], uint64_t base, uint32_t by) {
+    typedef const __attribute__((address_space(1))) char* at_t;
+#pragma unroll
+    for (int j = 0; j < PG_PIECES<DT>; ++j)
+        x[j] = __builtin_nontemporal_load(reinterpret_cast<const __attribute__((address_space(1))) pg_u32x4*>(
+            reinterpret_cast<at_t>(base) + (by + j / (PG_PIECES<DT> / 4) * PG_ROW<DT> + j % (PG_PIECES<DT> / 4) * 256)));
 }
 
 // A chunk of consecutive rows from `row` on, a multiple of 16 and the same in all lanes, in a page of 16 rows or more: what differs
@@ -269,15 +297,10 @@ __device__ __forceinline__ void pg_fetch(PgChunk<DT>& c, const PgRows<DT>& src, 
     const uint64_t at = (uint64_t)(uint32_t)(n < 0 ? 0 : n) * PG_ROW<DT>;
     uint64_t k_at = (uint64_t)src.k + at, v_at = (uint64_t)src.v + at;
     asm("" : "+s"(k_at), "+s"(v_at));                        // (a scalar base and a lane's place: left to itself the compiler adds them up in vector registers)
-    typedef const __attribute__((address_space(1))) char* at_t;
-    auto load = [](uint64_t base, uint32_t by) {
-        return __builtin_nontemporal_load(reinterpret_cast<const __attribute__((address_space(1))) pg_u32x4*>(reinterpret_cast<at_t>(base) + by));
-    };
+    c.at[0] = v_at;
+    c.at[1] = mine;
     c.there = 0u;
-#pragma unroll
-    for (int j = 0; j < PG_PIECES<DT>; ++j) c.k[j] = load(k_at, mine + j / (PG_PIECES<DT> / 4) * PG_ROW<DT> + j % (PG_PIECES<DT> / 4) * 256);
-#pragma unroll
-    for (int j = 0; j < PG_PIECES<DT>; ++j) c.v[j] = load(v_at, mine + j / (PG_PIECES<DT> / 4) * PG_ROW<DT> + j % (PG_PIECES<DT> / 4) * 256);
+    pg_consecutive<DT>(c.k, k_at, mine);
 #pragma unroll
     for (int j = 0; j < 4; ++j) c.there |= (n >= 0 && row + 4 * kg + j < to ? 1u : 0u) << j;
 }
@@ -348,14 +371,14 @@ __global__ __launch_bounds__(PG_WAVES * RA_WAVE, DT == RA_BF16 ? 4 : 2) void pg_
             for (int number_of = number(row); row < to; row += step) {
                 const int next = number(row + step);         // (asked for first: loads come back in order)
                 pg_fetch<true>(a, src, number_of, lane);
-                s.template add<false>(a, lds.stage(wv), lane);
+                s.template add<false, DT == RA_F32>(a, [&](PgChunk<DT>& c) { pg_values<true>(c, src); }, lds.stage(wv), lane);
                 number_of = next;
             }
         } else {
             for (int next = src.page_of(row); row < to; row += step) {
                 pg_fetch(a, src, next, row, to, lane);
                 next = src.page_of(row + step);
-                s.template add<false>(a, lds.stage(wv), lane);
+                s.template add<false, DT == RA_F32>(a, [](PgChunk<DT>& c) { pg_consecutive<DT>(c.v, c.at[0], (uint32_t)c.at[1]); }, lds.stage(wv), lane);
             }
         }
         const size_t places = (size_t)gridDim.x + (size_t)n_seq * jobs, place = (size_t)wg + (size_t)seq * jobs + job;
@@ -577,13 +600,14 @@ __global__ __launch_bounds__(WAVES * RA_WAVE, DT == RA_BF16 ? 4 : 2) void pg_att
     st.start(reinterpret_cast<const char*>(q) + head0 * PG_ROW<DT>, heads, lane);
     if (EARLY) __syncthreads();
     PgChunk<DT> a;
+    auto values = [&](PgChunk<DT>& c) { pg_values<false>(c, src); };
     // What leads to the next chunk's rows, their entries of the table and before these the ids, is asked for ahead of the current chunk's rows:
     // loads come back in order, and who waits for one behind the rows waits for the rows.
     if (!om) {
         for (; i < chunks; i += step) {
             const int next = w_row_of(i + step), next_page = src.page_of(next);
             pg_fetch<false>(a, src, (w0 + i) * PG_CHUNK + r < set.count ? src.number(page, row) : -1, lane);
-            st.template add<false>(a, lds.stage(wv), lane);
+            st.template add<false, true>(a, values, lds.stage(wv), lane);
             row = next;
             page = next_page;
         }
@@ -593,7 +617,7 @@ __global__ __launch_bounds__(WAVES * RA_WAVE, DT == RA_BF16 ? 4 : 2) void pg_att
         for (int next = i + step < chunks ? id_of(i + step) : -1; i < chunks; i += step) {
             const int next_page = page_of(next), after = id_of(i + 2 * step);
             pg_fetch<false>(a, src, row >= set.s && row < set.w ? src.number(page, row) : -1, lane);      // (members of W are attended there)
-            st.template add<true>(a, lds.stage(wv), lane, (g0 + i) / per_head);
+            st.template add<true, DT == RA_F32>(a, values, lds.stage(wv), lane, (g0 + i) / per_head);
             row = next;
             next = after;
             page = next_page;
