@@ -390,7 +390,8 @@ ra_status ra_gather_paged(const ra_paged_cache* cache, int values, int64_t T, in
 /* ra_full_attention over a cache in pages: q [n_seq][n_q_heads][128] of type dt; rows [0, n) of sequence s that have a page, n =
  * min(n_tokens[s], N) (device int32; NULL: N for every sequence), N <= table_pages page. A sequence without rows gets out = 0 and
  * lse = -inf. Other rows are not looked at, whatever they hold. float32 accumulation; the weights of the softmax meet the values with all
- * their 24 bits. With bfloat16, infinite values in rows that are attended come out as NaN.
+ * their 24 bits. An infinite value in a row that is attended makes its dimension infinite, NaN where both infinities meet or where the row's
+ * weight is below 2^-126 of the largest. Sums are divided at the end: of n values above 2^119 / n they may be infinite.
  * RA_EUNSUP from 2^23 tiles of up to 16 query heads of a KV head on, over N > 2^24 tokens from 2^21 on.
  * workspace: device memory of at least ra_full_attention_paged_workspace_bytes(...) bytes, 16-byte aligned, which nothing else may use
  * until the call has run; it needs no initialisation. */

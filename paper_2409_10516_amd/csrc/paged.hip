@@ -23,6 +23,7 @@ template <int DT> constexpr int PG_PIECES = PG_ROW<DT> / 64;                    
 
 typedef __bf16 pg_bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 pg_bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 pg_f16x2 __attribute__((ext_vector_type(2)));
 typedef short pg_s16x4 __attribute__((ext_vector_type(4)));
 typedef float pg_f32x4 __attribute__((ext_vector_type(4), may_alias));
 typedef uint32_t pg_u32x4 __attribute__((ext_vector_type(4), may_alias));
@@ -38,8 +39,10 @@ typedef uint32_t pg_u32x4 __attribute__((ext_vector_type(4), may_alias));
 // bytes of each of 16 rows an instruction, half of a line is fetched again where rows are not kept (65536 float32 rows of 8 heads 124 us a call,
 // this way 103; bfloat16 96, 94).
 // bfloat16: v_mfma_f32_16x16x32_bf16 for the logits, sums of exact products, and v_mfma_f32_16x16x16_bf16 for the sums. A float32 weight
-// goes in as three terms of bfloat16, the first as rounded, the next what the rounding left: all of its 24 bits. (An infinite value times the
-// lesser terms is not a number.)
+// goes in as three terms of bfloat16, the first as rounded, the next what the rounding left: all of its 24 bits. Infinite values meet the first
+// alone, or zero times infinity, or infinities of both signs, would be what is added up. Whether a chunk has one is asked with eight instructions: what has all bits of a
+// bfloat16 exponent set is no number when it is read as float16 (so are values above 2^121, which lose nothing), and the maximum of float16 keeps that. (It costs 0 to 2 %; with
+// masks and integer maxima, 31 instructions, 1 to 4 %; all rows again where a sum is no number, by a flag, 0 to 20 %, as registers run out.)
 // float32: v_mfma_f32_16x16x4_f32, products and sums in float32.
 // The running maximum of a head moves only when a logit exceeds it by more than 8 (in powers of two), which keeps the
 // lanes' exchange and the scaling of sums out of nearly every chunk.
@@ -142,22 +145,38 @@ struct PgWave {
                 }
                 P[t] = __builtin_bit_cast(pg_s16x4, (uint64_t)pair[1] << 32 | pair[0]);
             }
+            uint32_t a[8][2];                                // dimension i of the lane's 8, of rows 0 and 1, 2 and 3
+            pg_f16x2 odd = {0, 0};                           // no number in a half: values may be infinite
 #pragma unroll
-            for (int y = 0; y < 4; ++y) {                    // dimensions 2 y and 2 y + 1 of the lane's 8, which share a word of every row
+            for (int y = 0; y < 4; ++y) {                    // dimensions 2 y and 2 y + 1 share a word of every row
                 uint32_t w[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) w[j] = (c.there >> j) & 1u ? c.v[j][y] : 0u;          // (0 * NaN is not 0)
 #pragma unroll
-                for (int o = 0; o < 2; ++o) {
-                    const uint32_t half = o ? 0x07060302u : 0x05040100u;
-                    const pg_s16x4 a = __builtin_bit_cast(pg_s16x4, (uint64_t)__builtin_amdgcn_perm(w[3], w[2], half) << 32 |
-                                                                    __builtin_amdgcn_perm(w[1], w[0], half));
-                    pg_f32x4 sum = acc[2 * y + o];
+                for (int j = 0; j < 4; ++j) odd = __builtin_elementwise_maximum(odd, __builtin_bit_cast(pg_f16x2, w[j]));
 #pragma unroll
-                    for (int t = 2; t >= 0; --t) sum = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, P[t], sum, 0, 0, 0);
-                    acc[2 * y + o] = mine ? sum : acc[2 * y + o];
-                }
+                for (int i = 0; i < 4; ++i) a[2 * y + i / 2][i % 2] = __builtin_amdgcn_perm(w[i % 2 * 2 + 1], w[i % 2 * 2], i / 2 ? 0x07060302u : 0x05040100u);
             }
+            auto rows = [&](int i) { return __builtin_bit_cast(pg_s16x4, (uint64_t)a[i][1] << 32 | a[i][0]); };
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const pg_f32x4 sum = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(rows(i), P[0], acc[i], 0, 0, 0);
+                acc[i] = mine ? sum : acc[i];
+            }
+            // what is infinite or no number has met the first terms
+            if (__builtin_amdgcn_ballot_w64(odd[0] != odd[0] || odd[1] != odd[1]) != 0ull) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        if ((a[i][j] & 0x7f80u) == 0x7f80u) a[i][j] &= 0xffff0000u;
+                        if ((a[i][j] & 0x7f800000u) == 0x7f800000u) a[i][j] &= 0xffffu;
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)                      // (of heads that are not `mine` these terms are zero)
+#pragma unroll
+                for (int t = 1; t < 3; ++t) acc[i] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(rows(i), P[t], acc[i], 0, 0, 0);
         } else {
 #pragma unroll
             for (int h = 0; h < 2; ++h)

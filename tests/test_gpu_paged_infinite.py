@@ -5,7 +5,7 @@ import torch
 
 import paper_2409_10516_amd as ra
 from oracle import attention as OA, paged as OP
-from tests.test_gpu_paged import DEV, Cache, check, ints, queries
+from tests.test_gpu_paged import DEV, TYPES, Cache, check, ints, queries
 from tests.util import to_np
 
 pytestmark = pytest.mark.gpu
@@ -31,7 +31,7 @@ def _put(c, s, kv, rows, dims):
         c.V[int(c.table[s][r // c.page]), kv, r % c.page, d] = float("inf") if i % 2 else -float("inf")
 
 
-@pytest.mark.parametrize("dtype", [torch.float32])
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("page", [4, 16, 64])
 @pytest.mark.parametrize("n,n_q", [(1, 2), (16, 2), (300, 2), (300, 17), (5003, 2)])
 def test_full_attention(dtype, page, n, n_q):
@@ -50,7 +50,7 @@ def test_full_attention(dtype, page, n, n_q):
             _check(out[s, h], lse[s, h], to_np(q[s, h]), *c.rows(s, 0, range(c.lens[s]))) if c.lens[s] else None
 
 
-@pytest.mark.parametrize("dtype", [torch.float32])
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("n_seq,window", [(1, 40), (1, 100), (1, 700), (20, 300), (130, 100), (130, 700)])
 def test_sparse_and_static_attention(dtype, n_seq, window):
     """In either set, whether a job is one workgroup's or several whose records fill the trips of what combines them, or do not."""
@@ -71,3 +71,16 @@ def test_sparse_and_static_attention(dtype, n_seq, window):
             W, om = OP.sets(n, n, 4, window, ids[s, h].tolist())
             for (o, l), rows in zip((got[0:2], got[2:4], got[4:6]), (np.concatenate([W, om]), om, W)):
                 _check(o[s, h], l[s, h], to_np(q[s, h]), *c.rows(s, h // 4, rows.tolist()))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_the_largest_values(dtype):
+    """A row by itself has a weight of one and comes out as it is, whatever its values."""
+    most = torch.finfo(dtype).max
+    V = torch.tensor([most, -most, 2.0 ** 121, 2.0 ** 121 * 1.25, -(2.0 ** 127), 2.0 ** -126, float("inf"), -float("inf")], dtype=dtype).repeat(16)
+    K, V = torch.ones((1, 1, 16, 128), dtype=dtype, device=DEV), V.to(DEV).expand(1, 1, 16, 128).contiguous()
+    cache = ra.PagedCache(K, V, ints([[0]]))
+    q = queries(1, 3, dtype, 1).to(DEV)
+    ids = ints([[[0]]]).expand(1, 3, 1).contiguous()
+    for out, _ in (ra.ra_full_attention_paged(q, cache, N=1), ra.ra_attend_paged(q, cache, 1, 0, ids, N=1), ra.ra_attend_paged(q, cache, 0, 0, ids, N=1)):
+        assert torch.equal(out, V[0, 0, :1].float().expand(1, 3, 128))
