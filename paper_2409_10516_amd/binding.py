@@ -841,10 +841,16 @@ class PagedCache:
         return self._ref
 
 
+def _is_paged(cache) -> None:
+    if not isinstance(cache, PagedCache):
+        raise TypeError(f"cache must be a PagedCache, not {type(cache).__name__}")
+
+
 def ra_append_tokens_paged(q, k, v, first, cache: PagedCache, *, n_new=None, q_weight=None, k_weight=None, eps: float = 1e-6, inv_freq=None,
                            interleaved: bool = False, rot_scale: float = 1.0, q_out=None, stream=None):
     """ra_append_tokens into a cache in pages; cosines and sines times rot_scale. k and v may be None: nothing of K or V is
     written. -> q_out [n_seq][n_q][T][128] (None without q), as there."""
+    _is_paged(cache)
     if stream is None:
         got = _short.append(q, k, v, first, cache._core, n_new, q_weight, k_weight, eps, inv_freq, interleaved, rot_scale, q_out)
         if got.__class__ is tuple:
@@ -895,6 +901,7 @@ def ra_append_tokens_paged(q, k, v, first, cache: PagedCache, *, n_new=None, q_w
 def ra_gather_paged(cache: PagedCache, values: bool = False, first=None, rows: Optional[int] = None, out=None, stream=None):
     """Rows first[s] .. first[s] + rows (None: from 0, all that the table has entries for) of K, or with `values` of V, side by side
     -> [n_seq][n_kv][rows][128]; rows without a page are zero."""
+    _is_paged(cache)
     if stream is None:
         got = _short.gather(cache._core, values, first, rows, out)
         if got.__class__ is tuple:
@@ -954,6 +961,7 @@ def _full_paged_room(dt: int, n_seq: int, n_q: int, n_kv: int, N: int) -> int:
 def ra_full_attention_paged(q, cache: PagedCache, n_tokens=None, N: Optional[int] = None, stream=None, workspace=None, out=None, lse=None):
     """Eq. 1 over the first n_tokens[s] rows (int32 [n_seq] on the GPU, at most N; None: N, by default cache.rows) of every sequence of a
     cache in pages, those that have a page -> (out float32 [n_seq][n_q][128], lse float32 [n_seq][n_q])."""
+    _is_paged(cache)
     if stream is None:
         got = _short.full(q, cache._core, n_tokens, N, workspace, out, lse)
         if got.__class__ is tuple:
@@ -983,6 +991,7 @@ def ra_attend_paged(q, cache: PagedCache, sink: int, window: int, ids: torch.Ten
     """ra_attend over a cache in pages, of n_tokens[s] rows (int32 [n_seq] on the GPU, at most N; None: N, by default cache.rows), the first
     n_indexed[s] of which (None: all) an index was built over; those behind are static. ids in the static set are
     skipped. -> (out, lse) or, with partials=True, (out, lse, o_omega, lse_omega, o_w, lse_w)."""
+    _is_paged(cache)
     if stream is None and not partials:
         got = _short.attend(q, cache._core, sink, window, ids, n_tokens, n_indexed, N, workspace, out, lse)
         if got.__class__ is tuple:
