@@ -18,6 +18,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 # RA_LIBRARY names another build of the same library (a tuning build, say); default: the in-tree one
 LIB_PATH = os.environ.get("RA_LIBRARY") or os.path.join(_HERE, "libra.so")
+CALLS_PATH = os.path.join(_HERE, "_calls.so")
 
 RA_F32, RA_BF16 = 0, 1
 RA_CFG_HELPERS, RA_CFG_HELPER_SPIN, RA_CFG_SEEDS, RA_CFG_SEED_SHARES = 0, 1, 2, 3
@@ -776,14 +777,16 @@ _short = None
 
 def _calls():
     """Load _calls.so (once): the calls around a cache in pages made and checked by compiled code, with the same outcome, where nothing is
-    out of the ordinary; else they return None."""
+    out of the ordinary; else they return None. None where it has not been built: the checks below are all there are then."""
     global _short
     if _short is None:
         L = lib()
+        if not os.path.exists(CALLS_PATH):
+            return None
         try:
             from . import _calls as m
         except ImportError as e:
-            raise RuntimeError("_calls.so is missing or broken: build it as libra.so") from e
+            raise RuntimeError("_calls.so is broken: build it as libra.so") from e
         at = [C.cast(f, C.c_void_p).value for f in (L.ra_append_tokens_paged, L.ra_gather_paged, L.ra_full_attention_paged,
                                                     L.ra_full_attention_paged_workspace_bytes, L.ra_attend_paged, L.ra_attend_paged_workspace_bytes)]
         m.bind(_RAW or (lambda here: torch.cuda.current_stream(here).cuda_stream), *at)
@@ -819,7 +822,8 @@ class PagedCache:
         self._at = tuple((t.data_ptr, t.data_ptr()) for t in (K, V, table) if t is not None)
         self._c = _PagedCache(_ptr(K), _ptr(V), table.data_ptr(), stride, dt, table.shape[0], shape[1], shape[0], shape[2], table.shape[1])
         self._ref = C.byref(self._c)
-        self._core = _calls().cache(K, V, table, C.addressof(self._c), self._here)
+        short = _calls()
+        self._core = short.cache(K, V, table, C.addressof(self._c), self._here) if short else None
         self._dt, self._dtype, self._n_seq, self._n_kv, self._rows = dt, some.dtype, table.shape[0], shape[1], table.shape[1] * shape[2]
 
     K = property(lambda s: s._K)
@@ -851,7 +855,7 @@ def ra_append_tokens_paged(q, k, v, first, cache: PagedCache, *, n_new=None, q_w
     """ra_append_tokens into a cache in pages; cosines and sines times rot_scale. k and v may be None: nothing of K or V is
     written. -> q_out [n_seq][n_q][T][128] (None without q), as there."""
     _is_paged(cache)
-    if stream is None:
+    if stream is None and cache._core is not None:
         got = _short.append(q, k, v, first, cache._core, n_new, q_weight, k_weight, eps, inv_freq, interleaved, rot_scale, q_out)
         if got.__class__ is tuple:
             return got[0]
@@ -902,7 +906,7 @@ def ra_gather_paged(cache: PagedCache, values: bool = False, first=None, rows: O
     """Rows first[s] .. first[s] + rows (None: from 0, all that the table has entries for) of K, or with `values` of V, side by side
     -> [n_seq][n_kv][rows][128]; rows without a page are zero."""
     _is_paged(cache)
-    if stream is None:
+    if stream is None and cache._core is not None:
         got = _short.gather(cache._core, values, first, rows, out)
         if got.__class__ is tuple:
             return got[0]
@@ -962,7 +966,7 @@ def ra_full_attention_paged(q, cache: PagedCache, n_tokens=None, N: Optional[int
     """Eq. 1 over the first n_tokens[s] rows (int32 [n_seq] on the GPU, at most N; None: N, by default cache.rows) of every sequence of a
     cache in pages, those that have a page -> (out float32 [n_seq][n_q][128], lse float32 [n_seq][n_q])."""
     _is_paged(cache)
-    if stream is None:
+    if stream is None and cache._core is not None:
         got = _short.full(q, cache._core, n_tokens, N, workspace, out, lse)
         if got.__class__ is tuple:
             return got
@@ -992,7 +996,7 @@ def ra_attend_paged(q, cache: PagedCache, sink: int, window: int, ids: torch.Ten
     n_indexed[s] of which (None: all) an index was built over; those behind are static. ids in the static set are
     skipped. -> (out, lse) or, with partials=True, (out, lse, o_omega, lse_omega, o_w, lse_w)."""
     _is_paged(cache)
-    if stream is None and not partials:
+    if stream is None and not partials and cache._core is not None:
         got = _short.attend(q, cache._core, sink, window, ids, n_tokens, n_indexed, N, workspace, out, lse)
         if got.__class__ is tuple:
             return got
