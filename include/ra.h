@@ -404,6 +404,9 @@ ra_status ra_full_attention_paged(const void* q, const ra_paged_cache* cache, in
  * with n = min(n_tokens[s], N) and n_i = min(n_indexed[s], n) (device int32; NULL: N, and n) W = [0, sink) u [min(n - window, n_i), n):
  * tokens behind the n_i that the index was built over are static. Entries of ids that are not in [0, n), or are members of W (they are
  * attended there), are skipped; one that is given twice counts twice. Rows without a page are not attended. Weights and infinite values as above.
+ * The work is cut by sink, window and topk; tokens behind the n_i are not known to the host, and where there are many of them beside a small window
+ * or few ids, or in one sequence of a batch of 128 KV heads or more, few workgroups have them all (30000 of one sequence of 8 KV heads: window 640, topk 100
+ * 40 us, window 64, topk 16 150 us; of one sequence among 16 286 us, where none has grown 18 us). ra_full_attention_paged is not cut so.
  * RA_EUNSUP past 65535 sequences, 65535 tiles of up to 16 query heads of a KV head, or 2^22 - 1 of both.
  * workspace: as above, of ra_attend_paged_workspace_bytes(...) bytes. */
 size_t ra_attend_paged_workspace_bytes(ra_dtype dt, int n_seq, int n_q_heads, int n_kv_heads, int64_t N, int sink, int window, int topk);

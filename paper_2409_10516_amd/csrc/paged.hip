@@ -557,8 +557,9 @@ __device__ __forceinline__ PgSets pg_sets(int lens, bool has_tokens, bool has_in
 // A job is a KV head of a sequence, and up to 16 of its query heads: chunks of W, for all of the heads, and of each head's Omega. It is cut into
 // `parts` workgroups, each of which takes an equal stretch of either list and shares its wavefronts out between the two.
 // They leave a record of each set per head, or, where a job is one workgroup's, the results. grid: x = part, y = KV head (with its tile), z = sequence. What bounds it is the way from the
-// lengths and ids to the table and from there to the rows, three trips, and the second launch; where jobs are many, scattered rows (256 jobs of 644
-// static rows and 4 x 100 ids, 137 MB, 34 us).
+// lengths and ids to the table and from there to the rows, three trips, and the second launch; where jobs are many, the same way of each, as a
+// workgroup has a compute unit to itself (bfloat16: 139 KB of shared memory; float32: registers for two wavefronts a SIMD) and nothing runs beside its
+// start and end (256 jobs of 644 static rows and 4 x 100 ids, 137 MB, 32 to 34 us, 128 float32 ones, 137 MB, 38).
 template <int DT, int WAVES>
 __global__ __launch_bounds__(WAVES * RA_WAVE, DT == RA_BF16 ? 4 : 2) void pg_attend_kernel(
     const void* __restrict__ q, PgCache c, const int32_t* __restrict__ table, int group, int n_kv, int N, const int32_t* __restrict__ n_tokens,
@@ -690,8 +691,9 @@ __global__ __launch_bounds__(2 * RA_D * SLICES) void pg_merge_kernel(const float
 
 // How a job is cut: half a round of chunks for a workgroup's wavefronts each, up to so many workgroups that each has a compute unit to itself
 // (us, a whole round and half of one: 8 jobs of 644 static rows and 4 x 100 ids 9.8, 9.7, with 2000 static rows 12.6, 10.6, with 30000
-// 59.5, 41.5, float32 13.9, 12.6; 16 query heads of one KV head 12.0, 13.1). Tokens that have come since the index was built are not counted, nobody
-// here knows how many they are.
+// 59.5, 41.5, float32 13.9, 12.6; 16 query heads of one KV head 12.0, 13.1). Tokens that have come since the index was built are not counted, as the host does
+// not know how many they are: a job that has grown by 30000 rows is cut by its window and ids alone (one KV head, window 0, one id, one workgroup 197 us;
+// eight, window 64, 16 ids 150, window 640, 100 ids 40; one sequence of 16, in bfloat16 a workgroup for each KV head, 286).
 // Many jobs are one workgroup's each (128 of them, bfloat16, by themselves with 16 wavefronts 18.2, with eight 19.9, in two 19.6 and a launch more;
 // 64 14.8, in four 13.5; float32, which has registers for eight wavefronts: 128 48, in two 40).
 static int pg_parts(ra_dtype dt, int n_seq, int n_q, int n_kv, int64_t N, int sink, int window, int topk, int* tiles) {
